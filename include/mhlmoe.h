@@ -456,13 +456,146 @@ mhlmoe_status mhlmoe_bias_update(const int32_t *counts, float *bias,
                                  hipStream_t stream);
 
 /*
+ * The operators around the heads: what stands between the layer and the
+ * network it is in.  8 bits are e4m3 (OCP: largest value 448, no infinities)
+ * with one float scale per block of 128 values along the contraction; a block
+ * of values v is held as
+ *
+ *   scale = max(max |v| / 448, 2^-126),   q = e4m3(v / scale), nearest even,
+ *
+ * so q * scale stands for v; the last block of a row may be shorter.  A block
+ * that holds an infinity or a NaN becomes NaN as a whole.
+ *
+ * Residual sum and root-mean-square norm, per row t of d_model columns c:
+ *
+ *   h = x + residual, rounded to dtype        (h = x where residual is NULL)
+ *   y[c] = h[c] / sqrt(mean_c' h[c']^2 + eps) * weight[c]
+ *
+ *   x        [T][d_model]  dtype                     (in)
+ *   residual [T][d_model]  dtype or NULL             (in)
+ *   weight   [d_model]     float                     (in)
+ *   sum      [T][d_model]  dtype  h, with residual only (out); may be x or
+ *            residual itself
+ *   y        [T][d_model]  dtype or NULL             (out); may be x
+ *   q        [T][d_model]  e4m3 or NULL              (out) y in 8 bits, with
+ *   scales   [T][ceil(d_model / 128)] float          (out) its scales; d_model
+ *            must be a multiple of 16
+ * y and q may both be asked for; at least one must be.  The norm is that of
+ * the rounded h, which mhlmoe_rmsnorm_backward reads.  1 <= d_model <= 65536,
+ * T < 2^31, eps finite and > 0.  Sums and the norm are in fp32.  No workspace.
+ */
+mhlmoe_status mhlmoe_rmsnorm(const void *x, const void *residual,
+                             const float *weight, int64_t T, int d_model,
+                             float eps, mhlmoe_dtype dtype, void *sum, void *y,
+                             void *q, float *scales, hipStream_t stream);
+
+/*
+ * Its gradient, with rs = 1 / sqrt(mean_c h^2 + eps) and g = dy * weight:
+ *
+ *   dx[c] = dsum[c] + rs (g[c] - h[c] rs^2 mean_c'(g[c'] h[c']))
+ *   dweight[c] = sum_t dy[c] h[c] rs
+ *
+ *   h       [T][d_model]  dtype  the forward's sum (x without residual) (in)
+ *   dy      [T][d_model]  dtype  the gradient of y                      (in)
+ *   dsum    [T][d_model]  dtype or NULL  the gradient that reaches h past the
+ *           norm (the residual stream's)                                (in)
+ *   dx      [T][d_model]  dtype  the gradient of x, and of residual    (out);
+ *           may be dy or dsum, not h
+ *   dweight [d_model]     float  overwritten; zeros where T = 0        (out)
+ * dweight is summed in a fixed order.  Workspace: the size that
+ * mhlmoe_rmsnorm_backward_workspace writes to *bytes.
+ */
+mhlmoe_status mhlmoe_rmsnorm_backward_workspace(int64_t T, int d_model,
+                                                size_t *bytes);
+mhlmoe_status mhlmoe_rmsnorm_backward(const void *h, const float *weight,
+                                      const void *dy, const void *dsum,
+                                      int64_t T, int d_model, float eps,
+                                      mhlmoe_dtype dtype, void *dx,
+                                      float *dweight, void *workspace,
+                                      size_t workspace_bytes,
+                                      hipStream_t stream);
+
+/*
+ * Quantisation of x [rows][cols] (dtype; cols a multiple of 16) in blocks of
+ * block_rows x 128: block_rows 1 gives every row its own scales (activations),
+ * 128 one scale per tile (weights).
+ *
+ *   transpose 0:  q [rows][cols] e4m3,
+ *                 scales [ceil(rows / block_rows)][ceil(cols / 128)] float
+ *   transpose 1:  x^T is quantised, its rows padded with zeros to a multiple
+ *                 of 16:  q [cols][rows16], rows16 = 16 ceil(rows / 16),
+ *                 scales [ceil(cols / block_rows)][ceil(rows / 128)]
+ * The transposed forms serve the gradients of mhlmoe_gemm_scaled: with C = A
+ * B^T, dA = dC B contracts over N and dB = dC^T A over M.  A 128 x 128 block's
+ * scale is the same either way.  rows, cols < 2^31 and fewer than 2^24 tiles
+ * of 128 x 128 (2^32 blocks of 1 x 128).  No workspace.
+ */
+mhlmoe_status mhlmoe_quantize(const void *x, int64_t rows, int64_t cols,
+                              mhlmoe_dtype dtype, int block_rows, int transpose,
+                              void *q, float *scales, hipStream_t stream);
+
+/*
+ * The 8-bit product C = A B^T with a scale per block of 128, KB = ceil(K / 128):
+ *
+ *   C[m][n] = sum_b scale_a[m][b] scale_b[n / b_block_rows][b]
+ *                   sum_{k = 128 b .. 128 b + 127} A[m][k] B[n][k]
+ *
+ *   A       [M][K] e4m3,  scale_a [M][KB] float                         (in)
+ *   B       [N][K] e4m3,  scale_b [ceil(N / b_block_rows)][KB] float    (in)
+ *   C       [M][N] out_dtype                                           (out)
+ * b_block_rows is 128 (weights quantised in tiles) or 1 (both operands
+ * quantised by rows: the weight gradient).  K must be a multiple of 16; M and
+ * N are any sizes (C's rows then need no alignment).  A block's sum is the
+ * matrix cores' (fp32), blocks are added in fp32 in a fixed order; C is
+ * rounded once.  K = 0 writes zeros.  M, N < 2^31, K < 2^24,
+ * ceil(M / 128) ceil(N / 128) < 2^24.  No workspace.
+ */
+mhlmoe_status mhlmoe_gemm_scaled(const void *A, const float *scale_a,
+                                 const void *B, const float *scale_b, int64_t M,
+                                 int64_t N, int64_t K, int b_block_rows,
+                                 mhlmoe_dtype out_dtype, void *C,
+                                 hipStream_t stream);
+
+/*
+ * mhlmoe_latent_layer for serving, behind its norm and with its projections in
+ * 8 bits (N = n_heads * d_head):
+ *
+ *   h     = x + residual (to sum); n = its RMS norm in 8 bits (mhlmoe_rmsnorm)
+ *   X_lat = n W_in^T,  R_lat = n W_r^T (W_r NULL: R_lat is X_lat)
+ *   Y_lat = the heads on X_lat, routed by R_lat (mhlmoe_layer_routed)
+ *   out   = Y_lat, quantised by rows, W_out^T
+ *
+ * bit for bit what the named calls, mhlmoe_quantize and mhlmoe_gemm_scaled
+ * give one by one.  W_in, W_r [N][d_model] and W_out [d_model][N] are e4m3 with
+ * scales per 128 x 128 tile (mhlmoe_quantize, block_rows 128); W_r gives the
+ * separate routing sub-tokens of Eq. (9).  residual and sum, X_lat, R_lat,
+ * Y_lat, idx, gate and counts are optional as in the calls themselves.
+ * d_model must be a multiple of 16 in [16, 65536].  Workspace: the size that
+ * mhlmoe_latent_layer_scaled_workspace writes to *bytes.
+ */
+mhlmoe_status mhlmoe_latent_layer_scaled_workspace(
+    int64_t T, int d_model, int n_heads, int d_head, int n_experts, int top_k,
+    int d_ff, mhlmoe_dtype dtype, size_t *bytes);
+mhlmoe_status mhlmoe_latent_layer_scaled(
+    const void *x, const void *residual, const float *norm_weight, float eps,
+    const void *W_in, const float *scale_in, const void *W_r,
+    const float *scale_r, const float *W_router, const float *bias,
+    const void *W1, const void *W3, const void *W2, const void *W_out,
+    const float *scale_out, int64_t T, int d_model, int n_heads, int d_head,
+    int n_experts, int top_k, int d_ff, mhlmoe_dtype dtype, void *out,
+    void *sum, void *X_lat, void *R_lat, void *Y_lat, int32_t *idx, float *gate,
+    int32_t *counts, void *workspace, size_t workspace_bytes,
+    hipStream_t stream);
+
+/*
  * Per-kernel timing (a measurement aid, off by default).  While enabled, each
  * kernel the library launches is bracketed by two HIP events recorded on the
  * caller's stream, so the measured interval is that kernel's execution on
  * the stream it actually runs on.  Kernel names: "route_fwd", "hist",
  * "count_scan", "scatter", "ffn", "combine", "bwd_dx", "bwd_combine",
  * "dw_plan", "bwd_dw", "router_dw", "route_bwd", "bias_update", "proj_in", "proj_out" and
- * "proj_bwd" (the projection GEMMs of the latent layer).
+ * "proj_bwd" (the projection GEMMs of the latent layer), "rmsnorm",
+ * "rmsnorm_bwd", "rmsnorm_dw", "quantize" and "gemm_scaled".
  *
  * mhlmoe_timing_enable(on)   start (on != 0) or stop recording; records
  *                            already taken are kept.

@@ -25,6 +25,9 @@ __all__ = [
     "mhlmoe_route", "mhlmoe_route_static", "mhlmoe_bucket", "mhlmoe_experts", "mhlmoe_layer",
     "mhlmoe_experts_gelu", "mhlmoe_layer_gelu",
     "mhlmoe_layer_backward", "workspace",
+    "mhlmoe_rmsnorm", "mhlmoe_rmsnorm_backward", "mhlmoe_rmsnorm_backward_workspace",
+    "mhlmoe_quantize", "mhlmoe_gemm_scaled", "mhlmoe_latent_layer_scaled",
+    "mhlmoe_latent_layer_scaled_workspace",
     "mhlmoe_timing_enable", "mhlmoe_timing_query", "mhlmoe_timing_reset",
 ]
 
@@ -84,6 +87,16 @@ def _declare(lib):
     lib.mhlmoe_latent_layer_backward.argtypes = ([_P] * 13 + [_I64] + [_I] * 8 + [_P] * 8
                                                  + [_SZ, _P])
     lib.mhlmoe_bias_update.argtypes = [_P, _P, _I, _I, ctypes.c_float, _P]
+    F = ctypes.c_float
+    lib.mhlmoe_rmsnorm.argtypes = [_P] * 3 + [_I64, _I, F, _I] + [_P] * 5
+    lib.mhlmoe_rmsnorm_backward_workspace.argtypes = [_I64, _I, ctypes.POINTER(_SZ)]
+    lib.mhlmoe_rmsnorm_backward.argtypes = [_P] * 4 + [_I64, _I, F, _I] + [_P] * 3 + [_SZ, _P]
+    lib.mhlmoe_quantize.argtypes = [_P, _I64, _I64, _I, _I, _I, _P, _P, _P]
+    lib.mhlmoe_gemm_scaled.argtypes = [_P] * 4 + [_I64] * 3 + [_I, _I, _P, _P]
+    lib.mhlmoe_latent_layer_scaled_workspace.argtypes = ([_I64] + [_I] * 7
+                                                         + [ctypes.POINTER(_SZ)])
+    lib.mhlmoe_latent_layer_scaled.argtypes = ([_P] * 3 + [F] + [_P] * 11 + [_I64] + [_I] * 7
+                                               + [_P] * 9 + [_SZ, _P])
     lib.mhlmoe_timing_enable.argtypes = [_I]
     lib.mhlmoe_timing_query.argtypes = [ctypes.c_char_p, ctypes.POINTER(ctypes.c_double),
                                         ctypes.POINTER(_I64)]
@@ -91,7 +104,10 @@ def _declare(lib):
     for name in ("mhlmoe_workspace_size", "mhlmoe_route", "mhlmoe_bucket", "mhlmoe_experts",
                  "mhlmoe_layer", "mhlmoe_layer_backward", "mhlmoe_experts_gelu",
                  "mhlmoe_layer_gelu", "mhlmoe_timing_enable",
-                 "mhlmoe_timing_query", "mhlmoe_timing_reset"):
+                 "mhlmoe_timing_query", "mhlmoe_timing_reset", "mhlmoe_rmsnorm",
+                 "mhlmoe_rmsnorm_backward", "mhlmoe_rmsnorm_backward_workspace",
+                 "mhlmoe_quantize", "mhlmoe_gemm_scaled", "mhlmoe_latent_layer_scaled",
+                 "mhlmoe_latent_layer_scaled_workspace"):
         getattr(lib, name).restype = _I
     return lib
 
@@ -547,6 +563,195 @@ def mhlmoe_layer_gelu_backward(X, W_router, W_in, W_out, idx, gate, dY, *, dX=No
         _dev(dW_in, "dW_in", f32, (Nh, Ne, dff, dh)), _dev(dW_out, "dW_out", f32, (Nh, Ne, dh, dff)),
         wsp, wsn, _stream(stream)))
     return dX, dW_router, dW_in, dW_out
+
+
+# The operators around the heads.  Their tensors must all be on one GPU, and
+# the call is enqueued there: on `stream`, or on that GPU's current stream.
+
+E4M3 = torch.float8_e4m3fn
+
+
+def _one_device(first, *others):
+    for t in others:
+        if isinstance(t, torch.Tensor) and t.device != first.device:
+            raise ValueError(f"tensors on {first.device} and {t.device}: one device is needed")
+
+
+def _launch(first, stream, call):
+    """call(stream) with the tensors' GPU as the current one."""
+    if first.device.type != "cuda" or first.device.index == torch.cuda.current_device():
+        _check(call(_stream(stream)))
+        return
+    with torch.cuda.device(first.device):
+        _check(call(_stream(stream)))
+
+
+def _rows_cols(t, name):
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must have 2 dimensions (got {t.dim()})")
+    return t.shape
+
+
+def _new(t, shape, dtype, like):
+    return t if t is not None else torch.empty(shape, dtype=dtype, device=like.device)
+
+
+def mhlmoe_rmsnorm(x, weight, eps, *, residual=None, quantized=False, sum=None, y=None, q=None,
+                   scales=None, stream=None):
+    """h = x + residual and its RMS norm.  x [T, d_model]; weight [d_model]
+    float.  quantized: the norm in 8 bits (q e4m3 and scales per 128 columns)
+    instead of y; pass y as well to have both.  Returns a dict with sum (with
+    residual), y, q and scales."""
+    T, d = _rows_cols(x, "x")
+    dt = _dtype_code(x)
+    if residual is not None:
+        sum = _new(sum, (T, d), x.dtype, x)
+    if quantized:
+        q = _new(q, (T, d), E4M3, x)
+        scales = _new(scales, (T, -(-d // 128)), torch.float32, x)
+    else:
+        if q is not None or scales is not None:
+            raise ValueError("q and scales are outputs of quantized=True")
+        y = _new(y, (T, d), x.dtype, x)
+    _one_device(x, weight, residual, sum, y, q, scales)
+    args = (_dev(x, "x"), _dev(residual, "residual", x.dtype, (T, d)),
+            _dev(weight, "weight", torch.float32, (d,)), T, d, float(eps), dt,
+            _dev(sum, "sum", x.dtype, (T, d)), _dev(y, "y", x.dtype, (T, d)),
+            _dev(q, "q", E4M3, (T, d)),
+            _dev(scales, "scales", torch.float32, (T, -(-d // 128))))
+    _launch(x, stream, lambda s: load_library().mhlmoe_rmsnorm(*args, s))
+    res = {}
+    for name, t in (("sum", sum), ("y", y), ("q", q), ("scales", scales)):
+        if t is not None:
+            res[name] = t
+    return res
+
+
+def mhlmoe_rmsnorm_backward_workspace(T: int, d_model: int) -> int:
+    """Workspace bytes of mhlmoe_rmsnorm_backward."""
+    out = _SZ(0)
+    _check(load_library().mhlmoe_rmsnorm_backward_workspace(T, d_model, ctypes.byref(out)))
+    return out.value
+
+
+def mhlmoe_rmsnorm_backward(h, weight, eps, dy, *, dsum=None, dx=None, dweight=None,
+                            workspace=None, stream=None):
+    """Backward of mhlmoe_rmsnorm from h, the forward's sum (x where there was
+    no residual): returns (dx, dweight).  dsum: the gradient that reaches h
+    past the norm; dx is the gradient of x and of residual."""
+    T, d = _rows_cols(h, "h")
+    dx = _new(dx, (T, d), h.dtype, h)
+    dweight = _new(dweight, (d,), torch.float32, h)
+    if workspace is None:
+        n = mhlmoe_rmsnorm_backward_workspace(T, d)
+        workspace = torch.empty(max(n, 256), dtype=torch.uint8, device=h.device)
+    _one_device(h, weight, dy, dsum, dx, dweight, workspace)
+    args = (_dev(h, "h"), _dev(weight, "weight", torch.float32, (d,)),
+            _dev(dy, "dy", h.dtype, (T, d)), _dev(dsum, "dsum", h.dtype, (T, d)), T, d, float(eps),
+            _dtype_code(h), _dev(dx, "dx", h.dtype, (T, d)),
+            _dev(dweight, "dweight", torch.float32, (d,)),
+            _dev(workspace, "workspace", torch.uint8), workspace.numel())
+    _launch(h, stream, lambda s: load_library().mhlmoe_rmsnorm_backward(*args, s))
+    return dx, dweight
+
+
+def mhlmoe_quantize(x, *, block_rows=1, transpose=False, q=None, scales=None, stream=None):
+    """x [rows, cols] in 8 bits with a scale per block_rows (1 or 128) x 128
+    block; with transpose, x's transpose, its rows padded with zeros to a
+    multiple of 16.  Returns (q, scales)."""
+    rows, cols = _rows_cols(x, "x")
+    a, k = (cols, -(-rows // 16) * 16) if transpose else (rows, cols)
+    grid = (-(-a // block_rows) if block_rows in (1, 128) else a, -(-k // 128))
+    q = _new(q, (a, k), E4M3, x)
+    scales = _new(scales, grid, torch.float32, x)
+    _one_device(x, q, scales)
+    args = (_dev(x, "x"), rows, cols, _dtype_code(x), int(block_rows), 1 if transpose else 0,
+            _dev(q, "q", E4M3, (a, k)), _dev(scales, "scales", torch.float32, grid))
+    _launch(x, stream, lambda s: load_library().mhlmoe_quantize(*args, s))
+    return q, scales
+
+
+def mhlmoe_gemm_scaled(A, scale_a, B, scale_b, *, b_block_rows=128, dtype=torch.bfloat16, C=None,
+                       stream=None):
+    """C [M, N] (dtype) = A [M, K] B [N, K]^T of e4m3 operands with scales per
+    block of 128 along K: scale_a [M, KB], scale_b [ceil(N / b_block_rows), KB]."""
+    M, K = _rows_cols(A, "A")
+    N = _rows_cols(B, "B")[0]
+    KB = -(-K // 128)
+    nb = -(-N // b_block_rows) if b_block_rows in (1, 128) else N
+    C = _new(C, (M, N), dtype, A)
+    _one_device(A, scale_a, B, scale_b, C)
+    f32 = torch.float32
+    args = (_dev(A, "A", E4M3), _dev(scale_a, "scale_a", f32, (M, KB)), _dev(B, "B", E4M3, (N, K)),
+            _dev(scale_b, "scale_b", f32, (nb, KB)), M, N, K, int(b_block_rows), _dtype_code(C),
+            _dev(C, "C", dtype, (M, N)))
+    _launch(A, stream, lambda s: load_library().mhlmoe_gemm_scaled(*args, s))
+    return C
+
+
+def mhlmoe_latent_layer_scaled_workspace(T: int, d_model: int, n_heads: int, d_head: int,
+                                         n_experts: int, top_k: int, d_ff: int,
+                                         dtype: int = MHLMOE_BF16) -> int:
+    """Workspace bytes of mhlmoe_latent_layer_scaled."""
+    out = _SZ(0)
+    _check(load_library().mhlmoe_latent_layer_scaled_workspace(
+        T, d_model, n_heads, d_head, n_experts, top_k, d_ff, dtype, ctypes.byref(out)))
+    return out.value
+
+
+def mhlmoe_latent_layer_scaled(x, norm_weight, eps, W_in, scale_in, W_router, bias, W1, W3, W2,
+                               W_out, scale_out, n_heads, top_k, *, residual=None, W_r=None,
+                               scale_r=None, out=None, sum=None, X_lat=None, R_lat=None,
+                               Y_lat=None, idx=None, gate=None, counts=None, workspace=None,
+                               stream=None):
+    """The latent layer behind its norm, with its projections in 8 bits (W_in
+    [N, d_model], W_out [d_model, N] and, for separate routing sub-tokens, W_r
+    [N, d_model]: e4m3 with scales per 128 x 128 tile).  Returns a dict with
+    out, sum (with residual), X_lat, R_lat (with W_r), Y_lat, idx, gate,
+    counts."""
+    T, dm = _rows_cols(x, "x")
+    Ne, dff, dh = W1.shape[1], W1.shape[2], W1.shape[3]
+    Nh, N = n_heads, n_heads * dh
+    dt = _dtype_code(x)
+    f32, i32 = torch.float32, torch.int32
+    out = _new(out, (T, dm), x.dtype, x)
+    if residual is not None:
+        sum = _new(sum, (T, dm), x.dtype, x)
+    X_lat = _new(X_lat, (T, Nh, dh), x.dtype, x)
+    if W_r is not None:
+        R_lat = _new(R_lat, (T, Nh, dh), x.dtype, x)
+    Y_lat = _new(Y_lat, (T, Nh, dh), x.dtype, x)
+    idx = _new(idx, (T, Nh, top_k), i32, x)
+    gate = _new(gate, (T, Nh, top_k), f32, x)
+    counts = _new(counts, (Nh, Ne), i32, x)
+    if workspace is None:
+        n = mhlmoe_latent_layer_scaled_workspace(T, dm, Nh, dh, Ne, top_k, dff, dt)
+        workspace = torch.empty(max(n, 256), dtype=torch.uint8, device=x.device)
+    _one_device(x, residual, norm_weight, W_in, scale_in, W_r, scale_r, W_router, bias, W1, W3, W2,
+                W_out, scale_out, out, sum, X_lat, R_lat, Y_lat, idx, gate, counts, workspace)
+    grid = (-(-N // 128), -(-dm // 128))
+    args = (_dev(x, "x"), _dev(residual, "residual", x.dtype, (T, dm)),
+            _dev(norm_weight, "norm_weight", f32, (dm,)), float(eps),
+            _dev(W_in, "W_in", E4M3, (N, dm)), _dev(scale_in, "scale_in", f32, grid),
+            _dev(W_r, "W_r", E4M3, (N, dm)), _dev(scale_r, "scale_r", f32, grid),
+            _dev(W_router, "W_router", f32, (Nh, Ne, dh)), _dev(bias, "bias", f32, (Nh, Ne)),
+            _dev(W1, "W1", x.dtype, (Nh, Ne, dff, dh)), _dev(W3, "W3", x.dtype, (Nh, Ne, dff, dh)),
+            _dev(W2, "W2", x.dtype, (Nh, Ne, dh, dff)), _dev(W_out, "W_out", E4M3, (dm, N)),
+            _dev(scale_out, "scale_out", f32, grid[::-1]), T, dm, Nh, dh, Ne, top_k, dff, dt,
+            _dev(out, "out", x.dtype, (T, dm)), _dev(sum, "sum", x.dtype, (T, dm)),
+            _dev(X_lat, "X_lat", x.dtype, (T, Nh, dh)), _dev(R_lat, "R_lat", x.dtype, (T, Nh, dh)),
+            _dev(Y_lat, "Y_lat", x.dtype, (T, Nh, dh)), _dev(idx, "idx", i32, (T, Nh, top_k)),
+            _dev(gate, "gate", f32, (T, Nh, top_k)), _dev(counts, "counts", i32, (Nh, Ne)),
+            _dev(workspace, "workspace", torch.uint8), workspace.numel())
+    _launch(x, stream, lambda s: load_library().mhlmoe_latent_layer_scaled(*args, s))
+    res = {"out": out, "X_lat": X_lat, "Y_lat": Y_lat, "idx": idx, "gate": gate, "counts": counts}
+    if residual is not None:
+        res["sum"] = sum
+    if W_r is not None:
+        res["R_lat"] = R_lat
+    return res
 
 
 def mhlmoe_timing_enable(on: bool = True) -> None:

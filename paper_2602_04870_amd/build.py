@@ -36,10 +36,12 @@ COMMON_FLAGS = [
     f"-I{INCLUDE}", f"-I{CSRC}",
 ]
 
-SOURCES = ["api.cpp", "route.hip", "route_64_bf16.hip", "route_64_f32.hip",
+SOURCES = ["api.cpp", "api_scaled.cpp", "route.hip", "route_64_bf16.hip", "route_64_f32.hip",
            "route_128_bf16.hip", "route_128_f32.hip", "bucket.hip", "experts.hip", "ffn_ws.hip",
-           "backward.hip", "projection.cpp", "static_scratch.hip"]
-HEADERS = ["device_common.hpp", "ffn_common.hpp", "launch.hpp", "route_kernel.hpp", "sort_networks.hpp"]
+           "backward.hip", "projection.cpp", "static_scratch.hip", "norm.hip", "quantize.hip",
+           "gemm_scaled.hip"]
+HEADERS = ["api_internal.hpp", "device_common.hpp", "ffn_common.hpp", "launch.hpp", "route_kernel.hpp", "scaled_common.hpp",
+           "scaled_launch.hpp", "sort_networks.hpp"]
 
 
 def _compile(src: str) -> str:

@@ -16,11 +16,17 @@
 #include <vector>
 
 #include "mhlmoe.h"
+#include "api_internal.hpp"
 #include "launch.hpp"
 
 namespace {
 
 thread_local std::string g_error;
+
+}  // namespace
+
+namespace mhl {
+namespace api {
 
 mhlmoe_status fail(mhlmoe_status st, const char* fmt, ...) {
   char buf[512];
@@ -31,6 +37,15 @@ mhlmoe_status fail(mhlmoe_status st, const char* fmt, ...) {
   g_error = buf;
   return st;
 }
+
+void clear_error() { g_error.clear(); }
+
+}  // namespace api
+}  // namespace mhl
+
+using namespace mhl::api;
+
+namespace {
 
 bool debug_sync() {
   static const bool on = [] {
@@ -83,33 +98,6 @@ mhlmoe_status check_ffn_shape(const Shape& s) {
   return MHLMOE_OK;
 }
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-mhlmoe_status need(const void* p, const char* name) {
-  if (p == nullptr) return fail(MHLMOE_EINVAL, "%s is NULL", name);
-  if (!aligned16(p)) return fail(MHLMOE_EINVAL, "%s is not 16-byte aligned", name);
-  return MHLMOE_OK;
-}
-
-// Tensors with a T-sized dimension may be NULL when T == 0.
-mhlmoe_status need_rows(const void* p, const char* name, int64_t T) {
-  return T == 0 ? (p != nullptr && !aligned16(p)
-                       ? fail(MHLMOE_EINVAL, "%s is not 16-byte aligned", name)
-                       : MHLMOE_OK)
-                : need(p, name);
-}
-
-mhlmoe_status maybe(const void* p, const char* name) {
-  if (p != nullptr && !aligned16(p)) return fail(MHLMOE_EINVAL, "%s is not 16-byte aligned", name);
-  return MHLMOE_OK;
-}
-
-#define MHL_TRY(expr)                       \
-  do {                                      \
-    const mhlmoe_status st_ = (expr);       \
-    if (st_ != MHLMOE_OK) return st_;       \
-  } while (0)
-
 // Workspace: a list of 256-byte aligned regions.
 struct Layout {
   size_t ticket = 0, counts = 0, partial = 0, base = 0, offsets = 0, tile_start = 0,
@@ -117,12 +105,6 @@ struct Layout {
          dw_order = 0, rdw_base = 0, rdw_part = 0, lat_x = 0, lat_r = 0, lat_y = 0, lat_dy = 0, lat_dx = 0, lat_dr = 0,
          blas = 0, total = 0;
 };
-
-size_t bump(size_t& cur, size_t bytes) {
-  const size_t at = cur;
-  cur += (bytes + 255) & ~size_t(255);
-  return at;
-}
 
 Layout make_layout(mhlmoe_op op, const Shape& s) {
   if (op == MHLMOE_OP_LATENT_LAYER || op == MHLMOE_OP_LATENT_BACKWARD) {
@@ -198,11 +180,6 @@ Layout make_layout(mhlmoe_op op, const Shape& s) {
   return L;
 }
 
-template <typename T>
-T* at(void* ws, size_t off) {
-  return reinterpret_cast<T*>(reinterpret_cast<uint8_t*>(ws) + off);
-}
-
 mhlmoe_status check_ws(mhlmoe_op op, const Shape& s, void* ws, size_t ws_bytes, Layout& L) {
   L = make_layout(op, s);
   if (L.total > 0) {
@@ -212,15 +189,6 @@ mhlmoe_status check_ws(mhlmoe_op op, const Shape& s, void* ws, size_t ws_bytes, 
     if (ws_bytes < L.total)
       return fail(MHLMOE_EWORKSPACE, "workspace has %zu bytes, need %zu", ws_bytes, L.total);
   }
-  return MHLMOE_OK;
-}
-
-mhlmoe_status launched(hipError_t e, const char* what, hipStream_t stream) {
-  if (e == hipSuccess && debug_sync()) {
-    e = hipStreamSynchronize(stream);
-    if (e == hipSuccess) e = hipGetLastError();
-  }
-  if (e != hipSuccess) return fail(MHLMOE_EHIP, "%s: %s", what, hipGetErrorString(e));
   return MHLMOE_OK;
 }
 
@@ -246,25 +214,42 @@ hipEvent_t take_event() {
   return e;
 }
 
-// Launch one kernel (the callable returns the launch's hipError_t).
-template <class F>
-mhlmoe_status run_kernel(const char* name, hipStream_t stream, F&& launch) {
-  hipEvent_t a = nullptr, b = nullptr;
-  const bool timing = g_timing.load(std::memory_order_relaxed);
-  if (timing) {
-    std::lock_guard<std::mutex> lk(g_timing_mu);
-    a = take_event();
-    b = take_event();
-    if (a) hipEventRecord(a, stream);
+}  // namespace
+
+namespace mhl {
+namespace api {
+
+mhlmoe_status launched(hipError_t e, const char* what, hipStream_t stream) {
+  if (e == hipSuccess && debug_sync()) {
+    e = hipStreamSynchronize(stream);
+    if (e == hipSuccess) e = hipGetLastError();
   }
-  const hipError_t e = launch();
-  if (timing && a && b) {
-    hipEventRecord(b, stream);
-    std::lock_guard<std::mutex> lk(g_timing_mu);
-    g_records.push_back(TimingRecord{name, a, b});
-  }
-  return launched(e, name, stream);
+  if (e != hipSuccess) return fail(MHLMOE_EHIP, "%s: %s", what, hipGetErrorString(e));
+  return MHLMOE_OK;
 }
+
+TimedLaunch timing_begin(hipStream_t stream) {
+  TimedLaunch t{nullptr, nullptr};
+  if (g_timing.load(std::memory_order_relaxed)) {
+    std::lock_guard<std::mutex> lk(g_timing_mu);
+    t.start = take_event();
+    t.stop = take_event();
+    if (t.start) hipEventRecord(t.start, stream);
+  }
+  return t;
+}
+
+void timing_end(const char* name, const TimedLaunch& t, hipStream_t stream) {
+  if (t.start == nullptr || t.stop == nullptr) return;
+  hipEventRecord(t.stop, stream);
+  std::lock_guard<std::mutex> lk(g_timing_mu);
+  g_records.push_back(TimingRecord{name, t.start, t.stop});
+}
+
+}  // namespace api
+}  // namespace mhl
+
+namespace {
 
 // Clustering from the per-block histograms in the workspace: counts,
 // offsets, (tile_rows > 0) the FFN tile list, and perm.

@@ -1,0 +1,422 @@
+// The residual sum and RMS norm in front of the layer, and their gradient.
+//
+//   h = round(x + residual);  rs = 1 / sqrt(mean_c h^2 + eps);  y = h rs w
+//
+// and, for a gradient dy of y and dsum of h (from h's other readers),
+//
+//   g = dy w;  dx = dsum + rs (g - h rs^2 mean_c(g h));  dw = sum_t dy h rs.
+//
+// The norm is that of the stored (rounded) h, so the backward, which has only
+// h, differentiates what the forward computed.  Sums are in fp32.
+//
+// Every element is read once: up to 16384 columns a row stays in the registers
+// of the lanes that normalise it, a wavefront (up to 4096 columns) or a
+// workgroup.  Wider rows, and rows whose width is no multiple of 8, are walked
+// twice by a workgroup (the second time out of the caches).
+
+#include "scaled_common.hpp"
+#include "scaled_launch.hpp"
+
+namespace mhl {
+namespace {
+
+constexpr int kNormThreads = 256;
+constexpr int kNormWaves = kNormThreads / kWave;
+constexpr unsigned kNormMaxGrid = 1u << 20;  // workgroups; rows beyond them are looped over
+
+// Sum over the lanes of a row: a wavefront, or the workgroup (whose
+// wavefronts' sums are added in their order).
+template <int LANES>
+__device__ __forceinline__ float row_sum(float v, float* lds) {
+  v = wave_sum(v);
+  if (LANES == kWave) return v;
+  __syncthreads();  // the readers of the sums before
+  if (lane_id() == 0) lds[threadIdx.x >> 6] = v;
+  __syncthreads();
+  float s = lds[0];
+#pragma unroll
+  for (int w = 1; w < LANES / kWave; ++w) s += lds[w];
+  return s;
+}
+
+// Writes eight columns of y: in the type, and/or in 8 bits with the scale of
+// the 16 lanes' 128 columns.  All lanes of the wavefront take part.
+template <bool F32>
+__device__ __forceinline__ void write_y(const float (&y)[8], bool ok, int64_t row, int col, int d,
+                                        void* out, uint8_t* q, float* scales) {
+  const int64_t at = row * d + col;
+  if (out && ok) store8<F32>(out, at, pack8<F32>(y));
+  if (q) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t b = magnitude(y[i]);
+      m = b > m ? b : m;
+    }
+    const float s = block_scale(max16(ok ? m : 0u));
+    const float inv = 1.0f / s;
+    float z[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) z[i] = over_scale(y[i], s, inv);
+    if (ok) {
+      *reinterpret_cast<u32x2*>(q + at) =
+          u32x2{pack_e4m3(z[0], z[1], z[2], z[3]), pack_e4m3(z[4], z[5], z[6], z[7])};
+      if ((threadIdx.x & 15) == 0)
+        scales[row * ceil_div(d, kScaleBlock) + col / kScaleBlock] = s;
+    }
+  }
+}
+
+__device__ __forceinline__ void load_weight(const float* w, int col, bool ok, float (&f)[8]) {
+  unpack8<true>(load8<true>(w, col, ok), f);
+}
+
+// LANES lanes per row, each with NV pieces of 8 columns; d a multiple of 8,
+// at most LANES * NV * 8.  residual == NULL: h is x, and sum is not written.
+// sum may be x or residual, y may be x: a lane stores only what it has read.
+template <bool F32, int LANES, int NV>
+__global__ __launch_bounds__(kNormThreads) void rmsnorm_kernel(
+    const void* x, const void* residual, const float* __restrict__ w, int64_t T, int d, float eps,
+    void* sum, void* y, uint8_t* q, float* scales) {
+  __shared__ float lds[kNormWaves];
+  constexpr int kRows = kNormThreads / LANES;
+  const int l = threadIdx.x % LANES;
+  for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES; row < T;
+       row += (int64_t)gridDim.x * kRows) {
+    Raw8<F32> hr[NV], rr[NV];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int col = (v * LANES + l) * 8;
+      hr[v] = load8<F32>(x, row * d + col, col < d);
+    }
+    if (residual) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const int col = (v * LANES + l) * 8;
+        rr[v] = load8<F32>(residual, row * d + col, col < d);
+      }
+    }
+    float ss = 0.0f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int col = (v * LANES + l) * 8;
+      float h[8];
+      unpack8<F32>(hr[v], h);
+      if (residual) {
+        float r[8];
+        unpack8<F32>(rr[v], r);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[i] += r[i];
+        hr[v] = pack8<F32>(h);
+        if (col < d) store8<F32>(sum, row * d + col, hr[v]);
+        unpack8<F32>(hr[v], h);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) ss = fmaf(h[i], h[i], ss);
+    }
+    const float rs = 1.0f / sqrtf(row_sum<LANES>(ss, lds) / (float)d + eps);
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int col = (v * LANES + l) * 8;
+      float h[8], wf[8];
+      unpack8<F32>(hr[v], h);
+      load_weight(w, col, col < d, wf);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) h[i] = h[i] * rs * wf[i];
+      write_y<F32>(h, col < d, row, col, d, y, q, scales);
+    }
+  }
+}
+
+// Any width, one workgroup per row, VEC columns at a time (VEC 8: d a multiple
+// of 8; VEC 1 writes no 8 bits).
+template <bool F32, int VEC>
+__global__ __launch_bounds__(kNormThreads) void rmsnorm_wide_kernel(
+    const void* x, const void* residual, const float* __restrict__ w, int64_t T, int d, float eps,
+    void* sum, void* y, uint8_t* q, float* scales) {
+  __shared__ float lds[kNormWaves];
+  for (int64_t row = blockIdx.x; row < T; row += gridDim.x) {
+    const void* h_src = residual ? sum : x;  // each thread reads back what it wrote itself
+    float ss = 0.0f;
+    for (int c = threadIdx.x * VEC; c < d; c += kNormThreads * VEC) {
+      const int64_t at = row * d + c;
+      if constexpr (VEC == 8) {
+        float h[8];
+        unpack8<F32>(load8<F32>(x, at, true), h);
+        if (residual) {
+          float r[8];
+          unpack8<F32>(load8<F32>(residual, at, true), r);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) h[i] += r[i];
+          const Raw8<F32> p = pack8<F32>(h);
+          store8<F32>(sum, at, p);
+          unpack8<F32>(p, h);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) ss = fmaf(h[i], h[i], ss);
+      } else {
+        float h = load1<F32>(x, at);
+        if (residual) {
+          h = round1<F32>(h + load1<F32>(residual, at));
+          store1<F32>(sum, at, h);
+        }
+        ss = fmaf(h, h, ss);
+      }
+    }
+    const float rs = 1.0f / sqrtf(row_sum<kNormThreads>(ss, lds) / (float)d + eps);
+    if constexpr (VEC == 8) {
+      // whole wavefronts to the end: the 8-bit output reduces over 16 lanes
+      for (int c0 = 0; c0 < d; c0 += kNormThreads * VEC) {
+        const int c = c0 + threadIdx.x * VEC;
+        float h[8], wf[8];
+        unpack8<F32>(load8<F32>(h_src, row * d + c, c < d), h);
+        load_weight(w, c, c < d, wf);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[i] = h[i] * rs * wf[i];
+        write_y<F32>(h, c < d, row, c, d, y, q, scales);
+      }
+    } else {
+      for (int c = threadIdx.x; c < d; c += kNormThreads)
+        store1<F32>(y, row * d + c, load1<F32>(h_src, row * d + c) * rs * w[c]);
+    }
+  }
+}
+
+// The gradient, rows as above; a workgroup goes over rows blockIdx.x,
+// blockIdx.x + gridDim.x, ... (of kRows rows each) with its columns' dw in
+// registers and leaves their sum in part[blockIdx.x][d], its rows' lanes added
+// in order.  dx may be dy or dsum.
+template <bool F32, int LANES, int NV>
+__global__ __launch_bounds__(kNormThreads) void rmsnorm_bwd_kernel(
+    const void* h_src, const float* __restrict__ w, const void* dy, const void* dsum, int64_t T,
+    int d, float eps, void* dx, float* __restrict__ part) {
+  constexpr int kRows = kNormThreads / LANES;
+  __shared__ float lds[2 * kNormWaves];
+  __shared__ float add[kRows > 1 ? kNormThreads * 8 : 1];
+  const int l = threadIdx.x % LANES;
+  float dw[NV][8];
+#pragma unroll
+  for (int v = 0; v < NV; ++v)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) dw[v][i] = 0.0f;
+  for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES; row < T;
+       row += (int64_t)gridDim.x * kRows) {
+    Raw8<F32> hr[NV], gr[NV], sr[NV];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int col = (v * LANES + l) * 8;
+      hr[v] = load8<F32>(h_src, row * d + col, col < d);
+      gr[v] = load8<F32>(dy, row * d + col, col < d);
+    }
+    if (dsum) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const int col = (v * LANES + l) * 8;
+        sr[v] = load8<F32>(dsum, row * d + col, col < d);
+      }
+    }
+    float ss = 0.0f, gh = 0.0f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int col = (v * LANES + l) * 8;
+      float h[8], g[8], wf[8];
+      unpack8<F32>(hr[v], h);
+      unpack8<F32>(gr[v], g);
+      load_weight(w, col, col < d, wf);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        ss = fmaf(h[i], h[i], ss);
+        gh = fmaf(g[i] * wf[i], h[i], gh);
+      }
+    }
+    ss = row_sum<LANES>(ss, lds);
+    gh = row_sum<LANES>(gh, lds + kNormWaves);
+    const float rs = 1.0f / sqrtf(ss / (float)d + eps);
+    const float k = gh / (float)d * rs * rs;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int col = (v * LANES + l) * 8;
+      float h[8], g[8], wf[8], s[8];
+      unpack8<F32>(hr[v], h);
+      unpack8<F32>(gr[v], g);
+      load_weight(w, col, col < d, wf);
+      if (dsum) unpack8<F32>(sr[v], s);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        dw[v][i] = fmaf(g[i], h[i] * rs, dw[v][i]);
+        const float t = rs * fmaf(-h[i], k, g[i] * wf[i]);
+        h[i] = dsum ? s[i] + t : t;
+      }
+      if (col < d) store8<F32>(dx, row * d + col, pack8<F32>(h));
+    }
+  }
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    const int col = (v * LANES + l) * 8;
+    if (kRows > 1) {
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 8; ++i) add[i * kNormThreads + threadIdx.x] = dw[v][i];
+      __syncthreads();
+      if (threadIdx.x < LANES) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          float t = add[i * kNormThreads + l];
+#pragma unroll
+          for (int r = 1; r < kRows; ++r) t += add[i * kNormThreads + r * LANES + l];
+          dw[v][i] = t;
+        }
+      }
+    }
+    if (threadIdx.x < LANES && col < d)
+      store8<true>(part, (int64_t)blockIdx.x * d + col, pack8<true>(dw[v]));
+  }
+}
+
+// Any width: dx, and rs of every row for the columns' sums.
+template <bool F32>
+__global__ __launch_bounds__(kNormThreads) void rmsnorm_bwd_wide_kernel(
+    const void* h_src, const float* __restrict__ w, const void* dy, const void* dsum, int64_t T,
+    int d, float eps, float* __restrict__ rs_out, float* __restrict__ k_out) {
+  __shared__ float lds[2 * kNormWaves];
+  for (int64_t row = blockIdx.x; row < T; row += gridDim.x) {
+    float ss = 0.0f, gh = 0.0f;
+    for (int c = threadIdx.x; c < d; c += kNormThreads) {
+      const float h = load1<F32>(h_src, row * d + c);
+      ss = fmaf(h, h, ss);
+      gh = fmaf(load1<F32>(dy, row * d + c) * w[c], h, gh);
+    }
+    ss = row_sum<kNormThreads>(ss, lds);
+    gh = row_sum<kNormThreads>(gh, lds + kNormWaves);
+    const float rs = 1.0f / sqrtf(ss / (float)d + eps);
+    if (threadIdx.x == 0) {
+      rs_out[row] = rs;
+      k_out[row] = gh / (float)d * rs * rs;
+    }
+  }
+}
+
+// Grid (ceil(d / 256), chunks of rows): a thread goes down one column with
+// what the kernel above left of every row, writing dx and its chunk's dw.
+template <bool F32>
+__global__ __launch_bounds__(kNormThreads) void rmsnorm_bwd_columns_kernel(
+    const void* h_src, const float* __restrict__ w, const void* dy, const void* dsum, int64_t T,
+    int d, const float* __restrict__ rs_in, const float* __restrict__ k_in, void* dx,
+    float* __restrict__ part) {
+  const int c = blockIdx.x * kNormThreads + threadIdx.x;
+  if (c >= d) return;
+  const int64_t t0 = T * blockIdx.y / gridDim.y, t1 = T * (blockIdx.y + 1) / gridDim.y;
+  const float wc = w[c];
+  float dw = 0.0f;
+#pragma unroll 4
+  for (int64_t t = t0; t < t1; ++t) {
+    const float h = load1<F32>(h_src, t * d + c), g = load1<F32>(dy, t * d + c);
+    const float rs = rs_in[t];
+    dw = fmaf(g, h * rs, dw);
+    float v = rs * fmaf(-h, k_in[t], g * wc);
+    if (dsum) v += load1<F32>(dsum, t * d + c);
+    store1<F32>(dx, t * d + c, v);
+  }
+  part[(int64_t)blockIdx.y * d + c] = dw;
+}
+
+// dw[c] = the sum of n partial rows: 32 columns per workgroup, every 32nd row
+// per thread, the 32 threads of a column added in order.
+__global__ __launch_bounds__(1024) void rmsnorm_dw_kernel(const float* __restrict__ part, int n,
+                                                          int d, float* __restrict__ dw) {
+  __shared__ float lds[32][33];
+  const int c = blockIdx.x * 32 + threadIdx.x % 32, g = threadIdx.x / 32;
+  float s = 0.0f;
+  if (c < d) {
+#pragma unroll 8
+    for (int r = g; r < n; r += 32) s += part[(int64_t)r * d + c];
+  }
+  lds[g][threadIdx.x % 32] = s;
+  __syncthreads();
+  if (g == 0 && c < d) {
+    for (int i = 1; i < 32; ++i) s += lds[i][threadIdx.x];
+    dw[c] = s;
+  }
+}
+
+unsigned norm_grid(int64_t rows, int per_wg, unsigned most) {
+  const int64_t n = ceil_div(rows, per_wg);
+  return (unsigned)(n < (int64_t)most ? n : (int64_t)most);
+}
+
+}  // namespace
+
+hipError_t launch_rmsnorm(const void* x, const void* residual, const float* w, int64_t T, int d,
+                          float eps, bool f32, void* sum, void* y, void* q, float* scales,
+                          hipStream_t s) {
+  uint8_t* q8 = static_cast<uint8_t*>(q);
+#define MHL_NORM(F32, LANES, NV)                                                                   \
+  hipLaunchKernelGGL((rmsnorm_kernel<F32, LANES, NV>),                                             \
+                     dim3(norm_grid(T, kNormThreads / LANES, kNormMaxGrid)), dim3(kNormThreads), 0, \
+                     s, x, residual, w, T, d, eps, sum, y, q8, scales)
+#define MHL_NORM_WIDE(F32, VEC)                                                                   \
+  hipLaunchKernelGGL((rmsnorm_wide_kernel<F32, VEC>), dim3(norm_grid(T, 1, kNormMaxGrid)),        \
+                     dim3(kNormThreads), 0, s, x, residual, w, T, d, eps, sum, y, q8, scales)
+#define MHL_NORM_TYPE(F32)             \
+  do {                                 \
+    switch (norm_form(d)) {            \
+      case NormForm::kWave1: MHL_NORM(F32, 64, 1); break;   \
+      case NormForm::kWave2: MHL_NORM(F32, 64, 2); break;   \
+      case NormForm::kWave4: MHL_NORM(F32, 64, 4); break;   \
+      case NormForm::kWave8: MHL_NORM(F32, 64, 8); break;   \
+      case NormForm::kGroup4: MHL_NORM(F32, 256, 4); break; \
+      case NormForm::kGroup8: MHL_NORM(F32, 256, 8); break; \
+      case NormForm::kWide8: MHL_NORM_WIDE(F32, 8); break;  \
+      case NormForm::kWide1: MHL_NORM_WIDE(F32, 1); break;  \
+    }                                  \
+  } while (0)
+  if (f32)
+    MHL_NORM_TYPE(true);
+  else
+    MHL_NORM_TYPE(false);
+#undef MHL_NORM_TYPE
+#undef MHL_NORM_WIDE
+#undef MHL_NORM
+  return hipGetLastError();
+}
+
+hipError_t launch_rmsnorm_bwd(const void* h, const float* w, const void* dy, const void* dsum,
+                              int64_t T, int d, float eps, bool f32, void* dx, float* part,
+                              float* rows, hipStream_t s) {
+  const unsigned n = (unsigned)rmsnorm_bwd_parts(T, d);
+#define MHL_NORM(F32, LANES, NV)                                                              \
+  hipLaunchKernelGGL((rmsnorm_bwd_kernel<F32, LANES, NV>), dim3(n), dim3(kNormThreads), 0, s, h, \
+                     w, dy, dsum, T, d, eps, dx, part)
+#define MHL_NORM_TYPE(F32)                                                                       \
+  do {                                                                                           \
+    switch (norm_form(d)) {                                                                      \
+      case NormForm::kWave1: MHL_NORM(F32, 64, 1); break;                                        \
+      case NormForm::kWave2: MHL_NORM(F32, 64, 2); break;                                        \
+      case NormForm::kWave4: MHL_NORM(F32, 64, 4); break;                                        \
+      case NormForm::kWave8: MHL_NORM(F32, 64, 8); break;                                        \
+      case NormForm::kGroup4: MHL_NORM(F32, 256, 4); break;                                      \
+      case NormForm::kGroup8: MHL_NORM(F32, 256, 8); break;                                      \
+      default:                                                                                   \
+        hipLaunchKernelGGL((rmsnorm_bwd_wide_kernel<F32>), dim3(norm_grid(T, 1, kNormMaxGrid)),  \
+                           dim3(kNormThreads), 0, s, h, w, dy, dsum, T, d, eps, rows, rows + T); \
+        hipLaunchKernelGGL((rmsnorm_bwd_columns_kernel<F32>),                                    \
+                           dim3((unsigned)ceil_div(d, kNormThreads), n), dim3(kNormThreads), 0, s, h, w, \
+                           dy, dsum, T, d, rows, rows + T, dx, part);                            \
+    }                                                                                            \
+  } while (0)
+  if (f32)
+    MHL_NORM_TYPE(true);
+  else
+    MHL_NORM_TYPE(false);
+#undef MHL_NORM_TYPE
+#undef MHL_NORM
+  return hipGetLastError();
+}
+
+hipError_t launch_rmsnorm_dw(const float* part, int64_t n, int d, float* dw, hipStream_t s) {
+  hipLaunchKernelGGL(rmsnorm_dw_kernel, dim3((unsigned)ceil_div(d, 32)), dim3(1024), 0, s, part,
+                     (int)n, d, dw);
+  return hipGetLastError();
+}
+
+}  // namespace mhl
