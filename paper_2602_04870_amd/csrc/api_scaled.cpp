@@ -58,10 +58,10 @@ mhlmoe_status check_gemm(int64_t M, int64_t N, int64_t K, int b_block_rows) {
   if (b_block_rows != 1 && b_block_rows != 128)
     return fail(MHLMOE_EINVAL, "b_block_rows must be 1 or 128 (got %d)", b_block_rows);
   const int64_t most = int64_t(1) << 31;
-  if (M >= most || N >= most || K >= (int64_t(1) << 24) ||
+  if (M >= most || N >= most || K >= (int64_t(1) << 23) ||
       !fits_grid(mhl::ceil_div(M, 128), mhl::ceil_div(N, 128)))
     return fail(MHLMOE_EUNSUPPORTED,
-                "product too large: M, N < 2^31, K < 2^24, ceil(M/128) ceil(N/128) < 2^24");
+                "product too large: M, N < 2^31, K < 2^23, ceil(M/128) ceil(N/128) < 2^24");
   return MHLMOE_OK;
 }
 

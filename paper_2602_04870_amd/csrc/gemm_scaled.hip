@@ -36,7 +36,7 @@ __device__ __forceinline__ f32x4 mfma16_e4m3(i32x8 a, i32x8 b) {
                                                           0, 0, 0);
 }
 
-// The same through bf16, 32 values at a time (of the lane's 32, eight).
+// Eight values as bf16.
 __device__ __forceinline__ bf16x8 widen8(int lo, int hi) {
   const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false);
   const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
@@ -44,75 +44,253 @@ __device__ __forceinline__ bf16x8 widen8(int lo, int hi) {
   const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
-__device__ __forceinline__ f32x4 mfma16_widened(i32x8 a, i32x8 b) {
-  f32x4 d{0.f, 0.f, 0.f, 0.f};
+
+// A DMA offset past the end of every buffer here (at most 256 rows of less
+// than 2^23 bytes): zeros land in LDS.
+constexpr uint32_t kPastEnd = 0xC0000000u;
+
+// 64 lanes' 4 bytes each to lds + 4 lane, as dma_lds16 does 16 (zeros past the
+// buffer's end).
+__device__ __forceinline__ void dma_lds4(u32x4 rsrc, const void* lds, uint32_t voff) {
+  const uint32_t m0 = (uint32_t)__builtin_amdgcn_readfirstlane(
+      (int)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)lds);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, 0 offen lds"
+               :
+               : "s"(m0), "v"(voff), "s"(rsrc)
+               : "memory");
+}
+
+__device__ __forceinline__ i32x8 lds_fragment(const uint8_t* lo, const uint8_t* hi) {
+  const u32x4 a = *reinterpret_cast<const u32x4*>(lo), b = *reinterpret_cast<const u32x4*>(hi);
+  return i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
+}
+
+// A tile of C per workgroup: KS groups of WM x WN wavefronts of 16 MT x 16 NT
+// each.  The groups share the tile and take every KS-th block of 128 along K;
+// their sums are added at the end.
+template <int WM, int WN, int MT, int NT, int KS>
+struct Tile {
+  static constexpr int WAVES = WM * WN, THREADS = 64 * WAVES * KS;
+  static constexpr int BM = 16 * WM * MT, BN = 16 * WN * NT;
+  static constexpr int A = 0, B = BM * kScaleBlock, SA = B + BN * kScaleBlock, SB = SA + 4 * BM;
+  static constexpr int STAGE = SB + 4 * BN;
+  static constexpr int LDS = KS * 2 * STAGE;
+  // 1 KiB DMA instructions (8 rows of 128) per wavefront and block
+  static constexpr int PIECES_A = BM / 8 / WAVES, PIECES_B = BN / 8 / WAVES;
+  static_assert(PIECES_A * 8 * WAVES == BM && PIECES_B * 8 * WAVES == BN, "whole pieces");
+  static_assert((BM + BN) / 64 == WAVES && BM % 64 == 0, "a piece of the scales each");
+  static_assert(NT * 16 <= kScaleBlock && kScaleBlock % (NT * 16) == 0, "one tile scale per wavefront");
+  static_assert(LDS <= 160 * 1024 && (KS == 1 || 64 * WAVES * MT * NT * 16 <= LDS), "LDS");
+};
+
+// What a wavefront fetches of a block: its 1 KiB pieces of A and of B, and 64
+// rows' scales.
+template <class S>
+struct Fetch {
+  u32x4 rsrc_a, rsrc_b, rsrc_s;
+  // the lane's source bytes in its pieces of 8 rows: row lane / 8, the 16 bytes
+  // that belong at lane % 8 of the row in LDS
+  uint32_t voff[S::PIECES_A + S::PIECES_B];
+  uint32_t piece, scale_off;
+  int w, scale_at;
+  int64_t K;
+
+  __device__ __forceinline__ void operator()(uint8_t* stage, int kb) const {
+    const bool in = (int64_t)kb * kScaleBlock + piece < K;
 #pragma unroll
-  for (int i = 0; i < 8; i += 2)
-    d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(a[i], a[i + 1]), widen8(b[i], b[i + 1]), d, 0,
-                                                0, 0);
-  return d;
+    for (int i = 0; i < S::PIECES_A + S::PIECES_B; ++i) {
+      const bool a = i < S::PIECES_A;
+      const int p = (a ? i : i - S::PIECES_A) * S::WAVES + w;
+      dma_lds16(a ? rsrc_a : rsrc_b, stage + (a ? S::A : S::B) + p * 1024,
+                in ? voff[i] + (uint32_t)kb * kScaleBlock : kPastEnd, 0);
+    }
+    dma_lds4(rsrc_s, stage + scale_at, scale_off + (uint32_t)kb * 4);
+  }
+};
+
+template <class S, bool ROWS>
+__device__ __forceinline__ Fetch<S> make_fetch(const uint8_t* A, const float* sa, int rows_a,
+                                               const uint8_t* B, const float* sb, int rows_b,
+                                               int64_t K, int w) {
+  Fetch<S> f;
+  const int lane = lane_id();
+  const uint32_t KB = (uint32_t)ceil_div(K, kScaleBlock);
+  f.K = K;
+  f.w = w;
+  f.rsrc_a = buffer_words(A, (uint32_t)(rows_a * K));
+  f.rsrc_b = buffer_words(B, (uint32_t)(rows_b * K));
+  const bool of_b = w >= S::BM / 64;  // whose scales
+  const int row = 64 * (of_b ? w - S::BM / 64 : w) + lane;
+  const uint32_t srows = of_b ? (ROWS ? rows_b : (int)ceil_div(rows_b, kScaleBlock)) : rows_a;
+  f.rsrc_s = buffer_words(of_b ? sb : sa, srows * KB * 4);
+  f.scale_off = (uint32_t)(of_b && !ROWS ? row / kScaleBlock : row) * KB * 4;
+  f.scale_at = of_b ? S::SB + (w - S::BM / 64) * 256 : S::SA + w * 256;
+  f.piece = (uint32_t)((lane & 7) ^ (lane >> 3)) * 16;
+#pragma unroll
+  for (int i = 0; i < S::PIECES_A + S::PIECES_B; ++i) {
+    const int p = (i < S::PIECES_A ? i : i - S::PIECES_A) * S::WAVES + w;
+    f.voff[i] = (uint32_t)(8 * p + (lane >> 3)) * (uint32_t)K + f.piece;
+  }
+  return f;
 }
 
-// Pieces lane / 16 and 4 + lane / 16 of block kb of a row; zeros past K.
-__device__ __forceinline__ i32x8 load_fragment(const uint8_t* row, bool ok, int64_t K, int64_t kb) {
-  const int64_t k = kb * kScaleBlock + 16 * (lane_id() >> 4);
-  const u32x4 z{0u, 0u, 0u, 0u};
-  const u32x4 lo = ok && k < K ? *reinterpret_cast<const u32x4*>(row + k) : z;
-  const u32x4 hi = ok && k + 64 < K ? *reinterpret_cast<const u32x4*>(row + k + 64) : z;
-  return i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3],
-               (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
-}
-
-// A wavefront's 64 x 64 piece of C, fragments straight from memory.
-template <bool F32, bool ROWS>
-__global__ __launch_bounds__(256) void gemm_scaled_kernel(
+// Blocks of A and B (with their scales) go by LDS DMA into one of two stages
+// while the other is multiplied; rows of 128 bytes have their 16-byte pieces
+// XOR-ed by the row's low three bits, which makes the fragments' 16-byte reads
+// free of bank conflicts.  One barrier per block: it waits for the next
+// block's DMA, issued a block earlier.
+template <class S, int WM, int WN, int MT, int NT, int KS, bool F32, bool ROWS>
+__global__ __launch_bounds__(S::THREADS) void gemm_scaled_kernel(
     const uint8_t* __restrict__ A, const float* __restrict__ sa, const uint8_t* __restrict__ B,
     const float* __restrict__ sb, int64_t M, int64_t N, int64_t K, void* __restrict__ C) {
-  const int lane = lane_id(), wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
-  const int64_t tiles_n = ceil_div(N, 128), KB = ceil_div(K, kScaleBlock);
-  const int64_t m0 = blockIdx.x / tiles_n * 128 + (wave & 1) * 64;
-  const int64_t n0 = blockIdx.x % tiles_n * 128 + (wave >> 1) * 64;
-  f32x4 acc[4][4];
+  __shared__ __attribute__((aligned(16))) uint8_t smem[S::LDS];
+  const int lane = lane_id(), c = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const int kg = wave / S::WAVES, w = wave % S::WAVES;
+  const int wm = w % WM, wn = w / WM;
+  const int KB = (int)ceil_div(K, kScaleBlock);
+
+  // an accelerator die's workgroups take a contiguous run of tiles, ordered in
+  // bands of 8 tiles down m, so that what runs together shares rows in its L2
+  const int tm = (int)ceil_div(M, S::BM), tn = (int)ceil_div(N, S::BN);
+  int t;
+  {
+    const int xcd = (int)(blockIdx.x % kXcds), seq = (int)(blockIdx.x / kXcds);
+    const int per = (int)(gridDim.x / kXcds), rem = (int)(gridDim.x % kXcds);
+    t = xcd * per + (xcd < rem ? xcd : rem) + seq;
+  }
+  const int band = t / (8 * tn), in_band = t - band * 8 * tn;
+  const int band_m = tm - band * 8 < 8 ? tm - band * 8 : 8;
+  const int64_t m0 = (int64_t)(band * 8 + in_band % band_m) * S::BM;
+  const int64_t n0 = (int64_t)(in_band / band_m) * S::BN;
+
+  const int rows_a = M - m0 < S::BM ? (int)(M - m0) : S::BM;
+  const int rows_b = N - n0 < S::BN ? (int)(N - n0) : S::BN;
+  const Fetch<S> fetch = make_fetch<S, ROWS>(A + m0 * K, sa + m0 * KB, rows_a, B + n0 * K,
+                                             sb + (ROWS ? n0 : n0 / kScaleBlock) * KB, rows_b, K, w);
+
+  f32x4 acc[MT][NT];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < MT; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int64_t kb = 0; kb < KB; ++kb) {
-    i32x8 a[4], b[4];
-    float s[4];
+    for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  // the lane's pieces g and 4 + g of row c
+  const int frag_lo = c * kScaleBlock + ((g ^ (c & 7)) * 16), frag_hi = frag_lo ^ 64;
+  uint8_t* const stages = smem + kg * 2 * S::STAGE;
+  if (kg < KB) fetch(stages, kg);
+  const int steps = (KB + KS - 1) / KS;
+  for (int it = 0; it < steps; ++it) {
+    const int kb = it * KS + kg;
+    barrier_vm<0>();
+    if (kb + KS < KB) fetch(stages + ((it + 1) & 1) * S::STAGE, kb + KS);
+    if (kb >= KB) continue;
+    const uint8_t* st = stages + (it & 1) * S::STAGE;
+    const uint8_t* sta = st + S::A + wm * MT * 16 * kScaleBlock;
+    const uint8_t* stb = st + S::B + wn * NT * 16 * kScaleBlock;
+    const float* ssa = reinterpret_cast<const float*>(st + S::SA) + wm * MT * 16 + c;
+    const float* ssb = reinterpret_cast<const float*>(st + S::SB) + wn * NT * 16;
+    float s[MT];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int64_t m = m0 + 16 * i + c;
-      a[i] = load_fragment(A + m * K, m < M, K, kb);
-      s[i] = m < M ? sa[m * KB + kb] : 0.0f;
-    }
+    for (int i = 0; i < MT; ++i) s[i] = ROWS ? ssa[16 * i] : ssa[16 * i] * ssb[0];
+    if constexpr (!F32) {
+      i32x8 a[MT];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int64_t n = n0 + 16 * j;
-      b[j] = load_fragment(B + (n + c) * K, n + c < N, K, kb);
-      float t[4];
+      for (int i = 0; i < MT; ++i)
+        a[i] = lds_fragment(sta + frag_lo + i * 2048, sta + frag_hi + i * 2048);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int64_t ne = n + 4 * g + e;
-        t[e] = ne < N ? sb[(ROWS ? ne : ne / kScaleBlock) * KB + kb] : 0.0f;
+      for (int j = 0; j < NT; ++j) {
+        const i32x8 b = lds_fragment(stb + frag_lo + j * 2048, stb + frag_hi + j * 2048);
+        f32x4 r{1.f, 1.f, 1.f, 1.f};
+        if (ROWS) r = *reinterpret_cast<const f32x4*>(ssb + 16 * j + 4 * g);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          const f32x4 d = mfma16_e4m3(b, a[i]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            acc[i][j][e] = fmaf(ROWS ? s[i] * r[e] : s[i], d[e], acc[i][j][e]);
+        }
+      }
+    } else {
+      bf16x8 a[MT][4];
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        const i32x8 v = lds_fragment(sta + frag_lo + i * 2048, sta + frag_hi + i * 2048);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) a[i][q] = widen8(v[2 * q], v[2 * q + 1]);
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const f32x4 d = F32 ? mfma16_widened(b[j], a[i]) : mfma16_e4m3(b[j], a[i]);
+      for (int j = 0; j < NT; ++j) {
+        const i32x8 v = lds_fragment(stb + frag_lo + j * 2048, stb + frag_hi + j * 2048);
+        f32x4 r{1.f, 1.f, 1.f, 1.f};
+        if (ROWS) r = *reinterpret_cast<const f32x4*>(ssb + 16 * j + 4 * g);
+        f32x4 d[MT];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(s[i] * t[e], d[e], acc[i][j][e]);
+        for (int i = 0; i < MT; ++i) d[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const bf16x8 b = widen8(v[2 * q], v[2 * q + 1]);
+#pragma unroll
+          for (int i = 0; i < MT; ++i)
+            d[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, a[i][q], d[i], 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            acc[i][j][e] = fmaf(ROWS ? s[i] * r[e] : s[i], d[i][e], acc[i][j][e]);
       }
     }
   }
+
+  if constexpr (KS == 2) {
+    // each group hands half of its pieces to the other and keeps the rest
+    __syncthreads();
+    f32x4* x = reinterpret_cast<f32x4*>(smem) + w * MT * NT * 64 + lane;
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < MT; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+      for (int j = 0; j < NT; ++j)
+        if ((j < NT / 2) == (kg == 1)) x[(i * NT + j) * 64] = acc[i][j];
+    __syncthreads();
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int64_t m = m0 + 16 * i + c, n = n0 + 16 * j + 4 * g + e;
-        if (m < M && n < N) store1<F32>(C, m * N + n, acc[i][j][e]);
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+        if ((j < NT / 2) == (kg == 0)) acc[i][j] += x[(i * NT + j) * 64];
+  }
+  const bool whole = N % 4 == 0;  // rows of C keep four results together and aligned
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const int64_t m = m0 + (wm * MT + i) * 16 + c;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      if (KS == 2 && (j < NT / 2) != (kg == 0)) continue;
+      const int64_t n = n0 + (wn * NT + j) * 16 + 4 * g;
+      if (m >= M || n >= N) continue;
+      const f32x4 v = acc[i][j];
+      if (whole) {
+        if (F32)
+          *reinterpret_cast<f32x4*>(static_cast<float*>(C) + m * N + n) = v;
+        else
+          *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(C) + m * N + n) =
+              u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (n + e < N) store1<F32>(C, m * N + n + e, v[e]);
       }
+    }
+  }
+}
+
+template <int WM, int WN, int MT, int NT, int KS, bool F32, bool ROWS>
+void launch_tile(const uint8_t* A, const float* sa, const uint8_t* B, const float* sb, int64_t M,
+                 int64_t N, int64_t K, void* C, hipStream_t s) {
+  using S = Tile<WM, WN, MT, NT, KS>;
+  const dim3 grid((unsigned)(ceil_div(M, S::BM) * ceil_div(N, S::BN)));
+  hipLaunchKernelGGL((gemm_scaled_kernel<S, WM, WN, MT, NT, KS, F32, ROWS>), grid, dim3(S::THREADS),
+                     0, s, A, sa, B, sb, M, N, K, C);
 }
 
 }  // namespace
@@ -120,11 +298,16 @@ __global__ __launch_bounds__(256) void gemm_scaled_kernel(
 hipError_t launch_gemm_scaled(const void* A, const float* sa, const void* B, const float* sb,
                               int64_t M, int64_t N, int64_t K, bool b_rows, bool f32, void* C,
                               hipStream_t s) {
-  const dim3 grid((unsigned)(ceil_div(M, 128) * ceil_div(N, 128)));
-#define MHL_GEMM(F32, ROWS)                                                                    \
-  hipLaunchKernelGGL((gemm_scaled_kernel<F32, ROWS>), grid, dim3(256), 0, s,                   \
-                     static_cast<const uint8_t*>(A), sa, static_cast<const uint8_t*>(B), sb, M, \
-                     N, K, C)
+  const uint8_t* a = static_cast<const uint8_t*>(A);
+  const uint8_t* b = static_cast<const uint8_t*>(B);
+  const bool large = !f32 && ceil_div(M, 256) * ceil_div(N, 256) >= 192;
+#define MHL_GEMM(F32, ROWS)                                                     \
+  do {                                                                          \
+    if (large && !F32)                                                          \
+      launch_tile<4, 2, 4, 8, 1, false, ROWS>(a, sa, b, sb, M, N, K, C, s);     \
+    else                                                                        \
+      launch_tile<2, 2, 4, 4, 2, F32, ROWS>(a, sa, b, sb, M, N, K, C, s);       \
+  } while (0)
   if (f32 && b_rows)
     MHL_GEMM(true, true);
   else if (f32)
