@@ -49,15 +49,53 @@ __device__ __forceinline__ bf16x8 widen8(int lo, int hi) {
 // than 2^23 bytes): zeros land in LDS.
 constexpr uint32_t kPastEnd = 0xC0000000u;
 
-// 64 lanes' 4 bytes each to lds + 4 lane, as dma_lds16 does 16 (zeros past the
-// buffer's end).
-__device__ __forceinline__ void dma_lds4(u32x4 rsrc, const void* lds, uint32_t voff) {
-  const uint32_t m0 = (uint32_t)__builtin_amdgcn_readfirstlane(
-      (int)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)lds);
+__device__ __forceinline__ void widen(bf16x8 (&to)[4], i32x8 v) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) to[q] = widen8(v[2 * q], v[2 * q + 1]);
+}
+
+// Pieces lane / 16 and 4 + lane / 16 of a row's block at byte k; zeros past K.
+__device__ __forceinline__ i32x8 load_fragment(const uint8_t* row, bool ok, int64_t K, int64_t k) {
+  k += 16 * (lane_id() >> 4);
+  const u32x4 z{0u, 0u, 0u, 0u};
+  const u32x4 lo = ok && k < K ? *reinterpret_cast<const u32x4*>(row + k) : z;
+  const u32x4 hi = ok && k + 64 < K ? *reinterpret_cast<const u32x4*>(row + k + 64) : z;
+  return i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3],
+               (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+}
+
+// dma_lds16 to a byte offset of LDS (an LDS address as a number: from a pointer
+// the compiler computes it anew, null check and all, for every instruction),
+// and its form for 4 bytes per lane.
+__device__ __forceinline__ void dma16_at(u32x4 rsrc, uint32_t lds, uint32_t voff) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+               :
+               : "s"(lds), "v"(voff), "s"(rsrc)
+               : "memory");
+}
+__device__ __forceinline__ void dma4_at(u32x4 rsrc, uint32_t lds, uint32_t voff) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, 0 offen lds"
                :
-               : "s"(m0), "v"(voff), "s"(rsrc)
+               : "s"(lds), "v"(voff), "s"(rsrc)
                : "memory");
+}
+
+// Four results of one row of C, together (rows of a multiple of 4) ...
+template <bool F32>
+__device__ __forceinline__ void store4(void* C, int64_t at, f32x4 v) {
+  if (F32)
+    *reinterpret_cast<f32x4*>(static_cast<float*>(C) + at) = v;
+  else
+    *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(C) + at) =
+        u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+}
+// ... or those of them that C has.
+template <bool F32>
+__device__ __forceinline__ void store_edge(void* C, int64_t m, int64_t M, int64_t n, int64_t N, f32x4 v) {
+  if (m >= M) return;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (n + e < N) store1<F32>(C, m * N + n + e, v[e]);
 }
 
 __device__ __forceinline__ i32x8 lds_fragment(const uint8_t* lo, const uint8_t* hi) {
@@ -72,59 +110,86 @@ template <int WM, int WN, int MT, int NT, int KS>
 struct Tile {
   static constexpr int WAVES = WM * WN, THREADS = 64 * WAVES * KS;
   static constexpr int BM = 16 * WM * MT, BN = 16 * WN * NT;
-  static constexpr int A = 0, B = BM * kScaleBlock, SA = B + BN * kScaleBlock, SB = SA + 4 * BM;
-  static constexpr int STAGE = SB + 4 * BN;
-  static constexpr int LDS = KS * 2 * STAGE;
+  // a K group's LDS: two stages of a block's rows, and two chunks of the
+  // scales of CHUNK blocks (16 rows together: 64 bytes of one block, then of the next)
+  static constexpr int A = 0, B = BM * kScaleBlock, STAGE = B + BN * kScaleBlock;
+  static constexpr int CHUNK = 4;
+  static constexpr int SCALES = 2 * STAGE, SA = 0, SB = 4 * CHUNK * BM, CHUNK_BYTES = SB + 4 * CHUNK * BN;
+  static constexpr int GROUP = SCALES + 2 * CHUNK_BYTES, LDS = KS * GROUP;
   // 1 KiB DMA instructions (8 rows of 128) per wavefront and block
   static constexpr int PIECES_A = BM / 8 / WAVES, PIECES_B = BN / 8 / WAVES;
   static_assert(PIECES_A * 8 * WAVES == BM && PIECES_B * 8 * WAVES == BN, "whole pieces");
-  static_assert((BM + BN) / 64 == WAVES && BM % 64 == 0, "a piece of the scales each");
+  static constexpr int SPIECES_A = BM / 16 / WAVES, SPIECES_B = BN / 16 / WAVES;
+  static_assert(SPIECES_A * 16 * WAVES == BM && SPIECES_B * 16 * WAVES == BN, "whole pieces of scales");
   static_assert(NT * 16 <= kScaleBlock && kScaleBlock % (NT * 16) == 0, "one tile scale per wavefront");
-  static_assert(LDS <= 160 * 1024 && (KS == 1 || 64 * WAVES * MT * NT * 16 <= LDS), "LDS");
+  static_assert(LDS <= 160 * 1024 && (KS == 1 || KS * 64 * WAVES * MT * NT * 16 <= LDS), "LDS");
+  static_assert(NT % KS == 0, "a group's share of the columns");
 };
 
-// What a wavefront fetches of a block: its 1 KiB pieces of A and of B, and 64
-// rows' scales.
-template <class S>
+// What a wavefront fetches: of a block its 1 KiB pieces of A and of B; of the
+// scales, CHUNK of its group's blocks at a time, 16 rows per instruction (one
+// block's scales at a time are a line of memory per row and block: with them
+// the loads alone of 8192 x 8192 x 8192 took 487 us).
+template <class S, int KS, bool ROWS>
 struct Fetch {
-  u32x4 rsrc_a, rsrc_b, rsrc_s;
+  u32x4 rsrc_a, rsrc_b, rsrc_sa, rsrc_sb;
   // the lane's source bytes in its pieces of 8 rows: row lane / 8, the 16 bytes
   // that belong at lane % 8 of the row in LDS
   uint32_t voff[S::PIECES_A + S::PIECES_B];
-  uint32_t piece, scale_off;
-  int w, scale_at;
-  int64_t K;
+  uint32_t piece, K, KB, soff;
+  int w, kg;
 
-  __device__ __forceinline__ void operator()(uint8_t* stage, int kb) const {
-    const bool in = (int64_t)kb * kScaleBlock + piece < K;
+  static constexpr int COUNT = S::PIECES_A + S::PIECES_B;
+
+  // The i-th of COUNT instructions of block kb, to the stage at LDS byte `stage`.
+  __device__ __forceinline__ void one(int i, uint32_t stage, int kb) const {
+    const uint32_t k = (uint32_t)kb * kScaleBlock;
+    const bool a = i < S::PIECES_A;
+    const int p = (a ? i : i - S::PIECES_A) * S::WAVES + w;
+    dma16_at(a ? rsrc_a : rsrc_b, stage + (a ? S::A : S::B) + p * 1024,
+             k + piece < K ? voff[i] + k : kPastEnd);
+  }
+  __device__ __forceinline__ void all(uint32_t stage, int kb) const {
 #pragma unroll
-    for (int i = 0; i < S::PIECES_A + S::PIECES_B; ++i) {
-      const bool a = i < S::PIECES_A;
-      const int p = (a ? i : i - S::PIECES_A) * S::WAVES + w;
-      dma_lds16(a ? rsrc_a : rsrc_b, stage + (a ? S::A : S::B) + p * 1024,
-                in ? voff[i] + (uint32_t)kb * kScaleBlock : kPastEnd, 0);
+    for (int i = 0; i < COUNT; ++i) one(i, stage, kb);
+  }
+  // The scales of the group's blocks number CHUNK t and on; zeros past K, as the
+  // blocks there are.
+  __device__ __forceinline__ void scales(uint32_t chunk, int t) const {
+    const uint32_t kb = (uint32_t)(kg + KS * (S::CHUNK * t + (lane_id() >> 4)));
+    const uint32_t at = kb < KB ? soff + kb * 4 : kPastEnd;
+#pragma unroll
+    for (int i = 0; i < S::SPIECES_A; ++i) {
+      const uint32_t p = (uint32_t)(i * S::WAVES + w);
+      dma4_at(rsrc_sa, chunk + S::SA + p * 256, at + p * 64 * KB);
     }
-    dma_lds4(rsrc_s, stage + scale_at, scale_off + (uint32_t)kb * 4);
+    if (ROWS) {
+#pragma unroll
+      for (int i = 0; i < S::SPIECES_B; ++i) {
+        const uint32_t p = (uint32_t)(i * S::WAVES + w);
+        dma4_at(rsrc_sb, chunk + S::SB + p * 256, at + p * 64 * KB);
+      }
+    } else if (w == 0) {
+      dma4_at(rsrc_sb, chunk + S::SB, at);
+    }
   }
 };
 
-template <class S, bool ROWS>
-__device__ __forceinline__ Fetch<S> make_fetch(const uint8_t* A, const float* sa, int rows_a,
-                                               const uint8_t* B, const float* sb, int rows_b,
-                                               int64_t K, int w) {
-  Fetch<S> f;
+template <class S, int KS, bool ROWS>
+__device__ __forceinline__ Fetch<S, KS, ROWS> make_fetch(const uint8_t* A, const float* sa, int rows_a,
+                                                         const uint8_t* B, const float* sb, int rows_b,
+                                                         int64_t K, int w, int kg) {
+  Fetch<S, KS, ROWS> f;
   const int lane = lane_id();
-  const uint32_t KB = (uint32_t)ceil_div(K, kScaleBlock);
-  f.K = K;
+  f.K = (uint32_t)K;
+  f.KB = (uint32_t)ceil_div(K, kScaleBlock);
   f.w = w;
+  f.kg = kg;
   f.rsrc_a = buffer_words(A, (uint32_t)(rows_a * K));
   f.rsrc_b = buffer_words(B, (uint32_t)(rows_b * K));
-  const bool of_b = w >= S::BM / 64;  // whose scales
-  const int row = 64 * (of_b ? w - S::BM / 64 : w) + lane;
-  const uint32_t srows = of_b ? (ROWS ? rows_b : (int)ceil_div(rows_b, kScaleBlock)) : rows_a;
-  f.rsrc_s = buffer_words(of_b ? sb : sa, srows * KB * 4);
-  f.scale_off = (uint32_t)(of_b && !ROWS ? row / kScaleBlock : row) * KB * 4;
-  f.scale_at = of_b ? S::SB + (w - S::BM / 64) * 256 : S::SA + w * 256;
+  f.rsrc_sa = buffer_words(sa, (uint32_t)rows_a * f.KB * 4);
+  f.rsrc_sb = buffer_words(sb, (uint32_t)(ROWS ? rows_b : (int)ceil_div(rows_b, kScaleBlock)) * f.KB * 4);
+  f.soff = (uint32_t)(lane & 15) * f.KB * 4;
   f.piece = (uint32_t)((lane & 7) ^ (lane >> 3)) * 16;
 #pragma unroll
   for (int i = 0; i < S::PIECES_A + S::PIECES_B; ++i) {
@@ -134,11 +199,12 @@ __device__ __forceinline__ Fetch<S> make_fetch(const uint8_t* A, const float* sa
   return f;
 }
 
-// Blocks of A and B (with their scales) go by LDS DMA into one of two stages
+// Blocks of A and B go by LDS DMA into one of two stages
 // while the other is multiplied; rows of 128 bytes have their 16-byte pieces
 // XOR-ed by the row's low three bits, which makes the fragments' 16-byte reads
 // free of bank conflicts.  One barrier per block: it waits for the next
-// block's DMA, issued a block earlier.
+// block's DMA, issued a block earlier.  (Past the last block it fills a stage
+// with zeros that nobody reads.)
 template <class S, int WM, int WN, int MT, int NT, int KS, bool F32, bool ROWS>
 __global__ __launch_bounds__(S::THREADS) void gemm_scaled_kernel(
     const uint8_t* __restrict__ A, const float* __restrict__ sa, const uint8_t* __restrict__ B,
@@ -166,8 +232,9 @@ __global__ __launch_bounds__(S::THREADS) void gemm_scaled_kernel(
 
   const int rows_a = M - m0 < S::BM ? (int)(M - m0) : S::BM;
   const int rows_b = N - n0 < S::BN ? (int)(N - n0) : S::BN;
-  const Fetch<S> fetch = make_fetch<S, ROWS>(A + m0 * K, sa + m0 * KB, rows_a, B + n0 * K,
-                                             sb + (ROWS ? n0 : n0 / kScaleBlock) * KB, rows_b, K, w);
+  const Fetch<S, KS, ROWS> fetch =
+      make_fetch<S, KS, ROWS>(A + m0 * K, sa + m0 * KB, rows_a, B + n0 * K,
+                              sb + (ROWS ? n0 : n0 / kScaleBlock) * KB, rows_b, K, w, kg);
 
   f32x4 acc[MT][NT];
 #pragma unroll
@@ -177,111 +244,153 @@ __global__ __launch_bounds__(S::THREADS) void gemm_scaled_kernel(
 
   // the lane's pieces g and 4 + g of row c
   const int frag_lo = c * kScaleBlock + ((g ^ (c & 7)) * 16), frag_hi = frag_lo ^ 64;
-  uint8_t* const stages = smem + kg * 2 * S::STAGE;
-  if (kg < KB) fetch(stages, kg);
+  uint8_t* const own = smem + kg * S::GROUP;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)smem +
+                        (uint32_t)(kg * S::GROUP);
+  // where the wavefront's rows lie in a stage, and its scales in block it's
+  // chunk: of the lane's row c of A's piece i at 64 i, of B's rows 4 g .. + 3 of
+  // piece j at 64 j + 4 g, or one for all of the wavefront's columns
+  const int at_a = S::A + wm * MT * 16 * kScaleBlock, at_b = S::B + wn * NT * 16 * kScaleBlock;
+  auto scale_of = [&](int it) {
+    return reinterpret_cast<const float*>(own + S::SCALES + (it / S::CHUNK & 1) * S::CHUNK_BYTES) +
+           16 * (it % S::CHUNK);
+  };
+  const int at_sa = S::SA / 4 + 16 * S::CHUNK * MT * wm + c;
+  const int at_sb =
+      S::SB / 4 + (ROWS ? 16 * S::CHUNK * NT * wn + 4 * g : wn * NT * 16 / kScaleBlock);
   const int steps = (KB + KS - 1) / KS;
+  fetch.scales(lds0 + S::SCALES, 0);
+  fetch.all(lds0, kg);
+  // Unit u of a block is one MFMA (fp32 results: four, on widened pieces): A's
+  // piece i = u % MT by B's piece j = u / MT.  B's pieces are read two ahead.  The barrier stands two pieces before
+  // the block's end, when every read of the block is done and the next block's
+  // DMA (issued there in the block before) has had a block's time to land:
+  // behind it the last two pieces' MFMAs have their operands in registers, and
+  // the next block's first ones are read beneath them, A's piece i as soon as
+  // this block is done with its own.  So no wavefront waits for LDS where a
+  // block begins.  The FMAs of a unit follow the next unit's MFMA, across
+  // blocks, too.  sched_barrier keeps this order; the compiler would read each
+  // fragment right before its use.
+  constexpr int U = MT * NT, TAIL = U - 2 * MT, RING = NT % 4 == 0 && NT % 3 != 2 ? 4 : 3;
+  // the first piece's slot is free before the last piece, the second's behind it
+  constexpr int PIECES = S::PIECES_A + S::PIECES_B, EACH = PIECES / (2 * MT);
+  static_assert(NT >= 4 && (NT - 1) % RING != 0 && PIECES == 2 * MT * EACH, "slots and pieces");
+  i32x8 a[MT], b[RING];
+  bf16x8 aw[F32 ? MT : 1][4], bw[4];
+  f32x4 d[2], r[RING];
+  float s[MT], s_next[MT], sb_next = 0.f, s_last = 0.f;
+  d[1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int q = 0; q < RING; ++q) r[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+  auto read_a = [&](const uint8_t* st, int i) {
+    a[i] = lds_fragment(st + at_a + frag_lo + i * 2048, st + at_a + frag_hi + i * 2048);
+  };
+  auto read_b = [&](const uint8_t* st, const float* sc, int j) {
+    b[j % RING] = lds_fragment(st + at_b + frag_lo + j * 2048, st + at_b + frag_hi + j * 2048);
+    if (ROWS) r[j % RING] = *reinterpret_cast<const f32x4*>(sc + at_sb + 16 * S::CHUNK * j);
+  };
+  auto read_s = [&](const float* sc) {
+#pragma unroll
+    for (int i = 0; i < MT; ++i) s_next[i] = sc[at_sa + 16 * S::CHUNK * i];
+    if (!ROWS) sb_next = sc[at_sb];
+  };
+  auto scale = [&](int u, float f) {
+    const int i = u % MT, j = u / MT;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      acc[i][j][e] = fmaf(ROWS ? f * r[j % RING][e] : f, d[u % 2][e], acc[i][j][e]);
+  };
+  barrier_vm<0>();
+  fetch.all(lds0 + S::STAGE, kg + KS);
+  read_b(own, scale_of(0), 0);
+#pragma unroll
+  for (int i = 0; i < MT; ++i) read_a(own, i);
+  read_s(scale_of(0));
   for (int it = 0; it < steps; ++it) {
-    const int kb = it * KS + kg;
-    barrier_vm<0>();
-    if (kb + KS < KB) fetch(stages + ((it + 1) & 1) * S::STAGE, kb + KS);
-    if (kb >= KB) continue;
-    const uint8_t* st = stages + (it & 1) * S::STAGE;
-    const uint8_t* sta = st + S::A + wm * MT * 16 * kScaleBlock;
-    const uint8_t* stb = st + S::B + wn * NT * 16 * kScaleBlock;
-    const float* ssa = reinterpret_cast<const float*>(st + S::SA) + wm * MT * 16 + c;
-    const float* ssb = reinterpret_cast<const float*>(st + S::SB) + wn * NT * 16;
-    float s[MT];
+    const uint8_t* st = own + (it & 1) * S::STAGE;
+    const uint8_t* st_next = own + ((it + 1) & 1) * S::STAGE;
+    const float *sc = scale_of(it), *sc_next = scale_of(it + 1);
+    // (a branch further down would have the compiler sink FMAs past it)
+    if (it % S::CHUNK == 0)
+      fetch.scales(lds0 + S::SCALES + (uint32_t)((it / S::CHUNK + 1) & 1) * S::CHUNK_BYTES,
+                   it / S::CHUNK + 1);
+    static_for<0, U>([&](auto UC) {
+      constexpr int u = UC.value, i = u % MT, j = u / MT;
+      if constexpr (u == TAIL) barrier_vm<0>();
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (F32) {
+        // a piece is widened where it is first used
+        if constexpr (j == 0) widen(aw[i], a[i]);
+        if constexpr (i == 0) widen(bw, b[j % RING]);
+        d[u % 2] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < MT; ++i) s[i] = ROWS ? ssa[16 * i] : ssa[16 * i] * ssb[0];
-    if constexpr (!F32) {
-      i32x8 a[MT];
-#pragma unroll
-      for (int i = 0; i < MT; ++i)
-        a[i] = lds_fragment(sta + frag_lo + i * 2048, sta + frag_hi + i * 2048);
-#pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        const i32x8 b = lds_fragment(stb + frag_lo + j * 2048, stb + frag_hi + j * 2048);
-        f32x4 r{1.f, 1.f, 1.f, 1.f};
-        if (ROWS) r = *reinterpret_cast<const f32x4*>(ssb + 16 * j + 4 * g);
-#pragma unroll
-        for (int i = 0; i < MT; ++i) {
-          const f32x4 d = mfma16_e4m3(b, a[i]);
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            acc[i][j][e] = fmaf(ROWS ? s[i] * r[e] : s[i], d[e], acc[i][j][e]);
-        }
-      }
-    } else {
-      bf16x8 a[MT][4];
-#pragma unroll
-      for (int i = 0; i < MT; ++i) {
-        const i32x8 v = lds_fragment(sta + frag_lo + i * 2048, sta + frag_hi + i * 2048);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) a[i][q] = widen8(v[2 * q], v[2 * q + 1]);
-      }
-#pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        const i32x8 v = lds_fragment(stb + frag_lo + j * 2048, stb + frag_hi + j * 2048);
-        f32x4 r{1.f, 1.f, 1.f, 1.f};
-        if (ROWS) r = *reinterpret_cast<const f32x4*>(ssb + 16 * j + 4 * g);
-        f32x4 d[MT];
-#pragma unroll
-        for (int i = 0; i < MT; ++i) d[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const bf16x8 b = widen8(v[2 * q], v[2 * q + 1]);
-#pragma unroll
-          for (int i = 0; i < MT; ++i)
-            d[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, a[i][q], d[i], 0, 0, 0);
-        }
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            acc[i][j][e] = fmaf(ROWS ? s[i] * r[e] : s[i], d[i][e], acc[i][j][e]);
-      }
-    }
-  }
-
-  if constexpr (KS == 2) {
-    // each group hands half of its pieces to the other and keeps the rest
-    __syncthreads();
-    f32x4* x = reinterpret_cast<f32x4*>(smem) + w * MT * NT * 64 + lane;
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-      for (int j = 0; j < NT; ++j)
-        if ((j < NT / 2) == (kg == 1)) x[(i * NT + j) * 64] = acc[i][j];
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-      for (int j = 0; j < NT; ++j)
-        if ((j < NT / 2) == (kg == 0)) acc[i][j] += x[(i * NT + j) * 64];
-  }
-  const bool whole = N % 4 == 0;  // rows of C keep four results together and aligned
-#pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    const int64_t m = m0 + (wm * MT + i) * 16 + c;
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      if (KS == 2 && (j < NT / 2) != (kg == 0)) continue;
-      const int64_t n = n0 + (wn * NT + j) * 16 + 4 * g;
-      if (m >= M || n >= N) continue;
-      const f32x4 v = acc[i][j];
-      if (whole) {
-        if (F32)
-          *reinterpret_cast<f32x4*>(static_cast<float*>(C) + m * N + n) = v;
-        else
-          *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(C) + m * N + n) =
-              u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+        for (int q = 0; q < 4; ++q)
+          d[u % 2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bw[q], aw[i][q], d[u % 2], 0, 0, 0);
       } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (n + e < N) store1<F32>(C, m * N + n + e, v[e]);
+        d[u % 2] = mfma16_e4m3(b[j % RING], a[i]);
       }
-    }
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (u == 0) {
+        scale(U - 1, s_last);
+#pragma unroll
+        for (int q = 0; q < MT; ++q) s[q] = ROWS ? s_next[q] : s_next[q] * sb_next;
+        s_last = s[MT - 1];
+        read_b(st, sc, 1);
+      } else {
+        scale(u - 1, s[(u - 1) % MT]);
+      }
+      if constexpr (i == 1 && j + 2 < NT) read_b(st, sc, j + 2);
+      if constexpr (u == U - MT) {
+        read_b(st_next, sc_next, 0);
+        read_s(sc_next);
+      }
+      if constexpr (u >= U - MT) read_a(st_next, i);
+      if constexpr (u >= TAIL) {
+#pragma unroll
+        for (int q = 0; q < EACH; ++q)
+          fetch.one((u - TAIL) * EACH + q, lds0 + (uint32_t)(it & 1) * S::STAGE, (it + 2) * KS + kg);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    });
   }
+  scale(U - 1, s_last);
+  barrier_vm<0>();  // the last blocks' DMA (zeros: past the end of K) has landed, too
+  if constexpr (KS > 1) {
+    // each group adds up and stores its share of the columns, in the groups' order
+    f32x4* const x = reinterpret_cast<f32x4*>(smem) + w * MT * NT * 64 + lane;
+    constexpr int GROUP = S::WAVES * MT * NT * 64;
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int jj = 0; jj < NT; ++jj)
+        if (jj * KS / NT != kg) x[kg * GROUP + (i * NT + jj) * 64] = acc[i][jj];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int jj = 0; jj < NT; ++jj)
+        if (jj * KS / NT == kg) {
+          f32x4 v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int q = 0; q < KS; ++q) v += q == kg ? acc[i][jj] : x[q * GROUP + (i * NT + jj) * 64];
+          acc[i][jj] = v;
+        }
+  }
+  auto mine = [&](int jj) { return jj * KS / NT == kg; };
+  const int64_t mw = m0 + wm * MT * 16 + c, nw = n0 + wn * NT * 16 + 4 * g;
+  if (rows_a == S::BM && rows_b == S::BN && N % 4 == 0) {
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int jj = 0; jj < NT; ++jj)
+        if (mine(jj)) store4<F32>(C, (mw + 16 * i) * N + nw + 16 * jj, acc[i][jj]);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int jj = 0; jj < NT; ++jj)
+      if (mine(jj)) store_edge<F32>(C, mw + 16 * i, M, nw + 16 * jj, N, acc[i][jj]);
 }
 
 template <int WM, int WN, int MT, int NT, int KS, bool F32, bool ROWS>
@@ -293,6 +402,107 @@ void launch_tile(const uint8_t* A, const float* sa, const uint8_t* B, const floa
                      0, s, A, sa, B, sb, M, N, K, C);
 }
 
+// Few rows of A (at most 16 MT): B is read once, straight into registers.  A
+// workgroup has 16 NT rows of B; its wavefronts take a run of the blocks along K
+// each, and their sums are added in order through LDS.
+constexpr int kFewWaves = 8;
+
+template <int MT, int NT, int DEPTH, bool F32, bool ROWS>
+__global__ __launch_bounds__(64 * kFewWaves) void gemm_scaled_few_kernel(
+    const uint8_t* __restrict__ A, const float* __restrict__ sa, const uint8_t* __restrict__ B,
+    const float* __restrict__ sb, int M, int64_t N, int64_t K, void* __restrict__ C) {
+  __shared__ f32x4 part[kFewWaves][MT * NT][64];
+  const int lane = lane_id(), wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
+  const int KB = (int)ceil_div(K, kScaleBlock);
+  const int64_t n0 = (int64_t)blockIdx.x * 16 * NT;
+  f32x4 acc[MT][NT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  // DEPTH blocks' operands are in flight together
+  const int per = (KB + kFewWaves - 1) / kFewWaves, end = per * (wave + 1) < KB ? per * (wave + 1) : KB;
+  for (int first = per * wave; first < end; first += DEPTH) {
+    i32x8 a[DEPTH][MT], b[DEPTH][NT];
+    float s[DEPTH][MT];
+    f32x4 r[DEPTH][NT];
+#pragma unroll
+    for (int q = 0; q < DEPTH; ++q) {
+      const int kb = first + q;
+      const bool in = kb < end;
+      const int64_t k = (int64_t)kb * kScaleBlock;
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        const int64_t n = n0 + 16 * j + c;
+        b[q][j] = load_fragment(B + n * K, in && n < N, K, k);
+      }
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        const int m = 16 * i + c;
+        a[q][i] = load_fragment(A + (int64_t)m * K, in && m < M, K, k);
+        s[q][i] = in && m < M ? sa[(int64_t)m * KB + kb] : 0.0f;
+      }
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        if (ROWS) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int64_t n = n0 + 16 * j + 4 * g + e;
+            r[q][j][e] = in && n < N ? sb[n * KB + kb] : 0.0f;
+          }
+        } else {
+          const int64_t n = n0 + 16 * j;
+          r[q][j][0] = in && n < N ? sb[n / kScaleBlock * KB + kb] : 0.0f;
+        }
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < DEPTH; ++q)
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          f32x4 d;
+          if constexpr (F32) {
+            d = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int h = 0; h < 8; h += 2)
+              d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(b[q][j][h], b[q][j][h + 1]),
+                                                          widen8(a[q][i][h], a[q][i][h + 1]), d, 0, 0, 0);
+          } else {
+            d = mfma16_e4m3(b[q][j], a[q][i]);
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            acc[i][j][e] = fmaf(s[q][i] * r[q][j][ROWS ? e : 0], d[e], acc[i][j][e]);
+        }
+  }
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) part[wave][i * NT + j][lane] = acc[i][j];
+  __syncthreads();
+  if (wave >= MT * NT) return;
+  f32x4 v = part[0][wave][lane];
+#pragma unroll
+  for (int q = 1; q < kFewWaves; ++q) v += part[q][wave][lane];
+  const int64_t m = wave / NT * 16 + c, n = n0 + wave % NT * 16 + 4 * g;
+  if (N % 4 == 0) {
+    if (m < M && n < N) store4<F32>(C, m * N + n, v);
+  } else {
+    store_edge<F32>(C, m, M, n, N, v);
+  }
+}
+
+template <int MT, int NT, int DEPTH, bool F32, bool ROWS>
+void launch_few(const uint8_t* A, const float* sa, const uint8_t* B, const float* sb, int64_t M,
+                int64_t N, int64_t K, void* C, hipStream_t s) {
+  static_assert(MT * NT <= kFewWaves, "a wavefront per piece of C");
+  hipLaunchKernelGGL((gemm_scaled_few_kernel<MT, NT, DEPTH, F32, ROWS>),
+                     dim3((unsigned)ceil_div(N, 16 * NT)), dim3(64 * kFewWaves), 0, s, A, sa, B, sb,
+                     (int)M, N, K, C);
+}
+
 }  // namespace
 
 hipError_t launch_gemm_scaled(const void* A, const float* sa, const void* B, const float* sb,
@@ -300,10 +510,20 @@ hipError_t launch_gemm_scaled(const void* A, const float* sa, const void* B, con
                               hipStream_t s) {
   const uint8_t* a = static_cast<const uint8_t*>(A);
   const uint8_t* b = static_cast<const uint8_t*>(B);
+  const bool wide = N >= 32 * 256;
+  const bool small = ceil_div(M, 64) * ceil_div(N, 64) <= 256;
   const bool large = !f32 && ceil_div(M, 256) * ceil_div(N, 256) >= 192;
 #define MHL_GEMM(F32, ROWS)                                                     \
   do {                                                                          \
-    if (large && !F32)                                                          \
+    if (M <= 16)                                                                \
+      launch_few<1, 1, 4, F32, ROWS>(a, sa, b, sb, M, N, K, C, s);              \
+    else if (M <= 32 && wide)                                                   \
+      launch_few<2, 2, 2, F32, ROWS>(a, sa, b, sb, M, N, K, C, s);              \
+    else if (M <= 32)                                                           \
+      launch_few<2, 1, 4, F32, ROWS>(a, sa, b, sb, M, N, K, C, s);              \
+    else if (small)                                                             \
+      launch_tile<2, 1, 2, 4, 4, F32, ROWS>(a, sa, b, sb, M, N, K, C, s);       \
+    else if (large && !F32)                                                     \
       launch_tile<4, 2, 4, 8, 1, false, ROWS>(a, sa, b, sb, M, N, K, C, s);     \
     else                                                                        \
       launch_tile<2, 2, 4, 4, 2, F32, ROWS>(a, sa, b, sb, M, N, K, C, s);       \

@@ -236,7 +236,11 @@ GEMM_SHAPES = [(1, 1, 16), (1, 7, 128), (2, 128, 400), (3, 1000, 144), (15, 16, 
                (17, 130, 1040), (31, 512, 2048), (33, 96, 16), (48, 257, 640), (63, 64, 128),
                (64, 512, 384), (65, 127, 272), (100, 300, 512), (127, 129, 128), (128, 128, 1024),
                (129, 384, 160), (255, 257, 256), (256, 256, 128), (300, 520, 896), (513, 640, 1152),
-               (1100, 1300, 336)]
+               (1100, 1300, 336),
+               # B of 8192 rows and more under few rows of A; over 256 tiles of 64 x 64; 192 tiles of
+               # 256 x 256 and more, whole and not
+               (20, 8209, 272), (32, 8192, 1152), (1030, 1100, 144), (1152, 1152, 1152),
+               (3600, 3401, 272), (4096, 3328, 640)]
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
@@ -258,7 +262,8 @@ def test_gemm(M, N, K, block, dtype):
 
 
 @pytest.mark.parametrize("M,N,K", [(1, 40, 272), (37, 100, 144), (64, 256, 2048), (130, 270, 400),
-                                   (300, 260, 640), (1000, 1024, 512)])
+                                   (300, 260, 640), (1000, 1024, 512), (31, 8200, 400),
+                                   (1100, 1200, 912), (3500, 3600, 400)])
 @pytest.mark.parametrize("block", [128, 1])
 def test_gemm_exact(M, N, K, block):
     """Small whole numbers under powers of two as scales: every sum is exact in
@@ -301,12 +306,12 @@ def test_gemm_empty():
         assert q.numel() == 0 and s.numel() == 0
 
 
-@pytest.mark.parametrize("M", [5, 70, 300])
+@pytest.mark.parametrize("M", [5, 70, 300, 1500])
 def test_gemm_special_values_stay_in_their_row(M):
     """A NaN in a row of A, or an infinite scale, reaches that row of C alone."""
     g = _gen(M)
     A, sa = mh.mhlmoe_quantize(_randn(g, M, 384))
-    B, sb = mh.mhlmoe_quantize(_randn(g, 200, 384), block_rows=128)
+    B, sb = mh.mhlmoe_quantize(_randn(g, 200 if M < 1000 else 1100, 384), block_rows=128)
     clean = mh.mhlmoe_gemm_scaled(A, sa, B, sb, dtype=F32)
     A.view(torch.uint8)[1, 130] = 0x7F
     sa[3, 2] = float("inf")
