@@ -571,19 +571,29 @@ def mhlmoe_layer_gelu_backward(X, W_router, W_in, W_out, idx, gate, dY, *, dX=No
 E4M3 = torch.float8_e4m3fn
 
 
-def _one_device(first, *others):
-    for t in others:
-        if isinstance(t, torch.Tensor) and t.device != first.device:
-            raise ValueError(f"tensors on {first.device} and {t.device}: one device is needed")
+def _at(t, name, dtype, shape, device):
+    """Address of a contiguous tensor on `device` (None -> NULL); the small
+    calls' time is the host's, so everything is looked at once."""
+    if t is None:
+        return None
+    try:
+        if (t.dtype is dtype and t.shape == shape and t.get_device() == device and device >= 0
+                and t.is_contiguous()):
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _dev(t, name, dtype, shape)  # says what is wrong, but for the device's number
+    raise ValueError(f"{name} is on {t.device}: all tensors must be on one GPU")
 
 
-def _launch(first, stream, call):
-    """call(stream) with the tensors' GPU as the current one."""
-    if first.device.type != "cuda" or first.device.index == torch.cuda.current_device():
-        _check(call(_stream(stream)))
+def _launch(device, stream, fn, *args):
+    """fn(*args, stream) with GPU number `device` as the current one."""
+    if device == torch.cuda.current_device():
+        s = torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream)
+        _check(fn(*args, s))
         return
-    with torch.cuda.device(first.device):
-        _check(call(_stream(stream)))
+    with torch.cuda.device(device):
+        _check(fn(*args, _stream(stream)))
 
 
 def _rows_cols(t, name):
@@ -604,28 +614,29 @@ def mhlmoe_rmsnorm(x, weight, eps, *, residual=None, quantized=False, sum=None, 
     float.  quantized: the norm in 8 bits (q e4m3 and scales per 128 columns)
     instead of y; pass y as well to have both.  Returns a dict with sum (with
     residual), y, q and scales."""
-    T, d = _rows_cols(x, "x")
-    dt = _dtype_code(x)
+    T, d = shape = _rows_cols(x, "x")
+    dt, dtype, dev, f32 = _dtype_code(x), x.dtype, x.get_device(), torch.float32
+    grid = (T, -(-d // 128))
     if residual is not None:
-        sum = _new(sum, (T, d), x.dtype, x)
+        sum = _new(sum, shape, dtype, x)
     if quantized:
-        q = _new(q, (T, d), E4M3, x)
-        scales = _new(scales, (T, -(-d // 128)), torch.float32, x)
+        q = _new(q, shape, E4M3, x)
+        scales = _new(scales, grid, f32, x)
     else:
         if q is not None or scales is not None:
             raise ValueError("q and scales are outputs of quantized=True")
-        y = _new(y, (T, d), x.dtype, x)
-    _one_device(x, weight, residual, sum, y, q, scales)
-    args = (_dev(x, "x"), _dev(residual, "residual", x.dtype, (T, d)),
-            _dev(weight, "weight", torch.float32, (d,)), T, d, float(eps), dt,
-            _dev(sum, "sum", x.dtype, (T, d)), _dev(y, "y", x.dtype, (T, d)),
-            _dev(q, "q", E4M3, (T, d)),
-            _dev(scales, "scales", torch.float32, (T, -(-d // 128))))
-    _launch(x, stream, lambda s: load_library().mhlmoe_rmsnorm(*args, s))
+        y = _new(y, shape, dtype, x)
+    _launch(dev, stream, load_library().mhlmoe_rmsnorm, _at(x, "x", dtype, shape, dev),
+            _at(residual, "residual", dtype, shape, dev), _at(weight, "weight", f32, (d,), dev), T, d,
+            eps, dt, _at(sum, "sum", dtype, shape, dev), _at(y, "y", dtype, shape, dev),
+            _at(q, "q", E4M3, shape, dev), _at(scales, "scales", f32, grid, dev))
     res = {}
-    for name, t in (("sum", sum), ("y", y), ("q", q), ("scales", scales)):
-        if t is not None:
-            res[name] = t
+    if sum is not None:
+        res["sum"] = sum
+    if y is not None:
+        res["y"] = y
+    if quantized:
+        res["q"], res["scales"] = q, scales
     return res
 
 
@@ -641,19 +652,18 @@ def mhlmoe_rmsnorm_backward(h, weight, eps, dy, *, dsum=None, dx=None, dweight=N
     """Backward of mhlmoe_rmsnorm from h, the forward's sum (x where there was
     no residual): returns (dx, dweight).  dsum: the gradient that reaches h
     past the norm; dx is the gradient of x and of residual."""
-    T, d = _rows_cols(h, "h")
-    dx = _new(dx, (T, d), h.dtype, h)
-    dweight = _new(dweight, (d,), torch.float32, h)
+    T, d = shape = _rows_cols(h, "h")
+    dt, dtype, dev, f32 = _dtype_code(h), h.dtype, h.get_device(), torch.float32
+    dx = _new(dx, shape, dtype, h)
+    dweight = _new(dweight, (d,), f32, h)
     if workspace is None:
         n = mhlmoe_rmsnorm_backward_workspace(T, d)
         workspace = torch.empty(max(n, 256), dtype=torch.uint8, device=h.device)
-    _one_device(h, weight, dy, dsum, dx, dweight, workspace)
-    args = (_dev(h, "h"), _dev(weight, "weight", torch.float32, (d,)),
-            _dev(dy, "dy", h.dtype, (T, d)), _dev(dsum, "dsum", h.dtype, (T, d)), T, d, float(eps),
-            _dtype_code(h), _dev(dx, "dx", h.dtype, (T, d)),
-            _dev(dweight, "dweight", torch.float32, (d,)),
-            _dev(workspace, "workspace", torch.uint8), workspace.numel())
-    _launch(h, stream, lambda s: load_library().mhlmoe_rmsnorm_backward(*args, s))
+    _launch(dev, stream, load_library().mhlmoe_rmsnorm_backward, _at(h, "h", dtype, shape, dev),
+            _at(weight, "weight", f32, (d,), dev), _at(dy, "dy", dtype, shape, dev),
+            _at(dsum, "dsum", dtype, shape, dev), T, d, eps, dt, _at(dx, "dx", dtype, shape, dev),
+            _at(dweight, "dweight", f32, (d,), dev),
+            _at(workspace, "workspace", torch.uint8, (workspace.numel(),), dev), workspace.numel())
     return dx, dweight
 
 
@@ -662,14 +672,14 @@ def mhlmoe_quantize(x, *, block_rows=1, transpose=False, q=None, scales=None, st
     block; with transpose, x's transpose, its rows padded with zeros to a
     multiple of 16.  Returns (q, scales)."""
     rows, cols = _rows_cols(x, "x")
-    a, k = (cols, -(-rows // 16) * 16) if transpose else (rows, cols)
+    dt, dev, f32 = _dtype_code(x), x.get_device(), torch.float32
+    a, k = shape = (cols, -(-rows // 16) * 16) if transpose else (rows, cols)
     grid = (-(-a // block_rows) if block_rows in (1, 128) else a, -(-k // 128))
-    q = _new(q, (a, k), E4M3, x)
-    scales = _new(scales, grid, torch.float32, x)
-    _one_device(x, q, scales)
-    args = (_dev(x, "x"), rows, cols, _dtype_code(x), int(block_rows), 1 if transpose else 0,
-            _dev(q, "q", E4M3, (a, k)), _dev(scales, "scales", torch.float32, grid))
-    _launch(x, stream, lambda s: load_library().mhlmoe_quantize(*args, s))
+    q = _new(q, shape, E4M3, x)
+    scales = _new(scales, grid, f32, x)
+    _launch(dev, stream, load_library().mhlmoe_quantize, _at(x, "x", x.dtype, x.shape, dev), rows,
+            cols, dt, block_rows, 1 if transpose else 0, _at(q, "q", E4M3, shape, dev),
+            _at(scales, "scales", f32, grid, dev))
     return q, scales
 
 
@@ -679,15 +689,13 @@ def mhlmoe_gemm_scaled(A, scale_a, B, scale_b, *, b_block_rows=128, dtype=torch.
     block of 128 along K: scale_a [M, KB], scale_b [ceil(N / b_block_rows), KB]."""
     M, K = _rows_cols(A, "A")
     N = _rows_cols(B, "B")[0]
-    KB = -(-K // 128)
+    KB, dev, f32 = -(-K // 128), A.get_device(), torch.float32
     nb = -(-N // b_block_rows) if b_block_rows in (1, 128) else N
     C = _new(C, (M, N), dtype, A)
-    _one_device(A, scale_a, B, scale_b, C)
-    f32 = torch.float32
-    args = (_dev(A, "A", E4M3), _dev(scale_a, "scale_a", f32, (M, KB)), _dev(B, "B", E4M3, (N, K)),
-            _dev(scale_b, "scale_b", f32, (nb, KB)), M, N, K, int(b_block_rows), _dtype_code(C),
-            _dev(C, "C", dtype, (M, N)))
-    _launch(A, stream, lambda s: load_library().mhlmoe_gemm_scaled(*args, s))
+    _launch(dev, stream, load_library().mhlmoe_gemm_scaled, _at(A, "A", E4M3, A.shape, dev),
+            _at(scale_a, "scale_a", f32, (M, KB), dev), _at(B, "B", E4M3, (N, K), dev),
+            _at(scale_b, "scale_b", f32, (nb, KB), dev), M, N, K, b_block_rows, _dtype_code(C),
+            _at(C, "C", dtype, (M, N), dev))
     return C
 
 
@@ -714,38 +722,40 @@ def mhlmoe_latent_layer_scaled(x, norm_weight, eps, W_in, scale_in, W_router, bi
     T, dm = _rows_cols(x, "x")
     Ne, dff, dh = W1.shape[1], W1.shape[2], W1.shape[3]
     Nh, N = n_heads, n_heads * dh
-    dt = _dtype_code(x)
+    dt, dtype, dev = _dtype_code(x), x.dtype, x.get_device()
     f32, i32 = torch.float32, torch.int32
-    out = _new(out, (T, dm), x.dtype, x)
+    out = _new(out, (T, dm), dtype, x)
     if residual is not None:
-        sum = _new(sum, (T, dm), x.dtype, x)
-    X_lat = _new(X_lat, (T, Nh, dh), x.dtype, x)
+        sum = _new(sum, (T, dm), dtype, x)
+    X_lat = _new(X_lat, (T, Nh, dh), dtype, x)
     if W_r is not None:
-        R_lat = _new(R_lat, (T, Nh, dh), x.dtype, x)
-    Y_lat = _new(Y_lat, (T, Nh, dh), x.dtype, x)
+        R_lat = _new(R_lat, (T, Nh, dh), dtype, x)
+    Y_lat = _new(Y_lat, (T, Nh, dh), dtype, x)
     idx = _new(idx, (T, Nh, top_k), i32, x)
     gate = _new(gate, (T, Nh, top_k), f32, x)
     counts = _new(counts, (Nh, Ne), i32, x)
     if workspace is None:
         n = mhlmoe_latent_layer_scaled_workspace(T, dm, Nh, dh, Ne, top_k, dff, dt)
         workspace = torch.empty(max(n, 256), dtype=torch.uint8, device=x.device)
-    _one_device(x, residual, norm_weight, W_in, scale_in, W_r, scale_r, W_router, bias, W1, W3, W2,
-                W_out, scale_out, out, sum, X_lat, R_lat, Y_lat, idx, gate, counts, workspace)
     grid = (-(-N // 128), -(-dm // 128))
-    args = (_dev(x, "x"), _dev(residual, "residual", x.dtype, (T, dm)),
-            _dev(norm_weight, "norm_weight", f32, (dm,)), float(eps),
-            _dev(W_in, "W_in", E4M3, (N, dm)), _dev(scale_in, "scale_in", f32, grid),
-            _dev(W_r, "W_r", E4M3, (N, dm)), _dev(scale_r, "scale_r", f32, grid),
-            _dev(W_router, "W_router", f32, (Nh, Ne, dh)), _dev(bias, "bias", f32, (Nh, Ne)),
-            _dev(W1, "W1", x.dtype, (Nh, Ne, dff, dh)), _dev(W3, "W3", x.dtype, (Nh, Ne, dff, dh)),
-            _dev(W2, "W2", x.dtype, (Nh, Ne, dh, dff)), _dev(W_out, "W_out", E4M3, (dm, N)),
-            _dev(scale_out, "scale_out", f32, grid[::-1]), T, dm, Nh, dh, Ne, top_k, dff, dt,
-            _dev(out, "out", x.dtype, (T, dm)), _dev(sum, "sum", x.dtype, (T, dm)),
-            _dev(X_lat, "X_lat", x.dtype, (T, Nh, dh)), _dev(R_lat, "R_lat", x.dtype, (T, Nh, dh)),
-            _dev(Y_lat, "Y_lat", x.dtype, (T, Nh, dh)), _dev(idx, "idx", i32, (T, Nh, top_k)),
-            _dev(gate, "gate", f32, (T, Nh, top_k)), _dev(counts, "counts", i32, (Nh, Ne)),
-            _dev(workspace, "workspace", torch.uint8), workspace.numel())
-    _launch(x, stream, lambda s: load_library().mhlmoe_latent_layer_scaled(*args, s))
+
+    def at(t, name, dtype, *shape):
+        return _at(t, name, dtype, shape, dev)
+
+    _launch(dev, stream, load_library().mhlmoe_latent_layer_scaled,
+            at(x, "x", dtype, T, dm), at(residual, "residual", dtype, T, dm),
+            at(norm_weight, "norm_weight", f32, dm), eps,
+            at(W_in, "W_in", E4M3, N, dm), at(scale_in, "scale_in", f32, *grid),
+            at(W_r, "W_r", E4M3, N, dm), at(scale_r, "scale_r", f32, *grid),
+            at(W_router, "W_router", f32, Nh, Ne, dh), at(bias, "bias", f32, Nh, Ne),
+            at(W1, "W1", dtype, Nh, Ne, dff, dh), at(W3, "W3", dtype, Nh, Ne, dff, dh),
+            at(W2, "W2", dtype, Nh, Ne, dh, dff), at(W_out, "W_out", E4M3, dm, N),
+            at(scale_out, "scale_out", f32, *grid[::-1]), T, dm, Nh, dh, Ne, top_k, dff, dt,
+            at(out, "out", dtype, T, dm), at(sum, "sum", dtype, T, dm),
+            at(X_lat, "X_lat", dtype, T, Nh, dh), at(R_lat, "R_lat", dtype, T, Nh, dh),
+            at(Y_lat, "Y_lat", dtype, T, Nh, dh), at(idx, "idx", i32, T, Nh, top_k),
+            at(gate, "gate", f32, T, Nh, top_k), at(counts, "counts", i32, Nh, Ne),
+            at(workspace, "workspace", torch.uint8, workspace.numel()), workspace.numel())
     res = {"out": out, "X_lat": X_lat, "Y_lat": Y_lat, "idx": idx, "gate": gate, "counts": counts}
     if residual is not None:
         res["sum"] = sum

@@ -9,10 +9,9 @@
 // The norm is that of the stored (rounded) h, so the backward, which has only
 // h, differentiates what the forward computed.  Sums are in fp32.
 //
-// Every element is read once: up to 16384 columns a row stays in the registers
-// of the lanes that normalise it, a wavefront (up to 4096 columns) or a
-// workgroup.  Wider rows, and rows whose width is no multiple of 8, are walked
-// twice by a workgroup (the second time out of the caches).
+// Every element is read once: a row stays in the registers of the lanes that
+// normalise it, 16 of them to a workgroup (NormForm).  Rows too wide for that
+// are walked twice by a workgroup (the second time out of the caches).
 
 #include "scaled_common.hpp"
 #include "scaled_launch.hpp"
@@ -24,12 +23,12 @@ constexpr int kNormThreads = 256;
 constexpr int kNormWaves = kNormThreads / kWave;
 constexpr unsigned kNormMaxGrid = 1u << 20;  // workgroups; rows beyond them are looped over
 
-// Sum over the lanes of a row: a wavefront, or the workgroup (whose
+// Sum over the lanes of a row: part of a wavefront, or the workgroup (whose
 // wavefronts' sums are added in their order).
 template <int LANES>
 __device__ __forceinline__ float row_sum(float v, float* lds) {
-  v = wave_sum(v);
-  if (LANES == kWave) return v;
+  v = lane_sum<(LANES < kWave ? LANES : kWave)>(v);
+  if (LANES <= kWave) return v;
   __syncthreads();  // the readers of the sums before
   if (lane_id() == 0) lds[threadIdx.x >> 6] = v;
   __syncthreads();
@@ -39,14 +38,19 @@ __device__ __forceinline__ float row_sum(float v, float* lds) {
   return s;
 }
 
-// Writes eight columns of y: in the type, and/or in 8 bits with the scale of
-// the 16 lanes' 128 columns.  All lanes of the wavefront take part.
-template <bool F32>
-__device__ __forceinline__ void write_y(const float (&y)[8], bool ok, int64_t row, int col, int d,
+// Writes a lane's columns of y: in the type, and/or (VEC 8) in 8 bits with the
+// scale of the 16 lanes' 128 columns.  All 16 lanes take part.
+template <bool F32, int VEC>
+__device__ __forceinline__ void write_y(const float (&y)[VEC], bool ok, int64_t row, int col, int d,
                                         void* out, uint8_t* q, float* scales) {
   const int64_t at = row * d + col;
-  if (out && ok) store8<F32>(out, at, pack8<F32>(y));
-  if (q) {
+  if (out && ok) {
+    Piece<F32, VEC> p;
+    p.set(y);
+    p.store(out, at);
+  }
+  if constexpr (VEC == 8) {
+    if (!q) return;
     uint32_t m = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -67,14 +71,17 @@ __device__ __forceinline__ void write_y(const float (&y)[8], bool ok, int64_t ro
   }
 }
 
-__device__ __forceinline__ void load_weight(const float* w, int col, bool ok, float (&f)[8]) {
-  unpack8<true>(load8<true>(w, col, ok), f);
+template <int VEC>
+__device__ __forceinline__ void load_weight(const float* w, int col, bool ok, float (&f)[VEC]) {
+  Piece<true, VEC> p;
+  p.load(w, col, ok);
+  p.get(f);
 }
 
-// LANES lanes per row, each with NV pieces of 8 columns; d a multiple of 8,
-// at most LANES * NV * 8.  residual == NULL: h is x, and sum is not written.
+// LANES lanes per row, each with NV pieces of VEC columns; d a multiple of VEC,
+// at most LANES * NV * VEC.  residual == NULL: h is x, and sum is not written.
 // sum may be x or residual, y may be x: a lane stores only what it has read.
-template <bool F32, int LANES, int NV>
+template <bool F32, int VEC, int LANES, int NV>
 __global__ __launch_bounds__(kNormThreads) void rmsnorm_kernel(
     const void* x, const void* residual, const float* __restrict__ w, int64_t T, int d, float eps,
     void* sum, void* y, uint8_t* q, float* scales) {
@@ -83,47 +90,47 @@ __global__ __launch_bounds__(kNormThreads) void rmsnorm_kernel(
   const int l = threadIdx.x % LANES;
   for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES; row < T;
        row += (int64_t)gridDim.x * kRows) {
-    Raw8<F32> hr[NV], rr[NV];
+    Piece<F32, VEC> hr[NV], rr[NV];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int col = (v * LANES + l) * 8;
-      hr[v] = load8<F32>(x, row * d + col, col < d);
+      const int col = (v * LANES + l) * VEC;
+      hr[v].load(x, row * d + col, col < d);
     }
     if (residual) {
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
-        const int col = (v * LANES + l) * 8;
-        rr[v] = load8<F32>(residual, row * d + col, col < d);
+        const int col = (v * LANES + l) * VEC;
+        rr[v].load(residual, row * d + col, col < d);
       }
     }
     float ss = 0.0f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int col = (v * LANES + l) * 8;
-      float h[8];
-      unpack8<F32>(hr[v], h);
+      const int col = (v * LANES + l) * VEC;
+      float h[VEC];
+      hr[v].get(h);
       if (residual) {
-        float r[8];
-        unpack8<F32>(rr[v], r);
+        float r[VEC];
+        rr[v].get(r);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) h[i] += r[i];
-        hr[v] = pack8<F32>(h);
-        if (col < d) store8<F32>(sum, row * d + col, hr[v]);
-        unpack8<F32>(hr[v], h);
+        for (int i = 0; i < VEC; ++i) h[i] += r[i];
+        hr[v].set(h);
+        if (col < d) hr[v].store(sum, row * d + col);
+        hr[v].get(h);
       }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) ss = fmaf(h[i], h[i], ss);
+      for (int i = 0; i < VEC; ++i) ss = fmaf(h[i], h[i], ss);
     }
     const float rs = 1.0f / sqrtf(row_sum<LANES>(ss, lds) / (float)d + eps);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int col = (v * LANES + l) * 8;
-      float h[8], wf[8];
-      unpack8<F32>(hr[v], h);
-      load_weight(w, col, col < d, wf);
+      const int col = (v * LANES + l) * VEC;
+      float h[VEC], wf[VEC];
+      hr[v].get(h);
+      load_weight<VEC>(w, col, col < d, wf);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) h[i] = h[i] * rs * wf[i];
-      write_y<F32>(h, col < d, row, col, d, y, q, scales);
+      for (int i = 0; i < VEC; ++i) h[i] = h[i] * rs * wf[i];
+      write_y<F32, VEC>(h, col < d, row, col, d, y, q, scales);
     }
   }
 }
@@ -140,44 +147,35 @@ __global__ __launch_bounds__(kNormThreads) void rmsnorm_wide_kernel(
     float ss = 0.0f;
     for (int c = threadIdx.x * VEC; c < d; c += kNormThreads * VEC) {
       const int64_t at = row * d + c;
-      if constexpr (VEC == 8) {
-        float h[8];
-        unpack8<F32>(load8<F32>(x, at, true), h);
-        if (residual) {
-          float r[8];
-          unpack8<F32>(load8<F32>(residual, at, true), r);
+      Piece<F32, VEC> p;
+      float h[VEC];
+      p.load(x, at, true);
+      p.get(h);
+      if (residual) {
+        float r[VEC];
+        p.load(residual, at, true);
+        p.get(r);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) h[i] += r[i];
-          const Raw8<F32> p = pack8<F32>(h);
-          store8<F32>(sum, at, p);
-          unpack8<F32>(p, h);
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) ss = fmaf(h[i], h[i], ss);
-      } else {
-        float h = load1<F32>(x, at);
-        if (residual) {
-          h = round1<F32>(h + load1<F32>(residual, at));
-          store1<F32>(sum, at, h);
-        }
-        ss = fmaf(h, h, ss);
+        for (int i = 0; i < VEC; ++i) h[i] += r[i];
+        p.set(h);
+        p.store(sum, at);
+        p.get(h);
       }
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) ss = fmaf(h[i], h[i], ss);
     }
     const float rs = 1.0f / sqrtf(row_sum<kNormThreads>(ss, lds) / (float)d + eps);
-    if constexpr (VEC == 8) {
-      // whole wavefronts to the end: the 8-bit output reduces over 16 lanes
-      for (int c0 = 0; c0 < d; c0 += kNormThreads * VEC) {
-        const int c = c0 + threadIdx.x * VEC;
-        float h[8], wf[8];
-        unpack8<F32>(load8<F32>(h_src, row * d + c, c < d), h);
-        load_weight(w, c, c < d, wf);
+    // whole wavefronts to the end: the 8-bit output reduces over 16 lanes
+    for (int c0 = 0; c0 < d; c0 += kNormThreads * VEC) {
+      const int c = c0 + threadIdx.x * VEC;
+      Piece<F32, VEC> p;
+      float h[VEC], wf[VEC];
+      p.load(h_src, row * d + c, c < d);
+      p.get(h);
+      load_weight<VEC>(w, c, c < d, wf);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) h[i] = h[i] * rs * wf[i];
-        write_y<F32>(h, c < d, row, c, d, y, q, scales);
-      }
-    } else {
-      for (int c = threadIdx.x; c < d; c += kNormThreads)
-        store1<F32>(y, row * d + c, load1<F32>(h_src, row * d + c) * rs * w[c]);
+      for (int i = 0; i < VEC; ++i) h[i] = h[i] * rs * wf[i];
+      write_y<F32, VEC>(h, c < d, row, c, d, y, q, scales);
     }
   }
 }
@@ -186,45 +184,45 @@ __global__ __launch_bounds__(kNormThreads) void rmsnorm_wide_kernel(
 // blockIdx.x + gridDim.x, ... (of kRows rows each) with its columns' dw in
 // registers and leaves their sum in part[blockIdx.x][d], its rows' lanes added
 // in order.  dx may be dy or dsum.
-template <bool F32, int LANES, int NV>
+template <bool F32, int VEC, int LANES, int NV>
 __global__ __launch_bounds__(kNormThreads) void rmsnorm_bwd_kernel(
     const void* h_src, const float* __restrict__ w, const void* dy, const void* dsum, int64_t T,
     int d, float eps, void* dx, float* __restrict__ part) {
   constexpr int kRows = kNormThreads / LANES;
   __shared__ float lds[2 * kNormWaves];
-  __shared__ float add[kRows > 1 ? kNormThreads * 8 : 1];
+  __shared__ float add[kRows > 1 ? kNormThreads * VEC : 1];
   const int l = threadIdx.x % LANES;
-  float dw[NV][8];
+  float dw[NV][VEC];
 #pragma unroll
   for (int v = 0; v < NV; ++v)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) dw[v][i] = 0.0f;
+    for (int i = 0; i < VEC; ++i) dw[v][i] = 0.0f;
   for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES; row < T;
        row += (int64_t)gridDim.x * kRows) {
-    Raw8<F32> hr[NV], gr[NV], sr[NV];
+    Piece<F32, VEC> hr[NV], gr[NV], sr[NV];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int col = (v * LANES + l) * 8;
-      hr[v] = load8<F32>(h_src, row * d + col, col < d);
-      gr[v] = load8<F32>(dy, row * d + col, col < d);
+      const int col = (v * LANES + l) * VEC;
+      hr[v].load(h_src, row * d + col, col < d);
+      gr[v].load(dy, row * d + col, col < d);
     }
     if (dsum) {
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
-        const int col = (v * LANES + l) * 8;
-        sr[v] = load8<F32>(dsum, row * d + col, col < d);
+        const int col = (v * LANES + l) * VEC;
+        sr[v].load(dsum, row * d + col, col < d);
       }
     }
     float ss = 0.0f, gh = 0.0f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int col = (v * LANES + l) * 8;
-      float h[8], g[8], wf[8];
-      unpack8<F32>(hr[v], h);
-      unpack8<F32>(gr[v], g);
-      load_weight(w, col, col < d, wf);
+      const int col = (v * LANES + l) * VEC;
+      float h[VEC], g[VEC], wf[VEC];
+      hr[v].get(h);
+      gr[v].get(g);
+      load_weight<VEC>(w, col, col < d, wf);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < VEC; ++i) {
         ss = fmaf(h[i], h[i], ss);
         gh = fmaf(g[i] * wf[i], h[i], gh);
       }
@@ -235,32 +233,33 @@ __global__ __launch_bounds__(kNormThreads) void rmsnorm_bwd_kernel(
     const float k = gh / (float)d * rs * rs;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int col = (v * LANES + l) * 8;
-      float h[8], g[8], wf[8], s[8];
-      unpack8<F32>(hr[v], h);
-      unpack8<F32>(gr[v], g);
-      load_weight(w, col, col < d, wf);
-      if (dsum) unpack8<F32>(sr[v], s);
+      const int col = (v * LANES + l) * VEC;
+      float h[VEC], g[VEC], wf[VEC], s[VEC];
+      hr[v].get(h);
+      gr[v].get(g);
+      load_weight<VEC>(w, col, col < d, wf);
+      if (dsum) sr[v].get(s);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < VEC; ++i) {
         dw[v][i] = fmaf(g[i], h[i] * rs, dw[v][i]);
         const float t = rs * fmaf(-h[i], k, g[i] * wf[i]);
         h[i] = dsum ? s[i] + t : t;
       }
-      if (col < d) store8<F32>(dx, row * d + col, pack8<F32>(h));
+      hr[v].set(h);
+      if (col < d) hr[v].store(dx, row * d + col);
     }
   }
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
-    const int col = (v * LANES + l) * 8;
+    const int col = (v * LANES + l) * VEC;
     if (kRows > 1) {
       __syncthreads();
 #pragma unroll
-      for (int i = 0; i < 8; ++i) add[i * kNormThreads + threadIdx.x] = dw[v][i];
+      for (int i = 0; i < VEC; ++i) add[i * kNormThreads + threadIdx.x] = dw[v][i];
       __syncthreads();
       if (threadIdx.x < LANES) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < VEC; ++i) {
           float t = add[i * kNormThreads + l];
 #pragma unroll
           for (int r = 1; r < kRows; ++r) t += add[i * kNormThreads + r * LANES + l];
@@ -268,8 +267,11 @@ __global__ __launch_bounds__(kNormThreads) void rmsnorm_bwd_kernel(
         }
       }
     }
-    if (threadIdx.x < LANES && col < d)
-      store8<true>(part, (int64_t)blockIdx.x * d + col, pack8<true>(dw[v]));
+    if (threadIdx.x < LANES && col < d) {
+      Piece<true, VEC> p;
+      p.set(dw[v]);
+      p.store(part, (int64_t)blockIdx.x * d + col);
+    }
   }
 }
 
@@ -346,34 +348,41 @@ unsigned norm_grid(int64_t rows, int per_wg, unsigned most) {
 
 }  // namespace
 
+// The register forms: VEC, LANES, NV of NormForm's members.
+#define MHL_NORM_FORMS(F32, KERNEL)                        \
+  case NormForm::kPart16: KERNEL(F32, 8, 16, 1); break;    \
+  case NormForm::kPart32: KERNEL(F32, 8, 32, 1); break;    \
+  case NormForm::kWave1: KERNEL(F32, 8, 64, 1); break;     \
+  case NormForm::kWave2: KERNEL(F32, 8, 64, 2); break;     \
+  case NormForm::kWave4: KERNEL(F32, 8, 64, 4); break;     \
+  case NormForm::kWave8: KERNEL(F32, 8, 64, 8); break;     \
+  case NormForm::kGroup4: KERNEL(F32, 8, 256, 4); break;   \
+  case NormForm::kGroup8: KERNEL(F32, 8, 256, 8); break;   \
+  case NormForm::kOdd16: KERNEL(F32, 1, 16, 4); break;     \
+  case NormForm::kOddWave: KERNEL(F32, 1, 64, 8); break;   \
+  case NormForm::kOddGroup: KERNEL(F32, 1, 256, 16); break;
+
 hipError_t launch_rmsnorm(const void* x, const void* residual, const float* w, int64_t T, int d,
                           float eps, bool f32, void* sum, void* y, void* q, float* scales,
                           hipStream_t s) {
   uint8_t* q8 = static_cast<uint8_t*>(q);
-#define MHL_NORM(F32, LANES, NV)                                                                   \
-  hipLaunchKernelGGL((rmsnorm_kernel<F32, LANES, NV>),                                             \
+#define MHL_NORM(F32, VEC, LANES, NV)                                                              \
+  hipLaunchKernelGGL((rmsnorm_kernel<F32, VEC, LANES, NV>),                                        \
                      dim3(norm_grid(T, kNormThreads / LANES, kNormMaxGrid)), dim3(kNormThreads), 0, \
                      s, x, residual, w, T, d, eps, sum, y, q8, scales)
 #define MHL_NORM_WIDE(F32, VEC)                                                                   \
   hipLaunchKernelGGL((rmsnorm_wide_kernel<F32, VEC>), dim3(norm_grid(T, 1, kNormMaxGrid)),        \
                      dim3(kNormThreads), 0, s, x, residual, w, T, d, eps, sum, y, q8, scales)
-#define MHL_NORM_TYPE(F32)             \
-  do {                                 \
-    switch (norm_form(d)) {            \
-      case NormForm::kWave1: MHL_NORM(F32, 64, 1); break;   \
-      case NormForm::kWave2: MHL_NORM(F32, 64, 2); break;   \
-      case NormForm::kWave4: MHL_NORM(F32, 64, 4); break;   \
-      case NormForm::kWave8: MHL_NORM(F32, 64, 8); break;   \
-      case NormForm::kGroup4: MHL_NORM(F32, 256, 4); break; \
-      case NormForm::kGroup8: MHL_NORM(F32, 256, 8); break; \
-      case NormForm::kWide8: MHL_NORM_WIDE(F32, 8); break;  \
-      case NormForm::kWide1: MHL_NORM_WIDE(F32, 1); break;  \
-    }                                  \
-  } while (0)
+#define MHL_NORM_TYPE(F32)                                       \
+  switch (norm_form(d)) {                                        \
+    MHL_NORM_FORMS(F32, MHL_NORM)                                \
+    case NormForm::kWide8: MHL_NORM_WIDE(F32, 8); break;         \
+    case NormForm::kWide1: MHL_NORM_WIDE(F32, 1); break;         \
+  }
   if (f32)
-    MHL_NORM_TYPE(true);
+    MHL_NORM_TYPE(true)
   else
-    MHL_NORM_TYPE(false);
+    MHL_NORM_TYPE(false)
 #undef MHL_NORM_TYPE
 #undef MHL_NORM_WIDE
 #undef MHL_NORM
@@ -384,30 +393,23 @@ hipError_t launch_rmsnorm_bwd(const void* h, const float* w, const void* dy, con
                               int64_t T, int d, float eps, bool f32, void* dx, float* part,
                               float* rows, hipStream_t s) {
   const unsigned n = (unsigned)rmsnorm_bwd_parts(T, d);
-#define MHL_NORM(F32, LANES, NV)                                                              \
-  hipLaunchKernelGGL((rmsnorm_bwd_kernel<F32, LANES, NV>), dim3(n), dim3(kNormThreads), 0, s, h, \
-                     w, dy, dsum, T, d, eps, dx, part)
+#define MHL_NORM(F32, VEC, LANES, NV)                                                              \
+  hipLaunchKernelGGL((rmsnorm_bwd_kernel<F32, VEC, LANES, NV>), dim3(n), dim3(kNormThreads), 0, s, \
+                     h, w, dy, dsum, T, d, eps, dx, part)
 #define MHL_NORM_TYPE(F32)                                                                       \
-  do {                                                                                           \
-    switch (norm_form(d)) {                                                                      \
-      case NormForm::kWave1: MHL_NORM(F32, 64, 1); break;                                        \
-      case NormForm::kWave2: MHL_NORM(F32, 64, 2); break;                                        \
-      case NormForm::kWave4: MHL_NORM(F32, 64, 4); break;                                        \
-      case NormForm::kWave8: MHL_NORM(F32, 64, 8); break;                                        \
-      case NormForm::kGroup4: MHL_NORM(F32, 256, 4); break;                                      \
-      case NormForm::kGroup8: MHL_NORM(F32, 256, 8); break;                                      \
-      default:                                                                                   \
-        hipLaunchKernelGGL((rmsnorm_bwd_wide_kernel<F32>), dim3(norm_grid(T, 1, kNormMaxGrid)),  \
-                           dim3(kNormThreads), 0, s, h, w, dy, dsum, T, d, eps, rows, rows + T); \
-        hipLaunchKernelGGL((rmsnorm_bwd_columns_kernel<F32>),                                    \
-                           dim3((unsigned)ceil_div(d, kNormThreads), n), dim3(kNormThreads), 0, s, h, w, \
-                           dy, dsum, T, d, rows, rows + T, dx, part);                            \
-    }                                                                                            \
-  } while (0)
+  switch (norm_form(d)) {                                                                        \
+    MHL_NORM_FORMS(F32, MHL_NORM)                                                                \
+    default:                                                                                     \
+      hipLaunchKernelGGL((rmsnorm_bwd_wide_kernel<F32>), dim3(norm_grid(T, 1, kNormMaxGrid)),    \
+                         dim3(kNormThreads), 0, s, h, w, dy, dsum, T, d, eps, rows, rows + T);   \
+      hipLaunchKernelGGL((rmsnorm_bwd_columns_kernel<F32>),                                      \
+                         dim3((unsigned)ceil_div(d, kNormThreads), n), dim3(kNormThreads), 0, s, \
+                         h, w, dy, dsum, T, d, rows, rows + T, dx, part);                        \
+  }
   if (f32)
-    MHL_NORM_TYPE(true);
+    MHL_NORM_TYPE(true)
   else
-    MHL_NORM_TYPE(false);
+    MHL_NORM_TYPE(false)
 #undef MHL_NORM_TYPE
 #undef MHL_NORM
   return hipGetLastError();

@@ -77,10 +77,13 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_tile_kernel(
   __shared__ __align__(16) uint8_t turned[TRANSPOSE ? kScaleBlock * kScaleBlock : 16];
   const int tid = threadIdx.x, wave = tid >> 6;
   const int cg = tid % 16, rg = tid / 16;
-  // the tiles of one row of tiles of q on consecutive workgroups
+  // an accelerator die's workgroups take a contiguous run of tiles, along q's
+  // rows: where those are no multiple of 128 bytes apart, two tiles share lines
   const int64_t tiles_r = ceil_div(rows, kScaleBlock), tiles_c = ceil_div(cols, kScaleBlock);
-  const int64_t tr = TRANSPOSE ? blockIdx.x % tiles_r : blockIdx.x / tiles_c;
-  const int64_t tc = TRANSPOSE ? blockIdx.x / tiles_r : blockIdx.x % tiles_c;
+  const uint32_t xcd = blockIdx.x % kXcds, per = gridDim.x / kXcds, rem = gridDim.x % kXcds;
+  const uint32_t tile = xcd * per + (xcd < rem ? xcd : rem) + blockIdx.x / kXcds;
+  const int64_t tr = TRANSPOSE ? tile % tiles_r : tile / tiles_c;
+  const int64_t tc = TRANSPOSE ? tile / tiles_r : tile % tiles_c;
   const int64_t r0 = tr * kScaleBlock + rg * 8, c0 = tc * kScaleBlock + cg * 8;
 
   Raw8<F32> raw[8];

@@ -88,6 +88,27 @@ __device__ __forceinline__ void store1(void* p, int64_t at, float v) {
     reinterpret_cast<uint16_t*>(p)[at] = (uint16_t)pack_bf16x2(v, v);
 }
 
+// VEC (8 or 1) consecutive elements.
+template <bool F32, int VEC>
+struct Piece {
+  Raw8<F32> r;
+  __device__ __forceinline__ void load(const void* p, int64_t at, bool ok) { r = load8<F32>(p, at, ok); }
+  __device__ __forceinline__ void get(float (&f)[8]) const { unpack8<F32>(r, f); }
+  __device__ __forceinline__ void set(const float (&f)[8]) { r = pack8<F32>(f); }  // rounds
+  __device__ __forceinline__ void store(void* p, int64_t at) const { store8<F32>(p, at, r); }
+};
+template <bool F32>
+struct Piece<F32, 1> {
+  float v;
+  __device__ __forceinline__ void load(const void* p, int64_t at, bool ok) {
+    v = 0.0f;
+    if (ok) v = load1<F32>(p, at);
+  }
+  __device__ __forceinline__ void get(float (&f)[1]) const { f[0] = v; }
+  __device__ __forceinline__ void set(const float (&f)[1]) { v = round1<F32>(f[0]); }
+  __device__ __forceinline__ void store(void* p, int64_t at) const { store1<F32>(p, at, v); }
+};
+
 // The bits of |v|: ordered as integers they order magnitudes, with infinity
 // above every finite value and NaN above infinity, so one integer maximum
 // finds a block's largest magnitude and lets no NaN pass unseen.
@@ -107,11 +128,12 @@ __device__ __forceinline__ uint32_t max16(uint32_t v) {
   return dpp_max<0x140>(v);  // row_mirror
 }
 
-// Sum over the wavefront, the same in every lane (each step adds a pair's two
-// values, whose sum does not depend on their order).
-__device__ __forceinline__ float wave_sum(float v) {
+// Sum over aligned groups of LANES lanes, the same in each of them (each step
+// adds a pair's two values, whose sum does not depend on their order).
+template <int LANES>
+__device__ __forceinline__ float lane_sum(float v) {
 #pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) v += __shfl_xor(v, d, kWave);
+  for (int d = 1; d < LANES; d <<= 1) v += __shfl_xor(v, d, kWave);
   return v;
 }
 

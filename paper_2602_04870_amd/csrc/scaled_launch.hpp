@@ -8,20 +8,38 @@
 
 namespace mhl {
 
-// How a row of d columns is held by the norm kernels: in the registers of a
-// wavefront, 8 to 64 columns per lane (up to 4096 columns; no barrier, and four rows per
-// workgroup in flight), in those of a workgroup (up to 16384), or (wider, or
-// no multiple of 8) not at all.
-enum class NormForm { kWave1, kWave2, kWave4, kWave8, kGroup4, kGroup8, kWide8, kWide1 };
+// How a row of d columns is held by the norm kernels.  Multiples of 8 by pieces
+// of 8 columns: in the registers of 16 or 32 lanes (up to 128 or 256 columns),
+// of a wavefront (up to 4096, 1 to 8 pieces per lane; no barrier, four rows per
+// workgroup) or of a workgroup (up to 16384).  Other widths column by column: 16
+// lanes (up to 64 columns), a wavefront (512), a workgroup (4096).  Wider rows
+// are not held at all.
+enum class NormForm {
+  kPart16, kPart32, kWave1, kWave2, kWave4, kWave8, kGroup4, kGroup8,
+  kOdd16, kOddWave, kOddGroup, kWide8, kWide1
+};
 inline NormForm norm_form(int d) {
-  if (d % 8 != 0) return NormForm::kWide1;
-  return d <= 512     ? NormForm::kWave1
+  if (d % 8 != 0)
+    return d <= 64     ? NormForm::kOdd16
+           : d <= 512  ? NormForm::kOddWave
+           : d <= 4096 ? NormForm::kOddGroup
+                       : NormForm::kWide1;
+  return d <= 128     ? NormForm::kPart16
+         : d <= 256   ? NormForm::kPart32
+         : d <= 512   ? NormForm::kWave1
          : d <= 1024  ? NormForm::kWave2
          : d <= 2048  ? NormForm::kWave4
          : d <= 4096  ? NormForm::kWave8
          : d <= 8192  ? NormForm::kGroup4
          : d <= 16384 ? NormForm::kGroup8
                       : NormForm::kWide8;
+}
+// Rows that a workgroup of the register forms has at once.
+inline int norm_rows(NormForm f) {
+  return f == NormForm::kPart16 || f == NormForm::kOdd16 ? 16
+         : f == NormForm::kPart32                        ? 8
+         : f == NormForm::kGroup4 || f == NormForm::kGroup8 || f == NormForm::kOddGroup ? 1
+                                                                                        : 4;
 }
 
 // h = round(x + residual) to sum (residual NULL: h = x, sum not written), the
@@ -34,13 +52,15 @@ hipError_t launch_rmsnorm(const void* x, const void* residual, const float* w, i
 // The norm's gradient: dx, and dw as rmsnorm_bwd_parts partial rows of d
 // floats, which launch_rmsnorm_dw adds in order.  rows: 2 T floats where
 // rmsnorm_bwd_wide, else unused.
-inline bool rmsnorm_bwd_wide(int d) { return d % 8 != 0 || d > 16384; }
+inline bool rmsnorm_bwd_wide(int d) {
+  return norm_form(d) == NormForm::kWide8 || norm_form(d) == NormForm::kWide1;
+}
 inline int64_t rmsnorm_bwd_parts(int64_t T, int d) {
   if (rmsnorm_bwd_wide(d)) {  // chunks of rows under each 256 columns
     const int64_t most = (int64_t(1) << 19) / d > 16 ? (int64_t(1) << 19) / d : 16;
     return ceil_div(T, 8) < most ? ceil_div(T, 8) : most;
   }
-  const int64_t n = d > 4096 ? T : ceil_div(T, 4);  // workgroups, two per CU at most
+  const int64_t n = ceil_div(T, norm_rows(norm_form(d)));  // workgroups, two per CU at most
   return n < 512 ? n : 512;
 }
 hipError_t launch_rmsnorm_bwd(const void* h, const float* w, const void* dy, const void* dsum,

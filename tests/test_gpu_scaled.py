@@ -35,10 +35,10 @@ def _guarded(shape, dtype, fill=93):
     return t, untouched
 
 
-# widths of every form of the kernels: one lane short of full, full, odd, and
-# wider than the registers' forms
-WIDTHS = [1, 7, 8, 16, 120, 128, 136, 512, 520, 1000, 1001, 1024, 2040, 2048, 4096, 4112, 8192,
-          12304, 16384, 16400]
+# widths of every form of the kernels: full, one short of it, one past it, odd,
+# and wider than the registers' forms
+WIDTHS = [1, 7, 8, 16, 28, 63, 65, 100, 112, 128, 136, 250, 256, 264, 512, 513, 520, 1000, 1001,
+          1024, 1032, 2048, 2056, 4095, 4096, 4097, 4112, 8192, 8208, 12304, 16384, 16400, 20001]
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
