@@ -199,12 +199,18 @@ __device__ __forceinline__ Fetch<S, KS, ROWS> make_fetch(const uint8_t* A, const
   return f;
 }
 
-// Blocks of A and B go by LDS DMA into one of two stages
-// while the other is multiplied; rows of 128 bytes have their 16-byte pieces
-// XOR-ed by the row's low three bits, which makes the fragments' 16-byte reads
-// free of bank conflicts.  One barrier per block: it waits for the next
-// block's DMA, issued a block earlier.  (Past the last block it fills a stage
-// with zeros that nobody reads.)
+// Blocks of A and B go by LDS DMA into one of two stages while the other is
+// multiplied; rows of 128 bytes have their 16-byte pieces XOR-ed by the row's low
+// three bits, which makes the fragments' 16-byte reads free of bank conflicts.
+// One barrier per block: it waits for the next block's DMA, issued a block
+// earlier.  (Past the last block it fills a stage with zeros that nobody reads.)
+//
+// What bounds it at 8192 x 8192 x 8192 (456 us, 2.41 PFLOP/s; parts left out in
+// turn, same box): MFMAs on changing operands 256 us at the card's power limit,
+// with the LDS reads 338, with the FMAs 378, with the DMA 456; the DMA alone 317.
+// None of these waits for another (neither the barrier nor the wait for DMA
+// changes it by more than 5%): they share the clock that the power allows, 1.95
+// GHz here against 2.34 for the MFMAs alone.
 template <class S, int WM, int WN, int MT, int NT, int KS, bool F32, bool ROWS>
 __global__ __launch_bounds__(S::THREADS) void gemm_scaled_kernel(
     const uint8_t* __restrict__ A, const float* __restrict__ sa, const uint8_t* __restrict__ B,
@@ -262,13 +268,14 @@ __global__ __launch_bounds__(S::THREADS) void gemm_scaled_kernel(
   fetch.scales(lds0 + S::SCALES, 0);
   fetch.all(lds0, kg);
   // Unit u of a block is one MFMA (fp32 results: four, on widened pieces): A's
-  // piece i = u % MT by B's piece j = u / MT.  B's pieces are read two ahead.  The barrier stands two pieces before
-  // the block's end, when every read of the block is done and the next block's
-  // DMA (issued there in the block before) has had a block's time to land:
-  // behind it the last two pieces' MFMAs have their operands in registers, and
-  // the next block's first ones are read beneath them, A's piece i as soon as
-  // this block is done with its own.  So no wavefront waits for LDS where a
-  // block begins.  The FMAs of a unit follow the next unit's MFMA, across
+  // piece i = u % MT by B's piece j = u / MT.  B's pieces are read two ahead.
+  // The barrier stands two pieces before the block's end, when every read of the
+  // block is done and the next block's DMA (issued there in the block before) has
+  // had a block's time to land: behind it the last two pieces' MFMAs have their
+  // operands in registers, and the next block's first ones are read beneath them,
+  // A's piece i as soon as this block is done with its own.  So no wavefront waits
+  // for LDS where a block begins (8192 x 8192 x 8192: 517 us with the barrier
+  // there, 457 like this).  The FMAs of a unit follow the next unit's MFMA, across
   // blocks, too.  sched_barrier keeps this order; the compiler would read each
   // fragment right before its use.
   constexpr int U = MT * NT, TAIL = U - 2 * MT, RING = NT % 4 == 0 && NT % 3 != 2 ? 4 : 3;
@@ -510,32 +517,35 @@ hipError_t launch_gemm_scaled(const void* A, const float* sa, const void* B, con
                               hipStream_t s) {
   const uint8_t* a = static_cast<const uint8_t*>(A);
   const uint8_t* b = static_cast<const uint8_t*>(B);
-  const bool wide = N >= 32 * 256;
-  const bool small = ceil_div(M, 64) * ceil_div(N, 64) <= 256;
-  const bool large = !f32 && ceil_div(M, 256) * ceil_div(N, 256) >= 192;
-#define MHL_GEMM(F32, ROWS)                                                     \
-  do {                                                                          \
-    if (M <= 16)                                                                \
-      launch_few<1, 1, 4, F32, ROWS>(a, sa, b, sb, M, N, K, C, s);              \
-    else if (M <= 32 && wide)                                                   \
-      launch_few<2, 2, 2, F32, ROWS>(a, sa, b, sb, M, N, K, C, s);              \
-    else if (M <= 32)                                                           \
-      launch_few<2, 1, 4, F32, ROWS>(a, sa, b, sb, M, N, K, C, s);              \
-    else if (small)                                                             \
-      launch_tile<2, 1, 2, 4, 4, F32, ROWS>(a, sa, b, sb, M, N, K, C, s);       \
-    else if (large && !F32)                                                     \
-      launch_tile<4, 2, 4, 8, 1, false, ROWS>(a, sa, b, sb, M, N, K, C, s);     \
-    else                                                                        \
-      launch_tile<2, 2, 4, 4, 2, F32, ROWS>(a, sa, b, sb, M, N, K, C, s);       \
-  } while (0)
+  const GemmForm form = gemm_scaled_form(M, N, f32);
+#define MHL_GEMM(F32, ROWS)                                                               \
+  switch (form) {                                                                         \
+    case GemmForm::kFew16: launch_few<1, 1, 4, F32, ROWS>(a, sa, b, sb, M, N, K, C, s); break; \
+    case GemmForm::kFew32: launch_few<2, 1, 4, F32, ROWS>(a, sa, b, sb, M, N, K, C, s); break; \
+    case GemmForm::kFew32Wide:                                                            \
+      launch_few<2, 2, 2, F32, ROWS>(a, sa, b, sb, M, N, K, C, s);                        \
+      break;                                                                              \
+    case GemmForm::k64:                                                                   \
+      launch_tile<2, 1, 2, 4, 4, F32, ROWS>(a, sa, b, sb, M, N, K, C, s);                 \
+      break;                                                                              \
+    case GemmForm::k128Split:                                                             \
+      launch_tile<2, 2, 4, 4, 2, F32, ROWS>(a, sa, b, sb, M, N, K, C, s);                 \
+      break;                                                                              \
+    case GemmForm::k128:                                                                  \
+      launch_tile<2, 2, 4, 4, 1, F32, ROWS>(a, sa, b, sb, M, N, K, C, s);                 \
+      break;                                                                              \
+    case GemmForm::k256:                                                                  \
+      if (!F32) launch_tile<4, 2, 4, 8, 1, false, ROWS>(a, sa, b, sb, M, N, K, C, s);     \
+      break;                                                                              \
+  }
   if (f32 && b_rows)
-    MHL_GEMM(true, true);
+    MHL_GEMM(true, true)
   else if (f32)
-    MHL_GEMM(true, false);
+    MHL_GEMM(true, false)
   else if (b_rows)
-    MHL_GEMM(false, true);
+    MHL_GEMM(false, true)
   else
-    MHL_GEMM(false, false);
+    MHL_GEMM(false, false)
 #undef MHL_GEMM
   return hipGetLastError();
 }

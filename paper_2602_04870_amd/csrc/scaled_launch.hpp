@@ -10,12 +10,13 @@ namespace mhl {
 
 // How a row of d columns is held by the norm kernels.  Multiples of 8 by pieces
 // of 8 columns: in the registers of 16 or 32 lanes (up to 128 or 256 columns),
-// of a wavefront (up to 4096, 1 to 8 pieces per lane; no barrier, four rows per
-// workgroup) or of a workgroup (up to 16384).  Other widths column by column: 16
+// of a wavefront (up to 2048, 1 to 4 pieces per lane; no barrier, four rows per
+// workgroup) or of a workgroup (up to 16384; at 16384 rows of 4096 with 8 bits
+// out 46 us, 64 in a wavefront's registers).  Other widths column by column: 16
 // lanes (up to 64 columns), a wavefront (512), a workgroup (4096).  Wider rows
 // are not held at all.
 enum class NormForm {
-  kPart16, kPart32, kWave1, kWave2, kWave4, kWave8, kGroup4, kGroup8,
+  kPart16, kPart32, kWave1, kWave2, kWave4, kGroup2, kGroup4, kGroup8,
   kOdd16, kOddWave, kOddGroup, kWide8, kWide1
 };
 inline NormForm norm_form(int d) {
@@ -29,7 +30,7 @@ inline NormForm norm_form(int d) {
          : d <= 512   ? NormForm::kWave1
          : d <= 1024  ? NormForm::kWave2
          : d <= 2048  ? NormForm::kWave4
-         : d <= 4096  ? NormForm::kWave8
+         : d <= 4096  ? NormForm::kGroup2
          : d <= 8192  ? NormForm::kGroup4
          : d <= 16384 ? NormForm::kGroup8
                       : NormForm::kWide8;
@@ -38,8 +39,10 @@ inline NormForm norm_form(int d) {
 inline int norm_rows(NormForm f) {
   return f == NormForm::kPart16 || f == NormForm::kOdd16 ? 16
          : f == NormForm::kPart32                        ? 8
-         : f == NormForm::kGroup4 || f == NormForm::kGroup8 || f == NormForm::kOddGroup ? 1
-                                                                                        : 4;
+         : f == NormForm::kGroup2 || f == NormForm::kGroup4 || f == NormForm::kGroup8 ||
+                 f == NormForm::kOddGroup
+             ? 1
+             : 4;
 }
 
 // h = round(x + residual) to sum (residual NULL: h = x, sum not written), the
@@ -60,8 +63,11 @@ inline int64_t rmsnorm_bwd_parts(int64_t T, int d) {
     const int64_t most = (int64_t(1) << 19) / d > 16 ? (int64_t(1) << 19) / d : 16;
     return ceil_div(T, 8) < most ? ceil_div(T, 8) : most;
   }
-  const int64_t n = ceil_div(T, norm_rows(norm_form(d)));  // workgroups, two per CU at most
-  return n < 512 ? n : 512;
+  // one per workgroup: two workgroups per CU, four where their rows are short and
+  // many (us with 256, 512, 1024, 2048: 74, 63, 64, 67 at 16384 x 2048, 49, 36, 33, 36
+  // at 16384 x 1024, 14, 13, 13, 15 at 4096 x 1024)
+  const int64_t n = ceil_div(T, norm_rows(norm_form(d))), most = d <= 1024 && T >= 16384 ? 1024 : 512;
+  return n < most ? n : most;
 }
 hipError_t launch_rmsnorm_bwd(const void* h, const float* w, const void* dy, const void* dsum,
                               int64_t T, int d, float eps, bool f32, void* dx, float* part,
@@ -73,6 +79,39 @@ hipError_t launch_rmsnorm_dw(const float* part, int64_t n, int d, float* dw, hip
 // to 16]).
 hipError_t launch_quantize(const void* x, int64_t rows, int64_t cols, bool f32, int block_rows,
                            bool transpose, void* q, float* scales, hipStream_t s);
+
+// How the 8-bit product is cut up.  Few rows of A: B straight into registers, 16
+// or 32 of its rows per workgroup.  Else tiles of C: 64 x 64 with the blocks
+// along K over four groups of wavefronts (kept while they do not outnumber the
+// CUs), 128 x 128 over two groups, 128 x 128 with two workgroups per CU, or 256 x
+// 256 (bf16 results; fp32 ones need the registers for widened pieces).  us at
+// K = 1024 (2048 at N = 2048, 2048 at 3584, 8192 at 8192), bf16:
+//      M     N     64   128 split   128    256
+//    128  1024    5.8      8.8              28
+//   1024  1024    6.2      9.2              20
+//   2048  1024   10.8      9.7              20
+//   4096  1024   21       10.5     10.5     21
+//   8192  1024   40       18.8     15.5     22
+//   2048  2048   28       14.6     16.6     31
+//   4096  2048   55       26.6     23.0     32
+//   3584  3584            50       41.7     35
+//   8192  8192           766      602      456
+// A round of 256 x 256 tiles (one per CU) takes about 9 / 5 of one of 128 x 128
+// tiles (two per CU); whichever's rounds take less is chosen.  Rows of A, at N =
+// K = 8192: 12 us at 1, 20 at 16, 24 at 32 (32 with 16 rows of B per workgroup),
+// the 64 x 64 tiles 23 from 33 to 64 (33 us in registers).
+enum class GemmForm { kFew16, kFew32, kFew32Wide, k64, k128Split, k128, k256 };
+inline GemmForm gemm_scaled_form(int64_t M, int64_t N, bool f32) {
+  // (the former's workgroups of 512 threads must fit a grid of 2^32)
+  if (M <= 16 && N < (1 << 26)) return GemmForm::kFew16;
+  if (M <= 32 && N < (1 << 26)) return N >= 32 * 256 ? GemmForm::kFew32Wide : GemmForm::kFew32;
+  if (ceil_div(M, 64) * ceil_div(N, 64) <= 256) return GemmForm::k64;
+  const int64_t tiles = ceil_div(M, 128) * ceil_div(N, 128);
+  if (tiles <= 256) return GemmForm::k128Split;
+  const int64_t rounds = ceil_div(tiles, 512);
+  const int64_t rounds256 = ceil_div(ceil_div(M, 256) * ceil_div(N, 256), 256);
+  return !f32 && 9 * rounds256 <= 5 * rounds ? GemmForm::k256 : GemmForm::k128;
+}
 
 // C[M][N] (bf16, fp32 when f32) of 8-bit A[M][K] and B[N][K] (K a multiple of
 // 16) with scales sa[M][ceil(K / 128)] and sb[N or ceil(N / 128)][ceil(K / 128)]

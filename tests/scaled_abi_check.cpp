@@ -7,6 +7,7 @@
 #include <cstdio>
 
 #include "mhlmoe.h"
+#include "scaled_launch.hpp"
 
 namespace {
 int g_fail = 0;
@@ -51,6 +52,38 @@ int main() {
          MHLMOE_EINVAL);
   expect("gemm dtype", mhlmoe_gemm_scaled(A, F, A, F, 1, 64, 64, 128, (mhlmoe_dtype)77, A, nullptr),
          MHLMOE_EINVAL);
+  // every product that the ABI takes is a launch of fewer than 2^32 threads
+  const int64_t sizes[] = {1, 16, 17, 32, 33, 64, 65, 1000, 4096, 65536, 1 << 20, 1 << 24, 1 << 26,
+                           (1 << 26) + 1, 1 << 27, (int64_t(1) << 31) - 1};
+  for (int64_t M : sizes)
+    for (int64_t N : sizes) {
+      if (mhl::ceil_div(M, 128) >= (int64_t(1) << 24) / mhl::ceil_div(N, 128)) continue;
+      for (int f32 = 0; f32 < 2; ++f32) {
+        const mhl::GemmForm f = mhl::gemm_scaled_form(M, N, f32 != 0);
+        int64_t groups = 0, threads = 0;
+        switch (f) {
+          case mhl::GemmForm::kFew16:
+          case mhl::GemmForm::kFew32: groups = mhl::ceil_div(N, 16), threads = 512; break;
+          case mhl::GemmForm::kFew32Wide: groups = mhl::ceil_div(N, 32), threads = 512; break;
+          case mhl::GemmForm::k64:
+            groups = mhl::ceil_div(M, 64) * mhl::ceil_div(N, 64), threads = 512;
+            break;
+          case mhl::GemmForm::k128Split:
+            groups = mhl::ceil_div(M, 128) * mhl::ceil_div(N, 128), threads = 512;
+            break;
+          case mhl::GemmForm::k128:
+            groups = mhl::ceil_div(M, 128) * mhl::ceil_div(N, 128), threads = 256;
+            break;
+          case mhl::GemmForm::k256:
+            groups = mhl::ceil_div(M, 256) * mhl::ceil_div(N, 256), threads = 512;
+            break;
+        }
+        if (groups < 1 || groups * threads >= (int64_t(1) << 32) || (f32 && f == mhl::GemmForm::k256)) {
+          std::printf("FAIL form %lld %lld %d\n", (long long)M, (long long)N, f32);
+          ++g_fail;
+        }
+      }
+    }
   std::printf("done %d failures\n", g_fail);
   return g_fail == 0 ? 0 : 1;
 }

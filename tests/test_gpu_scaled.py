@@ -237,10 +237,10 @@ GEMM_SHAPES = [(1, 1, 16), (1, 7, 128), (2, 128, 400), (3, 1000, 144), (15, 16, 
                (64, 512, 384), (65, 127, 272), (100, 300, 512), (127, 129, 128), (128, 128, 1024),
                (129, 384, 160), (255, 257, 256), (256, 256, 128), (300, 520, 896), (513, 640, 1152),
                (1100, 1300, 336),
-               # B of 8192 rows and more under few rows of A; over 256 tiles of 64 x 64; 192 tiles of
-               # 256 x 256 and more, whole and not
+               # B of 8192 rows and more under few rows of A; over 256 tiles of 64 x 64, of 128 x 128;
+               # enough for tiles of 256 x 256, whole and not
                (20, 8209, 272), (32, 8192, 1152), (1030, 1100, 144), (1152, 1152, 1152),
-               (3600, 3401, 272), (4096, 3328, 640)]
+               (2310, 2050, 272), (2304, 2048, 896), (3600, 3401, 272), (4096, 3328, 640)]
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
@@ -263,7 +263,7 @@ def test_gemm(M, N, K, block, dtype):
 
 @pytest.mark.parametrize("M,N,K", [(1, 40, 272), (37, 100, 144), (64, 256, 2048), (130, 270, 400),
                                    (300, 260, 640), (1000, 1024, 512), (31, 8200, 400),
-                                   (1100, 1200, 912), (3500, 3600, 400)])
+                                   (1100, 1200, 912), (2400, 2100, 528), (3500, 3600, 400)])
 @pytest.mark.parametrize("block", [128, 1])
 def test_gemm_exact(M, N, K, block):
     """Small whole numbers under powers of two as scales: every sum is exact in
@@ -319,6 +319,46 @@ def test_gemm_special_values_stay_in_their_row(M):
     rows = [i for i in range(M) if i not in (1, 3)]
     assert torch.equal(C[rows], clean[rows])
     assert torch.isnan(C[1]).all() and not torch.isfinite(C[3]).any()
+
+
+def test_gemm_far_offsets():
+    """A of more than 2^32 bytes, K at its largest: what lies in the last rows
+    and the last blocks arrives, against the product of those blocks alone."""
+    M, N, K, used = 520, 130, (1 << 23) - 128, 272
+    g = _gen(6)
+    A = torch.zeros((M, K), dtype=torch.uint8, device="cuda").view(ref.E4M3)
+    B = torch.zeros((N, K), dtype=torch.uint8, device="cuda").view(ref.E4M3)
+    a, _ = mh.mhlmoe_quantize(_randn(g, M, used))
+    b, _ = mh.mhlmoe_quantize(_randn(g, N, used))
+    at = K - used - 112 - used % 128  # a block's start, and a block behind the last one used
+    at -= at % 128
+    A.view(torch.uint8)[:, at:at + used] = a.view(torch.uint8)
+    B.view(torch.uint8)[:, at:at + used] = b.view(torch.uint8)
+    KB, kb = K // 128, at // 128
+    sa, sb = torch.ones((M, KB), device="cuda"), torch.ones((2, KB), device="cuda")
+    sa[:, kb:] = torch.rand((M, KB - kb), generator=g, device="cuda")
+    sb[:, kb:] = torch.rand((2, KB - kb), generator=g, device="cuda")
+    C = mh.mhlmoe_gemm_scaled(A, sa, B, sb, dtype=F32)
+    n = -(-used // 128)
+    want, mag = ref.gemm64(ref.host(a), ref.host(sa[:, kb:kb + n]), ref.host(b),
+                           ref.host(sb[:, kb:kb + n]), 128)
+    assert np.all(np.abs(ref.host(C) - want) <= ref.gemm_bound(want, mag, used, F32))
+
+
+def test_gemm_many_columns():
+    """So many rows of B that a workgroup for every 16 would pass 2^32 threads."""
+    N, K = (1 << 26) + 37, 16
+    g = _gen(4)
+    A, sa = mh.mhlmoe_quantize(_randn(g, 3, K))
+    B = torch.randint(0, 120, (N, K), generator=g, device="cuda", dtype=torch.uint8).view(ref.E4M3)
+    sb = torch.rand((-(-N // 128), 1), generator=g, device="cuda")
+    C = mh.mhlmoe_gemm_scaled(A, sa, B, sb)
+    for at in (0, 1 << 25, N - 100 - N % 128):
+        rows = slice(at, min(at + 200, N))
+        tiles = sb[at // 128:at // 128 + 3]
+        want, mag = ref.gemm64(ref.host(A), ref.host(sa), ref.host(B[rows]),
+                               np.repeat(ref.host(tiles), 128, 0)[at % 128:][:B[rows].shape[0]], 1)
+        assert np.all(np.abs(ref.host(C[:, rows]) - want) <= ref.gemm_bound(want, mag, K, BF16))
 
 
 def test_gradient_products():
