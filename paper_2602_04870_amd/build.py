@@ -40,8 +40,8 @@ SOURCES = ["api.cpp", "api_scaled.cpp", "route.hip", "route_64_bf16.hip", "route
            "route_128_bf16.hip", "route_128_f32.hip", "bucket.hip", "experts.hip", "ffn_ws.hip",
            "backward.hip", "projection.cpp", "static_scratch.hip", "norm.hip", "quantize.hip",
            "gemm_scaled.hip"]
-HEADERS = ["api_internal.hpp", "device_common.hpp", "ffn_common.hpp", "launch.hpp", "route_kernel.hpp", "scaled_common.hpp",
-           "scaled_launch.hpp", "sort_networks.hpp"]
+HEADERS = ["api_internal.hpp", "device_common.hpp", "ffn_common.hpp", "launch.hpp",
+           "route_kernel.hpp", "scaled_common.hpp", "scaled_launch.hpp", "sort_networks.hpp"]
 
 
 def _compile(src: str) -> str:

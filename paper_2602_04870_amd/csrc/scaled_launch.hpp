@@ -87,19 +87,19 @@ hipError_t launch_quantize(const void* x, int64_t rows, int64_t cols, bool f32, 
 // 256 (bf16 results; fp32 ones need the registers for widened pieces).  us at
 // K = 1024 (2048 at N = 2048, 2048 at 3584, 8192 at 8192), bf16:
 //      M     N     64   128 split   128    256
-//    128  1024    5.8      8.8              28
-//   1024  1024    6.2      9.2              20
-//   2048  1024   10.8      9.7              20
-//   4096  1024   21       10.5     10.5     21
-//   8192  1024   40       18.8     15.5     22
-//   2048  2048   28       14.6     16.6     31
-//   4096  2048   55       26.6     23.0     32
-//   3584  3584            50       41.7     35
-//   8192  8192           766      602      456
+//    128  1024    5.6      7.7      8.0   14.3
+//   1024  1024    6.0      8.2      8.4   14.8
+//   2048  1024   10.4      8.7      8.8   15.4
+//   4096  1024   20.5     10.0     10.0   16.4
+//   8192  1024   38       18.4     14.6   18.2
+//   2048  2048   28       14.6     15.7   25.7
+//   4096  2048   53       27       22     28
+//   3584  3584   83       50       37     30
+//   8192  8192 1412      754      600    458
 // A round of 256 x 256 tiles (one per CU) takes about 9 / 5 of one of 128 x 128
 // tiles (two per CU); whichever's rounds take less is chosen.  Rows of A, at N =
 // K = 8192: 12 us at 1, 20 at 16, 24 at 32 (32 with 16 rows of B per workgroup),
-// the 64 x 64 tiles 23 from 33 to 64 (33 us in registers).
+// the 64 x 64 tiles 22.5 at 64 (33 with A in registers).
 enum class GemmForm { kFew16, kFew32, kFew32Wide, k64, k128Split, k128, k256 };
 inline GemmForm gemm_scaled_form(int64_t M, int64_t N, bool f32) {
   // (the former's workgroups of 512 threads must fit a grid of 2^32)

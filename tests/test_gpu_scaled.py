@@ -461,6 +461,14 @@ def test_latent_layer_scaled(case):
     assert np.all(off <= ref.gemm_bound(C, mag, dm, dtype))
 
 
+def test_latent_layer_scaled_empty_batch():
+    p = _layer_inputs(0, 208, 3, 64, 16, 64, BF16, True, False)
+    counts = torch.full((3, 16), 7, dtype=torch.int32, device="cuda")
+    got = _call_layer(p, 3, 2, counts=counts)
+    torch.cuda.synchronize()
+    assert got["out"].shape == (0, 208) and torch.all(counts == 0)
+
+
 def test_side_stream_and_graph():
     """The layer and the norm's gradient on a side stream, and captured into
     one graph that is replayed with new inputs and eager work between."""

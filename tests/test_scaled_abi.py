@@ -139,6 +139,16 @@ def test_names_of_the_product_are_declared():
         assert f'"{name}"' in header, name
 
 
+def test_product_kernels_issue_no_tracked_dma():
+    """The product's LDS DMA writes m0 without the compiler's knowledge, so its
+    kernels issue no DMA that the compiler tracks."""
+    text = open(os.path.join(CSRC, "gemm_scaled.hip")).read()
+    assert text.count("offen lds") == 2
+    assert "load_lds" not in text and "dma_lds16(" not in re.sub(r"//[^\n]*", "", text)
+    # and nothing is in flight when the tiles' LDS is used for the results
+    assert text.index("barrier_vm<0>();  // the last blocks' DMA") < text.index("turn = smem")
+
+
 SAN = ["-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=all"]
 
 
