@@ -20,7 +20,9 @@ namespace mhl {
 namespace {
 
 constexpr int kNormThreads = 256;
-constexpr int kNormWaves = kNormThreads / kWave;
+// threads of a workgroup with LANES lanes per row
+constexpr int norm_threads(int lanes) { return lanes > kNormThreads ? lanes : kNormThreads; }
+constexpr int kNormWaves = 512 / kWave;  // most of a workgroup
 constexpr unsigned kNormMaxGrid = 1u << 20;  // workgroups; rows beyond them are looped over
 
 // Sum over the lanes of a row: part of a wavefront, or the workgroup (whose
@@ -41,13 +43,12 @@ __device__ __forceinline__ float row_sum(float v, float* lds) {
 // Writes a lane's columns of y: in the type, and/or (VEC 8) in 8 bits with the
 // scale of the 16 lanes' 128 columns.  All 16 lanes take part.
 template <bool F32, int VEC>
-__device__ __forceinline__ void write_y(const float (&y)[VEC], bool ok, int64_t row, int col, int d,
-                                        void* out, uint8_t* q, float* scales) {
-  const int64_t at = row * d + col;
+__device__ __forceinline__ void write_y(const float (&y)[VEC], bool ok, int64_t row, uint32_t col,
+                                        int d, void* out, uint8_t* q, float* scales) {
   if (out && ok) {
     Piece<F32, VEC> p;
     p.set(y);
-    p.store(out, at);
+    p.store(from<F32>(out, row * d), col);
   }
   if constexpr (VEC == 8) {
     if (!q) return;
@@ -57,13 +58,13 @@ __device__ __forceinline__ void write_y(const float (&y)[VEC], bool ok, int64_t 
       const uint32_t b = magnitude(y[i]);
       m = b > m ? b : m;
     }
-    const float s = block_scale(max16(ok ? m : 0u));
-    const float inv = 1.0f / s;
+    float inv;
+    const float s = block_scale(max16(ok ? m : 0u), inv);
     float z[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) z[i] = over_scale(y[i], s, inv);
     if (ok) {
-      *reinterpret_cast<u32x2*>(q + at) =
+      *reinterpret_cast<u32x2*>(q + row * d + col) =
           u32x2{pack_e4m3(z[0], z[1], z[2], z[3]), pack_e4m3(z[4], z[5], z[6], z[7])};
       if ((threadIdx.x & 15) == 0)
         scales[row * ceil_div(d, kScaleBlock) + col / kScaleBlock] = s;
@@ -71,8 +72,18 @@ __device__ __forceinline__ void write_y(const float (&y)[VEC], bool ok, int64_t 
   }
 }
 
+// A thread's first row; one number per wavefront where the wavefront has one
+// row, so that its addresses are a scalar base and a lane's 32-bit offset.
+template <int LANES>
+__device__ __forceinline__ int64_t first_row() {
+  constexpr int kRows = norm_threads(LANES) / LANES;
+  const int r = threadIdx.x / LANES;
+  return (int64_t)blockIdx.x * kRows + (LANES >= kWave ? __builtin_amdgcn_readfirstlane(r) : r);
+}
+
 template <int VEC>
-__device__ __forceinline__ void load_weight(const float* w, int col, bool ok, float (&f)[VEC]) {
+__device__ __forceinline__ void load_weight(const float* w, uint32_t col, bool ok,
+                                            float (&f)[VEC]) {
   Piece<true, VEC> p;
   p.load(w, col, ok);
   p.get(f);
@@ -82,31 +93,32 @@ __device__ __forceinline__ void load_weight(const float* w, int col, bool ok, fl
 // at most LANES * NV * VEC.  residual == NULL: h is x, and sum is not written.
 // sum may be x or residual, y may be x: a lane stores only what it has read.
 template <bool F32, int VEC, int LANES, int NV>
-__global__ __launch_bounds__(kNormThreads) void rmsnorm_kernel(
+__global__ __launch_bounds__(norm_threads(LANES)) void rmsnorm_kernel(
     const void* x, const void* residual, const float* __restrict__ w, int64_t T, int d, float eps,
     void* sum, void* y, uint8_t* q, float* scales) {
   __shared__ float lds[kNormWaves];
-  constexpr int kRows = kNormThreads / LANES;
+  constexpr int kRows = norm_threads(LANES) / LANES;
   const int l = threadIdx.x % LANES;
-  for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES; row < T;
-       row += (int64_t)gridDim.x * kRows) {
+  for (int64_t row = first_row<LANES>(); row < T; row += (int64_t)gridDim.x * kRows) {
+    const void *x_row = from<F32>(x, row * d), *r_row = from<F32>(residual, row * d);
+    void* const sum_row = from<F32>(sum, row * d);
     Piece<F32, VEC> hr[NV], rr[NV];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int col = (v * LANES + l) * VEC;
-      hr[v].load(x, row * d + col, col < d);
+      const uint32_t col = (v * LANES + l) * VEC;
+      hr[v].load(x_row, col, col < (uint32_t)d);
     }
     if (residual) {
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
-        const int col = (v * LANES + l) * VEC;
-        rr[v].load(residual, row * d + col, col < d);
+        const uint32_t col = (v * LANES + l) * VEC;
+        rr[v].load(r_row, col, col < (uint32_t)d);
       }
     }
     float ss = 0.0f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int col = (v * LANES + l) * VEC;
+      const uint32_t col = (v * LANES + l) * VEC;
       float h[VEC];
       hr[v].get(h);
       if (residual) {
@@ -115,7 +127,7 @@ __global__ __launch_bounds__(kNormThreads) void rmsnorm_kernel(
 #pragma unroll
         for (int i = 0; i < VEC; ++i) h[i] += r[i];
         hr[v].set(h);
-        if (col < d) hr[v].store(sum, row * d + col);
+        if (col < (uint32_t)d) hr[v].store(sum_row, col);
         hr[v].get(h);
       }
 #pragma unroll
@@ -124,13 +136,13 @@ __global__ __launch_bounds__(kNormThreads) void rmsnorm_kernel(
     const float rs = 1.0f / sqrtf(row_sum<LANES>(ss, lds) / (float)d + eps);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int col = (v * LANES + l) * VEC;
+      const uint32_t col = (v * LANES + l) * VEC;
       float h[VEC], wf[VEC];
       hr[v].get(h);
-      load_weight<VEC>(w, col, col < d, wf);
+      load_weight<VEC>(w, col, col < (uint32_t)d, wf);
 #pragma unroll
       for (int i = 0; i < VEC; ++i) h[i] = h[i] * rs * wf[i];
-      write_y<F32, VEC>(h, col < d, row, col, d, y, q, scales);
+      write_y<F32, VEC>(h, col < (uint32_t)d, row, col, d, y, q, scales);
     }
   }
 }
@@ -185,13 +197,21 @@ __global__ __launch_bounds__(kNormThreads) void rmsnorm_wide_kernel(
 // registers and leaves their sum in part[blockIdx.x][d], its rows' lanes added
 // in order.  dx may be dy or dsum.
 template <bool F32, int VEC, int LANES, int NV>
-__global__ __launch_bounds__(kNormThreads) void rmsnorm_bwd_kernel(
+__global__ __launch_bounds__(norm_threads(LANES)) void rmsnorm_bwd_kernel(
     const void* h_src, const float* __restrict__ w, const void* dy, const void* dsum, int64_t T,
     int d, float eps, void* dx, float* __restrict__ part) {
-  constexpr int kRows = kNormThreads / LANES;
+  constexpr int kRows = norm_threads(LANES) / LANES;
   __shared__ float lds[2 * kNormWaves];
   __shared__ float add[kRows > 1 ? kNormThreads * VEC : 1];
   const int l = threadIdx.x % LANES;
+  // the weights stay in registers, too (62.2 -> 55.8 us at 16384 x 2048: loaded anew
+  // for every row they were most of the L1's traffic)
+  float wf[NV][VEC];
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    const uint32_t col = (v * LANES + l) * VEC;
+    load_weight<VEC>(w, col, col < (uint32_t)d, wf[v]);
+  }
   float dw[NV][VEC];
 #pragma unroll
   for (int v = 0; v < NV; ++v)
@@ -199,34 +219,34 @@ __global__ __launch_bounds__(kNormThreads) void rmsnorm_bwd_kernel(
     for (int i = 0; i < VEC; ++i) dw[v][i] = 0.0f;
   // (fetching the next row ahead of this one's work took registers and time: 62.5
   // -> 64.1 us at 16384 x 2048, 58.4 -> 66.7 at 8192 x 2048 in fp32)
-  for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES; row < T;
-       row += (int64_t)gridDim.x * kRows) {
+  for (int64_t row = first_row<LANES>(); row < T; row += (int64_t)gridDim.x * kRows) {
+    const void *h_row = from<F32>(h_src, row * d), *dy_row = from<F32>(dy, row * d);
+    const void* const dsum_row = from<F32>(dsum, row * d);
+    void* const dx_row = from<F32>(dx, row * d);
     Piece<F32, VEC> hr[NV], gr[NV], sr[NV];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int col = (v * LANES + l) * VEC;
-      hr[v].load(h_src, row * d + col, col < d);
-      gr[v].load(dy, row * d + col, col < d);
+      const uint32_t col = (v * LANES + l) * VEC;
+      hr[v].load(h_row, col, col < (uint32_t)d);
+      gr[v].load(dy_row, col, col < (uint32_t)d);
     }
     if (dsum) {
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
-        const int col = (v * LANES + l) * VEC;
-        sr[v].load(dsum, row * d + col, col < d);
+        const uint32_t col = (v * LANES + l) * VEC;
+        sr[v].load(dsum_row, col, col < (uint32_t)d);
       }
     }
     float ss = 0.0f, gh = 0.0f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int col = (v * LANES + l) * VEC;
-      float h[VEC], g[VEC], wf[VEC];
+      float h[VEC], g[VEC];
       hr[v].get(h);
       gr[v].get(g);
-      load_weight<VEC>(w, col, col < d, wf);
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
         ss = fmaf(h[i], h[i], ss);
-        gh = fmaf(g[i] * wf[i], h[i], gh);
+        gh = fmaf(g[i] * wf[v][i], h[i], gh);
       }
     }
     ss = row_sum<LANES>(ss, lds);
@@ -235,25 +255,24 @@ __global__ __launch_bounds__(kNormThreads) void rmsnorm_bwd_kernel(
     const float k = gh / (float)d * rs * rs;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int col = (v * LANES + l) * VEC;
-      float h[VEC], g[VEC], wf[VEC], s[VEC];
+      const uint32_t col = (v * LANES + l) * VEC;
+      float h[VEC], g[VEC], s[VEC];
       hr[v].get(h);
       gr[v].get(g);
-      load_weight<VEC>(w, col, col < d, wf);
       if (dsum) sr[v].get(s);
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
         dw[v][i] = fmaf(g[i], h[i] * rs, dw[v][i]);
-        const float t = rs * fmaf(-h[i], k, g[i] * wf[i]);
+        const float t = rs * fmaf(-h[i], k, g[i] * wf[v][i]);
         h[i] = dsum ? s[i] + t : t;
       }
       hr[v].set(h);
-      if (col < d) hr[v].store(dx, row * d + col);
+      if (col < (uint32_t)d) hr[v].store(dx_row, col);
     }
   }
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
-    const int col = (v * LANES + l) * VEC;
+    const uint32_t col = (v * LANES + l) * VEC;
     if (kRows > 1) {
       __syncthreads();
 #pragma unroll
@@ -269,7 +288,7 @@ __global__ __launch_bounds__(kNormThreads) void rmsnorm_bwd_kernel(
         }
       }
     }
-    if (threadIdx.x < LANES && col < d) {
+    if (threadIdx.x < LANES && col < (uint32_t)d) {
       Piece<true, VEC> p;
       p.set(dw[v]);
       p.store(part, (int64_t)blockIdx.x * d + col);
@@ -359,7 +378,7 @@ unsigned norm_grid(int64_t rows, int per_wg, unsigned most) {
   case NormForm::kWave4: KERNEL(F32, 8, 64, 4); break;     \
   case NormForm::kGroup2: KERNEL(F32, 8, 256, 2); break;   \
   case NormForm::kGroup4: KERNEL(F32, 8, 256, 4); break;   \
-  case NormForm::kGroup8: KERNEL(F32, 8, 256, 8); break;   \
+  case NormForm::kLarge4: KERNEL(F32, 8, 512, 4); break;   \
   case NormForm::kOdd16: KERNEL(F32, 1, 16, 4); break;     \
   case NormForm::kOddWave: KERNEL(F32, 1, 64, 8); break;   \
   case NormForm::kOddGroup: KERNEL(F32, 1, 256, 16); break;
@@ -370,8 +389,8 @@ hipError_t launch_rmsnorm(const void* x, const void* residual, const float* w, i
   uint8_t* q8 = static_cast<uint8_t*>(q);
 #define MHL_NORM(F32, VEC, LANES, NV)                                                              \
   hipLaunchKernelGGL((rmsnorm_kernel<F32, VEC, LANES, NV>),                                        \
-                     dim3(norm_grid(T, kNormThreads / LANES, kNormMaxGrid)), dim3(kNormThreads), 0, \
-                     s, x, residual, w, T, d, eps, sum, y, q8, scales)
+                     dim3(norm_grid(T, norm_threads(LANES) / LANES, kNormMaxGrid)),                \
+                     dim3(norm_threads(LANES)), 0, s, x, residual, w, T, d, eps, sum, y, q8, scales)
 #define MHL_NORM_WIDE(F32, VEC)                                                                   \
   hipLaunchKernelGGL((rmsnorm_wide_kernel<F32, VEC>), dim3(norm_grid(T, 1, kNormMaxGrid)),        \
                      dim3(kNormThreads), 0, s, x, residual, w, T, d, eps, sum, y, q8, scales)
@@ -396,8 +415,8 @@ hipError_t launch_rmsnorm_bwd(const void* h, const float* w, const void* dy, con
                               float* rows, hipStream_t s) {
   const unsigned n = (unsigned)rmsnorm_bwd_parts(T, d);
 #define MHL_NORM(F32, VEC, LANES, NV)                                                              \
-  hipLaunchKernelGGL((rmsnorm_bwd_kernel<F32, VEC, LANES, NV>), dim3(n), dim3(kNormThreads), 0, s, \
-                     h, w, dy, dsum, T, d, eps, dx, part)
+  hipLaunchKernelGGL((rmsnorm_bwd_kernel<F32, VEC, LANES, NV>), dim3(n),                           \
+                     dim3(norm_threads(LANES)), 0, s, h, w, dy, dsum, T, d, eps, dx, part)
 #define MHL_NORM_TYPE(F32)                                                                       \
   switch (norm_form(d)) {                                                                        \
     MHL_NORM_FORMS(F32, MHL_NORM)                                                                \

@@ -52,8 +52,8 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_rows_kernel(
         const uint32_t b = magnitude(f[e]);
         m = b > m ? b : m;
       }
-      const float s = block_scale(max16(m));
-      const float inv = 1.0f / s;
+      float inv;
+      const float s = block_scale(max16(m), inv);
 #pragma unroll
       for (int e = 0; e < 8; ++e) f[e] = over_scale(f[e], s, inv);
       if (ok[u])
@@ -114,8 +114,7 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_tile_kernel(
     m = 0;
 #pragma unroll
     for (int w = 0; w < 4; ++w) m = amax[w] > m ? amax[w] : m;
-    s[0] = block_scale(m);
-    inv[0] = 1.0f / s[0];
+    s[0] = block_scale(m, inv[0]);
     if (tid == 0) scales[TRANSPOSE ? tc * tiles_r + tr : tr * tiles_c + tc] = s[0];
   } else {
     uint32_t m[8];
@@ -152,8 +151,7 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_tile_kernel(
         const uint32_t o = amax[w * kScaleBlock + cg * 8 + e];
         v = o > v ? o : v;
       }
-      s[e] = block_scale(v);
-      inv[e] = 1.0f / s[e];
+      s[e] = block_scale(v, inv[e]);
     }
     if (rg == 0 && c0 < cols) {
 #pragma unroll

@@ -17,6 +17,16 @@ struct Raw8 {
   u32x4 v[F32 ? 2 : 1];
 };
 
+// Element at of p.
+template <bool F32>
+__device__ __forceinline__ const void* from(const void* p, int64_t at) {
+  return static_cast<const uint8_t*>(p) + at * (F32 ? 4 : 2);
+}
+template <bool F32>
+__device__ __forceinline__ void* from(void* p, int64_t at) {
+  return static_cast<uint8_t*>(p) + at * (F32 ? 4 : 2);
+}
+
 template <bool F32>
 __device__ __forceinline__ const u32x4* row_ptr(const void* p, int64_t at) {
   return reinterpret_cast<const u32x4*>(reinterpret_cast<const uint8_t*>(p) + at * (F32 ? 4 : 2));
@@ -137,20 +147,27 @@ __device__ __forceinline__ float lane_sum(float v) {
   return v;
 }
 
-// A block's scale from its largest magnitude.
-__device__ __forceinline__ float block_scale(uint32_t amax) {
-  const float s = __uint_as_float(amax) / kE4m3Max;
-  return s < kScaleMin ? kScaleMin : s;  // a NaN or infinity stays one
+// a / b by one multiply with (about) 1 / b and a correction: r + (a - r b) / b.
+__device__ __forceinline__ float quotient(float a, float b, float inv) {
+  const float r = a * inv;
+  return fmaf(fmaf(-r, b, a), inv, r);
 }
 
-// v / s by one multiply and a correction (r + (v - r s) / s: within an ulp of
-// the quotient, where the bare multiply moved values that lie on a border
-// between two of e4m3's, as bf16 inputs often do).  At most 448 (1 + 2^-23),
-// which e4m3 rounds to 448, so nothing has to be clamped.  A block whose scale
-// is not finite becomes NaN as a whole.
+// A block's scale from its largest magnitude (NaN from an infinity or a NaN),
+// and the scale's reciprocal to an ulp.
+__device__ __forceinline__ float block_scale(uint32_t amax, float& inv) {
+  const float q = quotient(__uint_as_float(amax), kE4m3Max, 1.0f / kE4m3Max);
+  const float s = q < kScaleMin ? kScaleMin : q;
+  inv = __builtin_amdgcn_rcpf(s);
+  return s;
+}
+
+// v over its block's scale s, within an ulp (the bare multiply moved values that
+// lie on a border between two of e4m3's, as bf16 inputs often do).  At most 448
+// (1 + 2^-22), which e4m3 rounds to 448, so nothing has to be clamped.  A block
+// whose scale is not finite becomes NaN as a whole.
 __device__ __forceinline__ float over_scale(float v, float s, float inv) {
-  const float r = v * inv;
-  return fmaf(fmaf(-r, s, v), inv, r);
+  return quotient(v, s, inv);
 }
 
 // Four values to e4m3 (nearest even), in one word.

@@ -11,12 +11,14 @@ namespace mhl {
 // How a row of d columns is held by the norm kernels.  Multiples of 8 by pieces
 // of 8 columns: in the registers of 16 or 32 lanes (up to 128 or 256 columns),
 // of a wavefront (up to 2048, 1 to 4 pieces per lane; no barrier, four rows per
-// workgroup) or of a workgroup (up to 16384; at 16384 rows of 4096 with 8 bits
-// out 46 us, 64 in a wavefront's registers).  Other widths column by column: 16
-// lanes (up to 64 columns), a wavefront (512), a workgroup (4096).  Wider rows
-// are not held at all.
+// workgroup) or of a workgroup (at 16384 rows of 4096 with 8 bits out 46 us, 64 in
+// a wavefront's registers) of 256 threads (up to 8192) or 512 (16384; us forward
+// and backward at 8192 rows of 16384 with 256 threads and 8 pieces 122 and 190,
+// with 512 and 4 97 and 167).  Other widths column by column: 16 lanes (up to 64
+// columns), a wavefront (512), a workgroup (4096).  Wider rows are not held at
+// all.
 enum class NormForm {
-  kPart16, kPart32, kWave1, kWave2, kWave4, kGroup2, kGroup4, kGroup8,
+  kPart16, kPart32, kWave1, kWave2, kWave4, kGroup2, kGroup4, kLarge4,
   kOdd16, kOddWave, kOddGroup, kWide8, kWide1
 };
 inline NormForm norm_form(int d) {
@@ -32,14 +34,14 @@ inline NormForm norm_form(int d) {
          : d <= 2048  ? NormForm::kWave4
          : d <= 4096  ? NormForm::kGroup2
          : d <= 8192  ? NormForm::kGroup4
-         : d <= 16384 ? NormForm::kGroup8
+         : d <= 16384 ? NormForm::kLarge4
                       : NormForm::kWide8;
 }
 // Rows that a workgroup of the register forms has at once.
 inline int norm_rows(NormForm f) {
   return f == NormForm::kPart16 || f == NormForm::kOdd16 ? 16
          : f == NormForm::kPart32                        ? 8
-         : f == NormForm::kGroup2 || f == NormForm::kGroup4 || f == NormForm::kGroup8 ||
+         : f == NormForm::kGroup2 || f == NormForm::kGroup4 || f == NormForm::kLarge4 ||
                  f == NormForm::kOddGroup
              ? 1
              : 4;
@@ -64,9 +66,10 @@ inline int64_t rmsnorm_bwd_parts(int64_t T, int d) {
     return ceil_div(T, 8) < most ? ceil_div(T, 8) : most;
   }
   // one per workgroup: two workgroups per CU, four where their rows are short and
-  // many (us with 256, 512, 1024, 2048: 74, 63, 64, 67 at 16384 x 2048, 49, 36, 33, 36
-  // at 16384 x 1024, 14, 13, 13, 15 at 4096 x 1024)
-  const int64_t n = ceil_div(T, norm_rows(norm_form(d))), most = d <= 1024 && T >= 16384 ? 1024 : 512;
+  // many (us with 256, 512, 1024, 2048: 61, 56, 58, 62 at 16384 x 2048, 34, 31, 32, 34
+  // at 16384 x 1024, 21, 17, 16, 19 at 16384 x 512, 12, 12, 13, 13 at 4096 x 1024)
+  const int64_t n = ceil_div(T, norm_rows(norm_form(d)));
+  const int64_t most = d <= 512 && T >= 16384 ? 1024 : 512;
   return n < most ? n : most;
 }
 hipError_t launch_rmsnorm_bwd(const void* h, const float* w, const void* dy, const void* dsum,

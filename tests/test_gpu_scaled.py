@@ -521,3 +521,38 @@ def test_many_rows():
     q, s = mh.mhlmoe_quantize(x[:, :512].contiguous())
     q2, s2 = mh.mhlmoe_quantize(rows[:, :512].contiguous())
     assert torch.equal(q.view(torch.uint8)[at], q2.view(torch.uint8)) and torch.equal(s[at], s2)
+
+
+@pytest.mark.parametrize("T,d", [(16383, 512), (16387, 512), (20001, 100), (40003, 64),
+                                 (16384, 1024)])
+def test_rmsnorm_backward_long_batch(T, d):
+    """Rows that the workgroups loop over, on both sides of the two numbers of
+    workgroups."""
+    g = _gen(T + d)
+    h, dy = _randn(g, T, d, dtype=BF16), _randn(g, T, d, dtype=BF16)
+    w = 1 + 0.3 * _randn(g, d)
+    dx, dw = mh.mhlmoe_rmsnorm_backward(h, w, EPS, dy)
+    want, wdw, t_abs, dw_abs = ref.norm_backward64(ref.host(h), ref.host(w), EPS, ref.host(dy), None)
+    eps = 3 * ref.norm_eps(d) + 4 * ref.U
+    assert np.all(np.abs(ref.host(dx) - want) <= eps * t_abs + (ref.HALF[BF16] + ref.U) * np.abs(want))
+    assert np.all(np.abs(ref.host(dw) - wdw) <= (T * ref.U + ref.norm_eps(d) + 2 * ref.U) * dw_abs)
+
+
+def test_rmsnorm_backward_far_rows():
+    """Offsets that pass 2^31 elements.  A row's dx does not depend on the other
+    rows; dy is zero but in four, so dw is their sum in some order."""
+    T, d = (1 << 22) + 3, 520
+    at = torch.tensor([0, 1 << 21, T - 2, T - 1], device="cuda")
+    h = torch.zeros((T, d), dtype=BF16, device="cuda")
+    dy = torch.zeros((T, d), dtype=BF16, device="cuda")
+    g = _gen(4)
+    rows, drows = _randn(g, 4, d, dtype=BF16), _randn(g, 4, d, dtype=BF16)
+    h[at], dy[at] = rows, drows
+    w = 1 + 0.3 * _randn(g, d)
+    dx, dw = mh.mhlmoe_rmsnorm_backward(h, w, EPS, dy)
+    dx4, dw4 = mh.mhlmoe_rmsnorm_backward(rows, w, EPS, drows)
+    assert torch.equal(dx[at], dx4)
+    assert not dx[1:1 << 21].any()
+    # two sums of the same four numbers, each within 3 roundings of the exact one
+    _, _, _, dw_abs = ref.norm_backward64(ref.host(rows), ref.host(w), EPS, ref.host(drows), None)
+    assert np.all(np.abs(ref.host(dw) - ref.host(dw4)) <= 6 * ref.U * dw_abs * (1 + 1e-5))
