@@ -344,19 +344,30 @@ __global__ __launch_bounds__(kNormThreads) void rmsnorm_bwd_columns_kernel(
 }
 
 // dw[c] = the sum of n partial rows: 32 columns per workgroup, every 32nd row
-// per thread, the 32 threads of a column added in order.
+// per thread, 16 of them on their way at once whatever their number (gradient of
+// 800 x 1024, 200 rows here: 8.1 -> 7.3 us against a loop unrolled 8 times, the
+// same at 512 rows), the 32 threads of a column added in order.
 __global__ __launch_bounds__(1024) void rmsnorm_dw_kernel(const float* __restrict__ part, int n,
                                                           int d, float* __restrict__ dw) {
   __shared__ float lds[32][33];
   const int c = blockIdx.x * 32 + threadIdx.x % 32, g = threadIdx.x / 32;
   float s = 0.0f;
   if (c < d) {
-#pragma unroll 8
-    for (int r = g; r < n; r += 32) s += part[(int64_t)r * d + c];
+    for (int r0 = g; r0 < n; r0 += 32 * 16) {
+      float v[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int r = r0 + 32 * i;
+        v[i] = r < n ? part[(int64_t)r * d + c] : 0.0f;
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s += v[i];
+    }
   }
   lds[g][threadIdx.x % 32] = s;
   __syncthreads();
   if (g == 0 && c < d) {
+#pragma unroll
     for (int i = 1; i < 32; ++i) s += lds[i][threadIdx.x];
     dw[c] = s;
   }
