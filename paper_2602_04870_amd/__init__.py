@@ -588,6 +588,8 @@ def _at(t, name, dtype, shape, device):
 
 def _launch(device, stream, fn, *args):
     """fn(*args, stream) with GPU number `device` as the current one."""
+    if stream is not None and getattr(stream, "device_index", device) != device:
+        raise ValueError(f"stream is on GPU {stream.device_index}, the tensors are on {device}")
     if device == torch.cuda.current_device():
         s = torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream)
         _check(fn(*args, s))
@@ -604,8 +606,18 @@ def _rows_cols(t, name):
     return t.shape
 
 
-def _new(t, shape, dtype, like):
-    return t if t is not None else torch.empty(shape, dtype=dtype, device=like.device)
+def _new(t, shape, dtype, like, stream):
+    """t, or a new tensor that belongs to the stream of the call, as one made
+    under torch.cuda.stream does: its memory goes back to that stream's work,
+    also where the caller drops it at once."""
+    if t is not None:
+        return t
+    if stream is None or not like.is_cuda:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(_stream(stream).value or 0, like.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=like.device)
 
 
 def mhlmoe_rmsnorm(x, weight, eps, *, residual=None, quantized=False, sum=None, y=None, q=None,
@@ -618,14 +630,14 @@ def mhlmoe_rmsnorm(x, weight, eps, *, residual=None, quantized=False, sum=None, 
     dt, dtype, dev, f32 = _dtype_code(x), x.dtype, x.get_device(), torch.float32
     grid = (T, -(-d // 128))
     if residual is not None:
-        sum = _new(sum, shape, dtype, x)
+        sum = _new(sum, shape, dtype, x, stream)
     if quantized:
-        q = _new(q, shape, E4M3, x)
-        scales = _new(scales, grid, f32, x)
+        q = _new(q, shape, E4M3, x, stream)
+        scales = _new(scales, grid, f32, x, stream)
     else:
         if q is not None or scales is not None:
             raise ValueError("q and scales are outputs of quantized=True")
-        y = _new(y, shape, dtype, x)
+        y = _new(y, shape, dtype, x, stream)
     _launch(dev, stream, load_library().mhlmoe_rmsnorm, _at(x, "x", dtype, shape, dev),
             _at(residual, "residual", dtype, shape, dev), _at(weight, "weight", f32, (d,), dev), T, d,
             eps, dt, _at(sum, "sum", dtype, shape, dev), _at(y, "y", dtype, shape, dev),
@@ -654,11 +666,11 @@ def mhlmoe_rmsnorm_backward(h, weight, eps, dy, *, dsum=None, dx=None, dweight=N
     past the norm; dx is the gradient of x and of residual."""
     T, d = shape = _rows_cols(h, "h")
     dt, dtype, dev, f32 = _dtype_code(h), h.dtype, h.get_device(), torch.float32
-    dx = _new(dx, shape, dtype, h)
-    dweight = _new(dweight, (d,), f32, h)
+    dx = _new(dx, shape, dtype, h, stream)
+    dweight = _new(dweight, (d,), f32, h, stream)
     if workspace is None:
         n = mhlmoe_rmsnorm_backward_workspace(T, d)
-        workspace = torch.empty(max(n, 256), dtype=torch.uint8, device=h.device)
+        workspace = _new(None, (max(n, 256),), torch.uint8, h, stream)
     _launch(dev, stream, load_library().mhlmoe_rmsnorm_backward, _at(h, "h", dtype, shape, dev),
             _at(weight, "weight", f32, (d,), dev), _at(dy, "dy", dtype, shape, dev),
             _at(dsum, "dsum", dtype, shape, dev), T, d, eps, dt, _at(dx, "dx", dtype, shape, dev),
@@ -675,8 +687,8 @@ def mhlmoe_quantize(x, *, block_rows=1, transpose=False, q=None, scales=None, st
     dt, dev, f32 = _dtype_code(x), x.get_device(), torch.float32
     a, k = shape = (cols, -(-rows // 16) * 16) if transpose else (rows, cols)
     grid = (-(-a // block_rows) if block_rows in (1, 128) else a, -(-k // 128))
-    q = _new(q, shape, E4M3, x)
-    scales = _new(scales, grid, f32, x)
+    q = _new(q, shape, E4M3, x, stream)
+    scales = _new(scales, grid, f32, x, stream)
     _launch(dev, stream, load_library().mhlmoe_quantize, _at(x, "x", x.dtype, x.shape, dev), rows,
             cols, dt, block_rows, 1 if transpose else 0, _at(q, "q", E4M3, shape, dev),
             _at(scales, "scales", f32, grid, dev))
@@ -691,7 +703,7 @@ def mhlmoe_gemm_scaled(A, scale_a, B, scale_b, *, b_block_rows=128, dtype=torch.
     N = _rows_cols(B, "B")[0]
     KB, dev, f32 = -(-K // 128), A.get_device(), torch.float32
     nb = -(-N // b_block_rows) if b_block_rows in (1, 128) else N
-    C = _new(C, (M, N), dtype, A)
+    C = _new(C, (M, N), dtype, A, stream)
     _launch(dev, stream, load_library().mhlmoe_gemm_scaled, _at(A, "A", E4M3, A.shape, dev),
             _at(scale_a, "scale_a", f32, (M, KB), dev), _at(B, "B", E4M3, (N, K), dev),
             _at(scale_b, "scale_b", f32, (nb, KB), dev), M, N, K, b_block_rows, _dtype_code(C),
@@ -724,19 +736,19 @@ def mhlmoe_latent_layer_scaled(x, norm_weight, eps, W_in, scale_in, W_router, bi
     Nh, N = n_heads, n_heads * dh
     dt, dtype, dev = _dtype_code(x), x.dtype, x.get_device()
     f32, i32 = torch.float32, torch.int32
-    out = _new(out, (T, dm), dtype, x)
+    out = _new(out, (T, dm), dtype, x, stream)
     if residual is not None:
-        sum = _new(sum, (T, dm), dtype, x)
-    X_lat = _new(X_lat, (T, Nh, dh), dtype, x)
+        sum = _new(sum, (T, dm), dtype, x, stream)
+    X_lat = _new(X_lat, (T, Nh, dh), dtype, x, stream)
     if W_r is not None:
-        R_lat = _new(R_lat, (T, Nh, dh), dtype, x)
-    Y_lat = _new(Y_lat, (T, Nh, dh), dtype, x)
-    idx = _new(idx, (T, Nh, top_k), i32, x)
-    gate = _new(gate, (T, Nh, top_k), f32, x)
-    counts = _new(counts, (Nh, Ne), i32, x)
+        R_lat = _new(R_lat, (T, Nh, dh), dtype, x, stream)
+    Y_lat = _new(Y_lat, (T, Nh, dh), dtype, x, stream)
+    idx = _new(idx, (T, Nh, top_k), i32, x, stream)
+    gate = _new(gate, (T, Nh, top_k), f32, x, stream)
+    counts = _new(counts, (Nh, Ne), i32, x, stream)
     if workspace is None:
         n = mhlmoe_latent_layer_scaled_workspace(T, dm, Nh, dh, Ne, top_k, dff, dt)
-        workspace = torch.empty(max(n, 256), dtype=torch.uint8, device=x.device)
+        workspace = _new(None, (max(n, 256),), torch.uint8, x, stream)
     grid = (-(-N // 128), -(-dm // 128))
 
     def at(t, name, dtype, *shape):

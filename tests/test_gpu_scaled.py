@@ -556,3 +556,33 @@ def test_rmsnorm_backward_far_rows():
     # two sums of the same four numbers, each within 3 roundings of the exact one
     _, _, _, dw_abs = ref.norm_backward64(ref.host(rows), ref.host(w), EPS, ref.host(drows), None)
     assert np.all(np.abs(ref.host(dw) - ref.host(dw4)) <= 6 * ref.U * dw_abs * (1 + 1e-5))
+
+
+@pytest.mark.parametrize("raw", [False, True])
+def test_tensors_of_a_call_belong_to_its_stream(raw):
+    """A workspace that the call makes, and an output that is dropped at once,
+    are not handed to the current stream while the given one still uses them."""
+    g = _gen(6)
+    T, d = 4096, 1024
+    h, dy = _randn(g, T, d, dtype=BF16), _randn(g, T, d, dtype=BF16)
+    w = 1 + 0.3 * _randn(g, d)
+    dx, dw = mh.mhlmoe_rmsnorm_backward(h, w, EPS, dy)
+    y = mh.mhlmoe_rmsnorm(h, w, EPS, residual=dy)["y"]
+    q, scales = mh.mhlmoe_quantize(h)
+    dx2, dw2, y2 = torch.empty_like(dx), torch.empty_like(dw), torch.empty_like(y)
+    a = _randn(g, 4096, 4096)
+    side = torch.cuda.Stream()
+    stream = side.cuda_stream if raw else side
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    with torch.cuda.stream(side):
+        for _ in range(10):  # milliseconds in front of the calls
+            a @ a
+    mh.mhlmoe_rmsnorm_backward(h, w, EPS, dy, dx=dx2, dweight=dw2, stream=stream)
+    mh.mhlmoe_rmsnorm(h, w, EPS, residual=dy, y=y2, stream=stream)
+    q2, scales2 = mh.mhlmoe_quantize(h, stream=stream)
+    fill = [torch.full((n,), float("nan"), device="cuda") for n in (T * d // 2, 512 * d) * 4]
+    torch.cuda.synchronize()
+    assert torch.equal(dx, dx2) and torch.equal(dw, dw2) and torch.equal(y, y2)
+    assert torch.equal(q.view(torch.uint8), q2.view(torch.uint8)) and torch.equal(scales, scales2)
+    assert all(torch.isnan(f).all() for f in fill)

@@ -131,6 +131,14 @@ def test_binding_refuses():
         m.mhlmoe_gemm_scaled(None, w, x, w)
 
 
+def test_binding_refuses_another_device_s_stream():
+    class Stream:
+        device_index, cuda_stream = 1, 0
+
+    with pytest.raises(ValueError, match="stream is on GPU 1, the tensors are on 0"):
+        m._launch(0, Stream(), lambda *a: pytest.fail("launched"))
+
+
 def test_names_of_the_product_are_declared():
     """Every kernel the scaled entry points time is named in the header."""
     header = open(m.HEADER).read()
