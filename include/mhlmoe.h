@@ -546,8 +546,9 @@ mhlmoe_status mhlmoe_quantize(const void *x, int64_t rows, int64_t cols,
  * b_block_rows is 128 (weights quantised in tiles) or 1 (both operands
  * quantised by rows: the weight gradient).  K must be a multiple of 16; M and
  * N are any sizes (C's rows then need no alignment).  A block's sum is the
- * matrix cores' (fp32), blocks are added in fp32 in a fixed order; C is
- * rounded once.  K = 0 writes zeros.  M, N < 2^31, K < 2^23,
+ * matrix cores' (fp32), its two scales' product is taken in fp32 (and must not
+ * overflow there), blocks are added in fp32 in a fixed order; C is rounded
+ * once.  K = 0 writes zeros.  M, N < 2^31, K < 2^23,
  * ceil(M / 128) ceil(N / 128) < 2^24.  No workspace.
  */
 mhlmoe_status mhlmoe_gemm_scaled(const void *A, const float *scale_a,

@@ -91,7 +91,8 @@ __device__ __forceinline__ void store4(void* C, int64_t at, f32x4 v) {
 }
 // ... or those of them that C has.
 template <bool F32>
-__device__ __forceinline__ void store_edge(void* C, int64_t m, int64_t M, int64_t n, int64_t N, f32x4 v) {
+__device__ __forceinline__ void store_edge(void* C, int64_t m, int64_t M, int64_t n, int64_t N,
+                                           f32x4 v) {
   if (m >= M) return;
 #pragma unroll
   for (int e = 0; e < 4; ++e)
@@ -138,7 +139,6 @@ struct Tile {
   static_assert(SPIECES_A * 16 * WAVES == BM && SPIECES_B * 16 * WAVES == BN, "whole pieces of scales");
   static_assert(NT * 16 <= kScaleBlock && kScaleBlock % (NT * 16) == 0, "one tile scale per wavefront");
   static_assert(LDS <= 160 * 1024 && (KS == 1 || KS * 64 * WAVES * MT * NT * 16 <= LDS), "LDS");
-
 };
 
 // What a wavefront fetches: of a block its 1 KiB pieces of A and of B; of the
@@ -549,13 +549,23 @@ hipError_t launch_gemm_scaled(const void* A, const float* sa, const void* B, con
                               hipStream_t s) {
   const uint8_t* a = static_cast<const uint8_t*>(A);
   const uint8_t* b = static_cast<const uint8_t*>(B);
-  const GemmForm form = gemm_scaled_form(M, N, f32);
+  const GemmForm form = gemm_scaled_form(M, N, K, f32);
 #define MHL_GEMM(F32, ROWS)                                                               \
   switch (form) {                                                                         \
-    case GemmForm::kFew16: launch_few<1, 1, 4, F32, ROWS>(a, sa, b, sb, M, N, K, C, s); break; \
-    case GemmForm::kFew32: launch_few<2, 1, 4, F32, ROWS>(a, sa, b, sb, M, N, K, C, s); break; \
+    case GemmForm::kFew16:                                                                \
+      launch_few<1, 1, 4, F32, ROWS>(a, sa, b, sb, M, N, K, C, s);                        \
+      break;                                                                              \
+    case GemmForm::kFew16Wide:                                                            \
+      launch_few<1, 2, 2, F32, ROWS>(a, sa, b, sb, M, N, K, C, s);                        \
+      break;                                                                              \
+    case GemmForm::kFew32:                                                                \
+      launch_few<2, 1, 4, F32, ROWS>(a, sa, b, sb, M, N, K, C, s);                        \
+      break;                                                                              \
     case GemmForm::kFew32Wide:                                                            \
       launch_few<2, 2, 2, F32, ROWS>(a, sa, b, sb, M, N, K, C, s);                        \
+      break;                                                                              \
+    case GemmForm::kFew32Widest:                                                          \
+      launch_few<2, 4, 1, F32, ROWS>(a, sa, b, sb, M, N, K, C, s);                        \
       break;                                                                              \
     case GemmForm::k64:                                                                   \
       launch_tile<2, 1, 2, 4, 4, F32, ROWS>(a, sa, b, sb, M, N, K, C, s);                 \

@@ -83,8 +83,8 @@ hipError_t launch_rmsnorm_dw(const float* part, int64_t n, int d, float* dw, hip
 hipError_t launch_quantize(const void* x, int64_t rows, int64_t cols, bool f32, int block_rows,
                            bool transpose, void* q, float* scales, hipStream_t s);
 
-// How the 8-bit product is cut up.  Few rows of A: B straight into registers, 16
-// or 32 of its rows per workgroup.  Else tiles of C: 64 x 64 with the blocks
+// How the 8-bit product is cut up.  Few rows of A: B straight into registers, 16,
+// 32 or 64 of its rows per workgroup (below).  Else tiles of C: 64 x 64 with the blocks
 // along K over four groups of wavefronts (kept while they do not outnumber the
 // CUs), 128 x 128 over two groups, 128 x 128 with two workgroups per CU, or 256 x
 // 256 (bf16 results; fp32 ones need the registers for widened pieces).  us at
@@ -100,14 +100,36 @@ hipError_t launch_quantize(const void* x, int64_t rows, int64_t cols, bool f32, 
 //   3584  3584   83       50       37     30
 //   8192  8192 1412      754      600    458
 // A round of 256 x 256 tiles (one per CU) takes about 9 / 5 of one of 128 x 128
-// tiles (two per CU); whichever's rounds take less is chosen.  Rows of A, at N =
-// K = 8192: 12 us at 1, 20 at 16, 24 at 32 (32 with 16 rows of B per workgroup),
-// the 64 x 64 tiles 22.5 at 64 (33 with A in registers).
-enum class GemmForm { kFew16, kFew32, kFew32Wide, k64, k128Split, k128, k256 };
-inline GemmForm gemm_scaled_form(int64_t M, int64_t N, bool f32) {
-  // (the former's workgroups of 512 threads must fit a grid of 2^32)
-  if (M <= 16 && N < (1 << 26)) return GemmForm::kFew16;
-  if (M <= 32 && N < (1 << 26)) return N >= 32 * 256 ? GemmForm::kFew32Wide : GemmForm::kFew32;
+// tiles (two per CU); whichever's rounds take less is chosen.
+//
+// Few rows of A, us by rows of B per workgroup, of which more share the reads of
+// A (64 x 64 tiles: 22.5 at 64 x 8192 x 8192, 33 with A in registers):
+//     M      N     K     16     32     64
+//     1   8192  8192   12.3   14.9   19.4
+//     1  16384  2048    8.4    7.2
+//     1  16384  8192   24.8   28.2
+//     1  65536  2048   29.5   25.9   27.0
+//    16   4096  4096    7.1    8.7   12.8
+//    16   8192  8192   20.5   18.5   23.4
+//    16  11264  1024    7.1    5.6
+//    16  12288  8192   31.1   32.3
+//    16  16384  8192   42.1   34.8
+//    16  65536  2048   43.4   32.8   32.1
+//    32   8192  8192   32     23.8   31.2
+//    32  16384  2048          11.8   10.5
+//    32  65536  2048          41.1   33.8
+enum class GemmForm {
+  kFew16, kFew16Wide, kFew32, kFew32Wide, kFew32Widest, k64, k128Split, k128, k256
+};
+inline GemmForm gemm_scaled_form(int64_t M, int64_t N, int64_t K, bool f32) {
+  // (the few rows' workgroups of 512 threads must fit a grid of 2^32)
+  if (M <= 16 && N < (1 << 26))
+    return (N >= 32 * 320 && K <= 4096) || (N >= 32 * 512 && M > 4) ? GemmForm::kFew16Wide
+                                                                    : GemmForm::kFew16;
+  if (M <= 32 && N < (1 << 26))
+    return N >= 64 * 256   ? GemmForm::kFew32Widest
+           : N >= 32 * 256 ? GemmForm::kFew32Wide
+                           : GemmForm::kFew32;
   if (ceil_div(M, 64) * ceil_div(N, 64) <= 256) return GemmForm::k64;
   const int64_t tiles = ceil_div(M, 128) * ceil_div(N, 128);
   if (tiles <= 256) return GemmForm::k128Split;

@@ -58,13 +58,17 @@ int main() {
   for (int64_t M : sizes)
     for (int64_t N : sizes) {
       if (mhl::ceil_div(M, 128) >= (int64_t(1) << 24) / mhl::ceil_div(N, 128)) continue;
-      for (int f32 = 0; f32 < 2; ++f32) {
-        const mhl::GemmForm f = mhl::gemm_scaled_form(M, N, f32 != 0);
+      for (int v = 0; v < 4; ++v) {
+        const int f32 = v & 1;
+        const int64_t K = v & 2 ? 8192 : 256;
+        const mhl::GemmForm f = mhl::gemm_scaled_form(M, N, K, f32 != 0);
         int64_t groups = 0, threads = 0;
         switch (f) {
           case mhl::GemmForm::kFew16:
           case mhl::GemmForm::kFew32: groups = mhl::ceil_div(N, 16), threads = 512; break;
+          case mhl::GemmForm::kFew16Wide:
           case mhl::GemmForm::kFew32Wide: groups = mhl::ceil_div(N, 32), threads = 512; break;
+          case mhl::GemmForm::kFew32Widest: groups = mhl::ceil_div(N, 64), threads = 512; break;
           case mhl::GemmForm::k64:
             groups = mhl::ceil_div(M, 64) * mhl::ceil_div(N, 64), threads = 512;
             break;

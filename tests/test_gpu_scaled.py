@@ -239,7 +239,8 @@ GEMM_SHAPES = [(1, 1, 16), (1, 7, 128), (2, 128, 400), (3, 1000, 144), (15, 16, 
                (1100, 1300, 336),
                # B of 8192 rows and more under few rows of A; over 256 tiles of 64 x 64, of 128 x 128;
                # enough for tiles of 256 x 256, whole and not
-               (20, 8209, 272), (32, 8192, 1152), (1030, 1100, 144), (1152, 1152, 1152),
+               (20, 8209, 272), (32, 8192, 1152), (1, 10249, 272), (16, 16384, 144), (19, 16401, 400),
+               (1030, 1100, 144), (1152, 1152, 1152),
                (2310, 2050, 272), (2304, 2048, 896), (3600, 3401, 272), (4096, 3328, 640)]
 
 
@@ -263,6 +264,8 @@ def test_gemm(M, N, K, block, dtype):
 
 @pytest.mark.parametrize("M,N,K", [(1, 40, 272), (37, 100, 144), (64, 256, 2048), (130, 270, 400),
                                    (300, 260, 640), (1000, 1024, 512), (31, 8200, 400),
+                                   (1, 10300, 272), (9, 16400, 4112), (16, 10240, 528),
+                                   (25, 16390, 656),
                                    (1100, 1200, 912), (2400, 2100, 528), (3500, 3600, 400)])
 @pytest.mark.parametrize("block", [128, 1])
 def test_gemm_exact(M, N, K, block):
