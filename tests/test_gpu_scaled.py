@@ -589,3 +589,24 @@ def test_tensors_of_a_call_belong_to_its_stream(raw):
     assert torch.equal(dx, dx2) and torch.equal(dw, dw2) and torch.equal(y, y2)
     assert torch.equal(q.view(torch.uint8), q2.view(torch.uint8)) and torch.equal(scales, scales2)
     assert all(torch.isnan(f).all() for f in fill)
+
+
+def test_default_stream_by_handle_and_capture_by_argument():
+    """stream may be the default stream's handle (0), and the capturing stream
+    itself: outputs and workspace are then the graph's."""
+    g = _gen(9)
+    h, dy, w = _randn(g, 70, 520, dtype=BF16), _randn(g, 70, 520, dtype=BF16), _randn(g, 520)
+    dx, dw = mh.mhlmoe_rmsnorm_backward(h, w, EPS, dy)
+    dx0, dw0 = mh.mhlmoe_rmsnorm_backward(h, w, EPS, dy, stream=0)
+    torch.cuda.synchronize()
+    assert torch.equal(dx, dx0) and torch.equal(dw, dw0)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        dx1, dw1 = mh.mhlmoe_rmsnorm_backward(h, w, EPS, dy, stream=torch.cuda.current_stream())
+    for i in range(3):
+        h.copy_(_randn(g, 70, 520))
+        torch.cuda.synchronize()
+        graph.replay()
+        dx, dw = mh.mhlmoe_rmsnorm_backward(h, w, EPS, dy)
+        torch.cuda.synchronize()
+        assert torch.equal(dx, dx1) and torch.equal(dw, dw1), i
