@@ -14,12 +14,12 @@ namespace mhl {
 // workgroup) or of a workgroup (at 16384 rows of 4096 with 8 bits out 46 us, 64 in
 // a wavefront's registers) of 256 threads (up to 8192) or 512 (16384; us forward
 // and backward at 8192 rows of 16384 with 256 threads and 8 pieces 122 and 190,
-// with 512 and 4 97 and 167).  Other widths column by column: 16 lanes (up to 64
-// columns), a wavefront (512), a workgroup (4096).  Wider rows are not held at
-// all.
+// with 512 and 4 97 and 167; forward only, up to 32768: 272 -> 223 at 4096 rows).
+// Other widths column by column: 16 lanes (up to 64 columns), a wavefront (512), a
+// workgroup (4096).  Wider rows are not held at all.
 enum class NormForm {
   kPart16, kPart32, kWave1, kWave2, kWave4, kGroup2, kGroup4, kLarge4,
-  kOdd16, kOddWave, kOddGroup, kWide8, kWide1
+  kOdd16, kOddWave, kOddGroup, kLarge8, kWide8, kWide1
 };
 inline NormForm norm_form(int d) {
   if (d % 8 != 0)
@@ -35,6 +35,7 @@ inline NormForm norm_form(int d) {
          : d <= 4096  ? NormForm::kGroup2
          : d <= 8192  ? NormForm::kGroup4
          : d <= 16384 ? NormForm::kLarge4
+         : d <= 32768 ? NormForm::kLarge8
                       : NormForm::kWide8;
 }
 // Rows that a workgroup of the register forms has at once.
@@ -42,7 +43,7 @@ inline int norm_rows(NormForm f) {
   return f == NormForm::kPart16 || f == NormForm::kOdd16 ? 16
          : f == NormForm::kPart32                        ? 8
          : f == NormForm::kGroup2 || f == NormForm::kGroup4 || f == NormForm::kLarge4 ||
-                 f == NormForm::kOddGroup
+                 f == NormForm::kLarge8 || f == NormForm::kOddGroup
              ? 1
              : 4;
 }
@@ -58,11 +59,11 @@ hipError_t launch_rmsnorm(const void* x, const void* residual, const float* w, i
 // floats, which launch_rmsnorm_dw adds in order.  rows: 2 T floats where
 // rmsnorm_bwd_wide, else unused.
 inline bool rmsnorm_bwd_wide(int d) {
-  return norm_form(d) == NormForm::kWide8 || norm_form(d) == NormForm::kWide1;
+  return norm_form(d) >= NormForm::kLarge8;  // the last three
 }
 inline int64_t rmsnorm_bwd_parts(int64_t T, int d) {
-  if (rmsnorm_bwd_wide(d)) {  // chunks of rows under each 256 columns
-    const int64_t most = (int64_t(1) << 19) / d > 16 ? (int64_t(1) << 19) / d : 16;
+  if (rmsnorm_bwd_wide(d)) {  // chunks of rows under each 2048 or 256 columns
+    const int64_t fill = (int64_t(1) << (d % 8 == 0 ? 22 : 19)) / d, most = fill > 16 ? fill : 16;
     return ceil_div(T, 8) < most ? ceil_div(T, 8) : most;
   }
   // one per workgroup: two workgroups per CU, four where their rows are short and

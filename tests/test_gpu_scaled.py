@@ -38,7 +38,8 @@ def _guarded(shape, dtype, fill=93):
 # widths of every form of the kernels: full, one short of it, one past it, odd,
 # and wider than the registers' forms
 WIDTHS = [1, 7, 8, 16, 28, 63, 65, 100, 112, 128, 136, 250, 256, 264, 512, 513, 520, 1000, 1001,
-          1024, 1032, 2048, 2056, 4095, 4096, 4097, 4112, 8192, 8208, 12304, 16384, 16400, 20001]
+          1024, 1032, 2048, 2056, 4095, 4096, 4097, 4112, 8192, 8208, 12304, 16384, 16400, 20001,
+          32768, 32784]
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
@@ -75,7 +76,7 @@ def test_rmsnorm(d, dtype, residual):
             ref.check_blocks(ref.host(out["q"]), ref.host(out["scales"]), want, 1, eps, f"d={d}")
 
 
-@pytest.mark.parametrize("d", [24, 1024, 5000, 20000])
+@pytest.mark.parametrize("d", [24, 1024, 5000, 20000, 40000])
 def test_rmsnorm_in_place(d):
     """sum may be x or residual, y may be x."""
     g = _gen(d)
@@ -527,10 +528,10 @@ def test_many_rows():
 
 
 @pytest.mark.parametrize("T,d", [(16383, 512), (16387, 512), (20001, 100), (40003, 64),
-                                 (16384, 1024)])
+                                 (16384, 1024), (2500, 16392), (600, 65536), (300, 65535)])
 def test_rmsnorm_backward_long_batch(T, d):
     """Rows that the workgroups loop over, on both sides of the two numbers of
-    workgroups."""
+    workgroups, and more of wide rows than there are chunks."""
     g = _gen(T + d)
     h, dy = _randn(g, T, d, dtype=BF16), _randn(g, T, d, dtype=BF16)
     w = 1 + 0.3 * _randn(g, d)
