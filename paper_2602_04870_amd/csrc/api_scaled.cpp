@@ -47,8 +47,9 @@ mhlmoe_status check_workspace(const void* ws, size_t have, size_t need_bytes) {
   return MHLMOE_OK;
 }
 
-// A launch's threads are counted in 32 bits.
-bool fits_grid(int64_t a, int64_t b) { return b == 0 || a < (int64_t(1) << 24) / b; }
+// Fewer than 2^24 workgroups (a launch's threads are counted in 32 bits); a and b
+// below 2^31, so that their product is exact.
+bool fits_grid(int64_t a, int64_t b) { return a * b < int64_t(1) << 24; }
 
 mhlmoe_status check_gemm(int64_t M, int64_t N, int64_t K, int b_block_rows) {
   if (M < 0 || N < 0 || K < 0)
@@ -187,11 +188,11 @@ mhlmoe_status mhlmoe_quantize(const void* x, int64_t rows, int64_t cols, mhlmoe_
   if (cols % 16 != 0)
     return fail(MHLMOE_EUNSUPPORTED, "cols %lld is no multiple of 16", (long long)cols);
   const int64_t most = int64_t(1) << 31;
-  // 1 x 128 blocks of x's rows are counted in 32 bits (256 rows of them stand for a tile), tiles
-  // as workgroups
+  // 1 x 128 blocks of x's rows are counted in 32 bits, tiles as workgroups
   if (rows >= most || cols >= most ||
-      !fits_grid(block_rows == 1 && !transpose ? rows / 256 : mhl::ceil_div(rows, 128),
-                 mhl::ceil_div(cols, 128)))
+      !(block_rows == 1 && !transpose
+            ? rows * mhl::ceil_div(cols, 128) < int64_t(1) << 32
+            : fits_grid(mhl::ceil_div(rows, 128), mhl::ceil_div(cols, 128))))
     return fail(MHLMOE_EUNSUPPORTED, "%lld x %lld is too large", (long long)rows, (long long)cols);
   const int64_t n = rows == 0 || cols == 0 ? 0 : 1;
   MHL_TRY(need_rows(x, "x", n));
