@@ -598,6 +598,13 @@ def _launch(device, stream, fn, *args):
         _check(fn(*args, _stream(stream)))
 
 
+def _int(v, name):
+    """v, where the C ABI takes an int: ctypes would pass on its low 32 bits."""
+    if not -(1 << 31) <= v < 1 << 31:
+        raise ValueError(f"{name} must fit 32 bits (got {v})")
+    return v
+
+
 def _rows_cols(t, name):
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
@@ -627,6 +634,7 @@ def mhlmoe_rmsnorm(x, weight, eps, *, residual=None, quantized=False, sum=None, 
     instead of y; pass y as well to have both.  Returns a dict with sum (with
     residual), y, q and scales."""
     T, d = shape = _rows_cols(x, "x")
+    _int(d, "d_model")
     dt, dtype, dev, f32 = _dtype_code(x), x.dtype, x.get_device(), torch.float32
     grid = (T, -(-d // 128))
     if residual is not None:
@@ -655,7 +663,8 @@ def mhlmoe_rmsnorm(x, weight, eps, *, residual=None, quantized=False, sum=None, 
 def mhlmoe_rmsnorm_backward_workspace(T: int, d_model: int) -> int:
     """Workspace bytes of mhlmoe_rmsnorm_backward."""
     out = _SZ(0)
-    _check(load_library().mhlmoe_rmsnorm_backward_workspace(T, d_model, ctypes.byref(out)))
+    _check(load_library().mhlmoe_rmsnorm_backward_workspace(T, _int(d_model, "d_model"),
+                                                            ctypes.byref(out)))
     return out.value
 
 
@@ -665,6 +674,7 @@ def mhlmoe_rmsnorm_backward(h, weight, eps, dy, *, dsum=None, dx=None, dweight=N
     no residual): returns (dx, dweight).  dsum: the gradient that reaches h
     past the norm; dx is the gradient of x and of residual."""
     T, d = shape = _rows_cols(h, "h")
+    _int(d, "d_model")
     dt, dtype, dev, f32 = _dtype_code(h), h.dtype, h.get_device(), torch.float32
     dx = _new(dx, shape, dtype, h, stream)
     dweight = _new(dweight, (d,), f32, h, stream)
@@ -685,6 +695,7 @@ def mhlmoe_quantize(x, *, block_rows=1, transpose=False, q=None, scales=None, st
     multiple of 16.  Returns (q, scales)."""
     rows, cols = _rows_cols(x, "x")
     dt, dev, f32 = _dtype_code(x), x.get_device(), torch.float32
+    _int(block_rows, "block_rows")
     a, k = shape = (cols, -(-rows // 16) * 16) if transpose else (rows, cols)
     grid = (-(-a // block_rows) if block_rows in (1, 128) else a, -(-k // 128))
     q = _new(q, shape, E4M3, x, stream)
@@ -702,6 +713,7 @@ def mhlmoe_gemm_scaled(A, scale_a, B, scale_b, *, b_block_rows=128, dtype=torch.
     M, K = _rows_cols(A, "A")
     N = _rows_cols(B, "B")[0]
     KB, dev, f32 = -(-K // 128), A.get_device(), torch.float32
+    _int(b_block_rows, "b_block_rows")
     nb = -(-N // b_block_rows) if b_block_rows in (1, 128) else N
     C = _new(C, (M, N), dtype, A, stream)
     _launch(dev, stream, load_library().mhlmoe_gemm_scaled, _at(A, "A", E4M3, A.shape, dev),
@@ -716,8 +728,10 @@ def mhlmoe_latent_layer_scaled_workspace(T: int, d_model: int, n_heads: int, d_h
                                          dtype: int = MHLMOE_BF16) -> int:
     """Workspace bytes of mhlmoe_latent_layer_scaled."""
     out = _SZ(0)
+    shape = dict(d_model=d_model, n_heads=n_heads, d_head=d_head, n_experts=n_experts,
+                 top_k=top_k, d_ff=d_ff)
     _check(load_library().mhlmoe_latent_layer_scaled_workspace(
-        T, d_model, n_heads, d_head, n_experts, top_k, d_ff, dtype, ctypes.byref(out)))
+        T, *(_int(v, name) for name, v in shape.items()), dtype, ctypes.byref(out)))
     return out.value
 
 
@@ -734,6 +748,9 @@ def mhlmoe_latent_layer_scaled(x, norm_weight, eps, W_in, scale_in, W_router, bi
     T, dm = _rows_cols(x, "x")
     Ne, dff, dh = W1.shape[1], W1.shape[2], W1.shape[3]
     Nh, N = n_heads, n_heads * dh
+    for v, name in ((dm, "d_model"), (Nh, "n_heads"), (Ne, "n_experts"), (top_k, "top_k"),
+                    (dff, "d_ff"), (dh, "d_head")):
+        _int(v, name)
     dt, dtype, dev = _dtype_code(x), x.dtype, x.get_device()
     f32, i32 = torch.float32, torch.int32
     out = _new(out, (T, dm), dtype, x, stream)
