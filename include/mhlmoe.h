@@ -482,7 +482,9 @@ mhlmoe_status mhlmoe_bias_update(const int32_t *counts, float *bias,
  *            must be a multiple of 16
  * y and q may both be asked for; at least one must be.  The norm is that of
  * the rounded h, which mhlmoe_rmsnorm_backward reads.  1 <= d_model <= 65536,
- * T < 2^31, eps finite and > 0.  Sums and the norm are in fp32.  No workspace.
+ * T < 2^31, eps finite and > 0.  Sums and the norm are in fp32: where the sum
+ * of a row's squares is infinite there, its finite elements become zeros.  No
+ * workspace.
  */
 mhlmoe_status mhlmoe_rmsnorm(const void *x, const void *residual,
                              const float *weight, int64_t T, int d_model,
@@ -545,11 +547,23 @@ mhlmoe_status mhlmoe_quantize(const void *x, int64_t rows, int64_t cols,
  *   C       [M][N] out_dtype                                           (out)
  * b_block_rows is 128 (weights quantised in tiles) or 1 (both operands
  * quantised by rows: the weight gradient).  K must be a multiple of 16; M and
- * N are any sizes (C's rows then need no alignment).  A block's sum is the
- * matrix cores' (fp32), its two scales' product is taken in fp32 (and must not
- * overflow there), blocks are added in fp32 in a fixed order; C is rounded
- * once.  K = 0 writes zeros.  M, N < 2^31, K < 2^23,
- * ceil(M / 128) ceil(N / 128) < 2^24.  No workspace.
+ * N are any sizes (C's rows then need no alignment).
+ *
+ * A block's sum depends on out_dtype.  MHLMOE_F32: the products are exact and
+ * added in fp32.  MHLMOE_BF16: the 8-bit matrix instructions (twice the rate)
+ * add eight products of a block at a time and drop of each what lies below
+ * 2^-13 of the largest of the eight, then add the groups in fp32.  Besides the
+ * roundings of fp32 a result is so off by up to 7 * 2^-13 of the sum of its
+ * terms' magnitudes before it is rounded to bf16: nothing next to that rounding
+ * where the terms are alike (about 1e-5 of the result for random operands), but
+ * products below 2^-13 of others that cancel are lost.  A caller who needs them
+ * asks for MHLMOE_F32.
+ *
+ * A block's two scales are multiplied in fp32 before they meet its sum: the
+ * product must not overflow, and below 2^-126 it loses bits, down to zero, even
+ * where the block's sum (up to 448 * 448 * 128 < 2^25) would lift the result back.
+ * Blocks are added in fp32 in a fixed order; C is rounded once.  K = 0 writes
+ * zeros.  M, N < 2^31, K < 2^23, ceil(M / 128) ceil(N / 128) < 2^24.  No workspace.
  */
 mhlmoe_status mhlmoe_gemm_scaled(const void *A, const float *scale_a,
                                  const void *B, const float *scale_b, int64_t M,
@@ -571,8 +585,11 @@ mhlmoe_status mhlmoe_gemm_scaled(const void *A, const float *scale_a,
  * scales per 128 x 128 tile (mhlmoe_quantize, block_rows 128); W_r gives the
  * separate routing sub-tokens of Eq. (9).  residual and sum, X_lat, R_lat,
  * Y_lat, idx, gate and counts are optional as in the calls themselves.
+ * The products are mhlmoe_gemm_scaled's with out_dtype = dtype: the latent
+ * activations, and with them the routing, of a bf16 layer carry its 8-bit sums.
  * d_model must be a multiple of 16 in [16, 65536].  Workspace: the size that
- * mhlmoe_latent_layer_scaled_workspace writes to *bytes.
+ * mhlmoe_latent_layer_scaled_workspace writes to *bytes, which has room for
+ * X_lat, R_lat and Y_lat whether or not the caller passes them.
  */
 mhlmoe_status mhlmoe_latent_layer_scaled_workspace(
     int64_t T, int d_model, int n_heads, int d_head, int n_experts, int top_k,
