@@ -463,7 +463,10 @@ mhlmoe_status mhlmoe_bias_update(const int32_t *counts, float *bias,
  *
  *   scale = max(max |v| / 448, 2^-126),   q = e4m3(v / scale), nearest even,
  *
- * so q * scale stands for v; the last block of a row may be shorter.  A block
+ * so q * scale stands for v; the last block of a row may be shorter.  The scale
+ * is rounded to fp32, and v / scale is taken in fp32 (within an ulp) on its way
+ * to e4m3: a quotient within an fp32 step of a border between two of e4m3's
+ * values, as those of bf16 values often are, can count as lying on it.  A block
  * that holds an infinity or a NaN becomes NaN as a whole.
  *
  * Residual sum and root-mean-square norm, per row t of d_model columns c:

@@ -162,10 +162,12 @@ __device__ __forceinline__ float block_scale(uint32_t amax, float& inv) {
   return s;
 }
 
-// v over its block's scale s, within an ulp (the bare multiply moved values that
-// lie on a border between two of e4m3's, as bf16 inputs often do).  At most 448
-// (1 + 2^-22), which e4m3 rounds to 448, so nothing has to be clamped.  A block
-// whose scale is not finite becomes NaN as a whole.
+// v over its block's scale s, less than 2^-44 of itself off before its rounding to
+// fp32 (an ulp for v below 2^-106, whose remainder is a denormal number; the bare
+// multiply, 2^-22 off, moved values that lie on a border between two of e4m3's, as
+// bf16 inputs often do).  At most 448 (1 + 2^-22), which e4m3 rounds to
+// 448, so nothing has to be clamped.  A block whose scale is not finite becomes NaN
+// as a whole.
 __device__ __forceinline__ float over_scale(float v, float s, float inv) {
   return quotient(v, s, inv);
 }
