@@ -102,6 +102,8 @@ hipError_t launch_quantize(const void* x, int64_t rows, int64_t cols, bool f32, 
 //   8192  8192 1412      754      600    458
 // A round of 256 x 256 tiles (one per CU) takes about 9 / 5 of one of 128 x 128
 // tiles (two per CU); whichever's rounds take less is chosen.
+// fp32 results (no 256 x 256) take the same thresholds, which were not measured
+// for them.
 //
 // Few rows of A, us by rows of B per workgroup, of which more share the reads of
 // A (64 x 64 tiles: 22.5 at 64 x 8192 x 8192, 33 with A in registers):
@@ -119,6 +121,10 @@ hipError_t launch_quantize(const void* x, int64_t rows, int64_t cols, bool f32, 
 //    32   8192  8192   32     23.8   31.2
 //    32  16384  2048          11.8   10.5
 //    32  65536  2048          41.1   33.8
+// The rule goes by the workgroups that are left.  Up to 16 rows of A: 32 of B where
+// that leaves 320 and K is at most 4096, or 512 and A has more than 4 rows (so 16
+// x 8192 x 8192 stays with 16, at 20.5 against 18.5, and 16 x 12288 x 8192 with 31.1
+// against 32.3).  Up to 32: 64 or else 32 where that leaves 256.
 enum class GemmForm {
   kFew16, kFew16Wide, kFew32, kFew32Wide, kFew32Widest, k64, k128Split, k128, k256
 };
