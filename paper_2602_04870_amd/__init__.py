@@ -709,7 +709,9 @@ def mhlmoe_quantize(x, *, block_rows=1, transpose=False, q=None, scales=None, st
 def mhlmoe_gemm_scaled(A, scale_a, B, scale_b, *, b_block_rows=128, dtype=torch.bfloat16, C=None,
                        stream=None):
     """C [M, N] (dtype) = A [M, K] B [N, K]^T of e4m3 operands with scales per
-    block of 128 along K: scale_a [M, KB], scale_b [ceil(N / b_block_rows), KB]."""
+    block of 128 along K: scale_a [M, KB], scale_b [ceil(N / b_block_rows), KB].
+    float32 results are sums in fp32; bfloat16 ones lose, of products in a group
+    of eight, what lies below 2^-13 of the largest."""
     M, K = _rows_cols(A, "A")
     N = _rows_cols(B, "B")[0]
     KB, dev, f32 = -(-K // 128), A.get_device(), torch.float32
