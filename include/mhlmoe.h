@@ -609,6 +609,179 @@ mhlmoe_status mhlmoe_latent_layer_scaled(
     hipStream_t stream);
 
 /*
+ * What a training step has around the layer besides: layer norm, the loss that
+ * balances the experts by gradient, and the optimiser's step.
+ *
+ * Residual sum and layer norm, per row t of d_model columns c:
+ *
+ *   h = x + residual, rounded to dtype        (h = x where residual is NULL)
+ *   y[c] = (h[c] - mu) / sqrt(var + eps) * weight[c] + bias[c],
+ *   mu = mean_c' h[c'],  var = mean_c' (h[c'] - mu)^2
+ *
+ *   bias [d_model] float or NULL (zeros)                               (in)
+ * The other arguments, what may be NULL, which of them may be the same tensor, the
+ * 8-bit output and the extents are mhlmoe_rmsnorm's.  Sums are in fp32; a row that
+ * holds an infinity or a NaN, or whose sums overflow there, becomes NaN or zeros
+ * in itself only.  No workspace.
+ */
+mhlmoe_status mhlmoe_layernorm(const void *x, const void *residual,
+                               const float *weight, const float *bias,
+                               int64_t T, int d_model, float eps,
+                               mhlmoe_dtype dtype, void *sum, void *y, void *q,
+                               float *scales, hipStream_t stream);
+
+/*
+ * Its gradient, with rs = 1 / sqrt(var + eps), n = (h - mu) rs, g = dy * weight:
+ *
+ *   dx[c] = dsum[c] + rs (g[c] - mean_c' g[c'] - n[c] mean_c'(g[c'] n[c']))
+ *   dweight[c] = sum_t dy[c] n[c],   dbias[c] = sum_t dy[c]
+ *
+ *   dbias [d_model] float or NULL (not wanted)  overwritten           (out)
+ * and the other arguments as in mhlmoe_rmsnorm_backward.  dweight and dbias are
+ * summed in a fixed order; zeros where T = 0.
+ */
+mhlmoe_status mhlmoe_layernorm_backward_workspace(int64_t T, int d_model,
+                                                  size_t *bytes);
+mhlmoe_status mhlmoe_layernorm_backward(const void *h, const float *weight,
+                                        const void *dy, const void *dsum,
+                                        int64_t T, int d_model, float eps,
+                                        mhlmoe_dtype dtype, void *dx,
+                                        float *dweight, float *dbias,
+                                        void *workspace, size_t workspace_bytes,
+                                        hipStream_t stream);
+
+/*
+ * Counts of the tokens that count:
+ *
+ *   counts[h][e] = #{(t, j): mask[t] != 0, idx[t][h][j] == e}
+ *
+ *   idx    [T][n_heads][top_k] int32; values outside [0, n_experts) are not
+ *          counted                                                     (in)
+ *   mask   [T] bytes or NULL (every token counts): 0 for a padded token (in)
+ *   counts [n_heads][n_experts] int32, overwritten; zeros where T = 0 (out)
+ * 1 <= n_heads, n_experts <= 1024, 1 <= top_k <= 32, T * top_k < 2^31.  No
+ * workspace.
+ */
+mhlmoe_status mhlmoe_expert_counts(const int32_t *idx, const uint8_t *mask,
+                                   int64_t T, int n_heads, int n_experts,
+                                   int top_k, int32_t *counts,
+                                   hipStream_t stream);
+
+/*
+ * The loss that balances a head's experts by gradient.  Over the n tokens of mask,
+ * with p_t = softmax_e(X[t,h,:] . W_router[h,e,:]) over all experts and
+ * f_e = counts[h][e] / sum_e' counts[h][e']:
+ *
+ *   loss[h] = n_experts sum_e f_e mean_t p_t(e)
+ *
+ * 1 for an even load or even probabilities, up to n_experts.  0 for a head whose
+ * counts are all zero; 1 where they are not and no token counts (n = 0).
+ *
+ *   X        [T][n_heads][d_head]         dtype                         (in)
+ *   W_router [n_heads][n_experts][d_head] float                         (in)
+ *   counts   [n_heads][n_experts] int32, e.g. mhlmoe_expert_counts', or these
+ *            summed over the batches or ranks of a step                 (in)
+ *   mask     [T] bytes or NULL, as above                                (in)
+ *   loss     [n_heads] float                                           (out)
+ *   stats    [T + 1][n_heads][2] float, for the gradient: log sum_e' exp of the
+ *            scores and sum_e p_t(e) (n_experts f_e - 1) of every token (zeros
+ *            where it does not count), and 1 / max(n, 1) and 0 as row T (out)
+ * What X holds at tokens that do not count is not read, so it may be anything.
+ * Scores are of fp32 accuracy (the paper's FP32 router) and never leave the chip.
+ * A token with a score that is not finite makes its head's loss NaN.
+ * d_head 64 or 128, 1 <= n_heads, n_experts <= 1024, T < 2^30.
+ */
+mhlmoe_status mhlmoe_balance_loss_workspace(int64_t T, int n_heads, int d_head,
+                                            int n_experts, size_t *bytes);
+mhlmoe_status mhlmoe_balance_loss(const void *X, const float *W_router,
+                                  const int32_t *counts, const uint8_t *mask,
+                                  int64_t T, int n_heads, int d_head,
+                                  int n_experts, mhlmoe_dtype dtype, float *loss,
+                                  float *stats, void *workspace,
+                                  size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Its gradient (the counts are no function of the router), added to gradients
+ * that are there already, such as mhlmoe_layer_backward's:
+ *
+ *   ds_t(e) = dloss[h] / n p_t(e) (n_experts f_e - 1 - stats[t][h][1])
+ *   dX[t,h,:] = dX_add[t,h,:] + sum_e ds_t(e) W_router[h,e,:]
+ *   dW_router[h,e,:] = dW_add[h,e,:] + sum_t ds_t(e) X[t,h,:]
+ *
+ *   dloss     [n_heads] float                                          (in)
+ *   dX_add    [T][n_heads][d_head] dtype or NULL (zeros); may be dX    (in)
+ *   dW_add    [n_heads][n_experts][d_head] float or NULL (zeros); may be
+ *             dW_router                                                (in)
+ *   dX        [T][n_heads][d_head] dtype; tokens that do not count get
+ *             dX_add; not X                                           (out)
+ *   dW_router [n_heads][n_experts][d_head] float; not W_router        (out)
+ * The other arguments are those of the mhlmoe_balance_loss call that wrote
+ * stats.  dX_add (dW_add) is added in fp32 before the one rounding of dX.
+ */
+mhlmoe_status mhlmoe_balance_loss_backward_workspace(int64_t T, int n_heads,
+                                                     int d_head, int n_experts,
+                                                     size_t *bytes);
+mhlmoe_status mhlmoe_balance_loss_backward(
+    const void *X, const float *W_router, const int32_t *counts,
+    const float *stats, const float *dloss, const uint8_t *mask,
+    const void *dX_add, const float *dW_add, int64_t T, int n_heads, int d_head,
+    int n_experts, mhlmoe_dtype dtype, void *dX, float *dW_router,
+    void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * One AdamW step over n_tensors tensors, per element in fp32:
+ *
+ *   g = grad_scale * grad
+ *   m = beta1 m + (1 - beta1) g
+ *   v = beta2 v + (1 - beta2) g^2
+ *   p = p - lr (m / (1 - beta1^step) / (sqrt(v / (1 - beta2^step)) + eps)
+ *               + weight_decay p)
+ *
+ * p is the fp32 master where there is one (param is then written as p rounded to
+ * bf16, and not read), else param itself.
+ */
+typedef struct mhlmoe_adamw_tensor {
+    void *param;   /* [n] param_dtype                               (in/out) */
+    float *master; /* [n], with a bf16 param only, or NULL          (in/out) */
+    const void *grad; /* [n] grad_dtype                                 (in) */
+    void *m;       /* [n] float, or with scales e4m3                (in/out) */
+    void *v;       /* [n] float; with scales sqrt(v) in e4m3        (in/out) */
+    float *m_scale; /* [ceil(n / 128)], or NULL (32-bit states) ... (in/out) */
+    float *v_scale; /* ... together with m_scale                    (in/out) */
+    int64_t n;
+    float weight_decay; /* finite and >= 0 */
+    uint32_t seed;      /* of the 8-bit states' rounding */
+    mhlmoe_dtype param_dtype, grad_dtype;
+} mhlmoe_adamw_tensor;
+
+typedef struct mhlmoe_adamw_step {
+    double lr;           /* finite and >= 0 */
+    double beta1, beta2; /* in [0, 1) */
+    double eps;          /* finite, > 0 as a float */
+    int64_t step;        /* from 1: the number of this step */
+    const float *grad_scale; /* one float on the device, or NULL (1) */
+} mhlmoe_adamw_step;
+
+/*
+ * The structs are read during the call and not kept.  m_scale and v_scale choose
+ * 8-bit states: m and sqrt(v) are held in blocks of 128 consecutive elements of
+ * the tensor (the last may be shorter) as described above for 8 bits, but each
+ * value is rounded up or down at random, up with the probability of the part
+ * below the step, and what is not zero of sqrt(v) does not become zero; a scale is
+ * the largest magnitude times 1 / 448 (at most an ulp from the quotient).  Zero
+ * states may be all zero bytes with any finite scales.  The random numbers are a
+ * hash of seed, step and the element's place: the same call gives the same bits.
+ * A value that is not finite makes its block of that state NaN.
+ *
+ * Memory that the step writes must not overlap any other memory of the step
+ * (MHLMOE_EINVAL); tensors may share a gradient.  lr and step are the call's: a
+ * captured call repeats the same step, and only grad_scale's value is read anew.
+ * No workspace; one kernel for every 48 tensors that are not empty.
+ */
+mhlmoe_status mhlmoe_adamw(const mhlmoe_adamw_tensor *tensors, int n_tensors,
+                           const mhlmoe_adamw_step *step, hipStream_t stream);
+
+/*
  * Per-kernel timing (a measurement aid, off by default).  While enabled, each
  * kernel the library launches is bracketed by two HIP events recorded on the
  * caller's stream, so the measured interval is that kernel's execution on
@@ -616,7 +789,9 @@ mhlmoe_status mhlmoe_latent_layer_scaled(
  * "count_scan", "scatter", "ffn", "combine", "bwd_dx", "bwd_combine",
  * "dw_plan", "bwd_dw", "router_dw", "route_bwd", "bias_update", "proj_in", "proj_out" and
  * "proj_bwd" (the projection GEMMs of the latent layer), "rmsnorm",
- * "rmsnorm_bwd", "rmsnorm_dw", "quantize" and "gemm_scaled".
+ * "rmsnorm_bwd", "rmsnorm_dw", "quantize" and "gemm_scaled"; "layernorm",
+ * "layernorm_bwd", "layernorm_dw", "expert_counts", "balance_weights",
+ * "balance_loss", "balance_sum", "balance_dx", "balance_dw" and "adamw".
  *
  * mhlmoe_timing_enable(on)   start (on != 0) or stop recording; records
  *                            already taken are kept.

@@ -28,6 +28,10 @@ __all__ = [
     "mhlmoe_rmsnorm", "mhlmoe_rmsnorm_backward", "mhlmoe_rmsnorm_backward_workspace",
     "mhlmoe_quantize", "mhlmoe_gemm_scaled", "mhlmoe_latent_layer_scaled",
     "mhlmoe_latent_layer_scaled_workspace",
+    "mhlmoe_layernorm", "mhlmoe_layernorm_backward", "mhlmoe_layernorm_backward_workspace",
+    "mhlmoe_expert_counts", "mhlmoe_balance_loss", "mhlmoe_balance_loss_workspace",
+    "mhlmoe_balance_loss_backward", "mhlmoe_balance_loss_backward_workspace",
+    "AdamWTensors", "mhlmoe_adamw",
     "mhlmoe_timing_enable", "mhlmoe_timing_query", "mhlmoe_timing_reset",
 ]
 
@@ -47,6 +51,17 @@ _P = ctypes.c_void_p
 _I64 = ctypes.c_int64
 _I = ctypes.c_int
 _SZ = ctypes.c_size_t
+
+
+class _AdamWTensor(ctypes.Structure):  # mhlmoe_adamw_tensor
+    _fields_ = [("param", _P), ("master", _P), ("grad", _P), ("m", _P), ("v", _P),
+                ("m_scale", _P), ("v_scale", _P), ("n", _I64), ("weight_decay", ctypes.c_float),
+                ("seed", ctypes.c_uint32), ("param_dtype", _I), ("grad_dtype", _I)]
+
+
+class _AdamWStep(ctypes.Structure):  # mhlmoe_adamw_step
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("step", _I64), ("grad_scale", _P)]
 
 
 class MhlmoeError(RuntimeError):
@@ -97,6 +112,17 @@ def _declare(lib):
                                                          + [ctypes.POINTER(_SZ)])
     lib.mhlmoe_latent_layer_scaled.argtypes = ([_P] * 3 + [F] + [_P] * 11 + [_I64] + [_I] * 7
                                                + [_P] * 9 + [_SZ, _P])
+    lib.mhlmoe_layernorm.argtypes = [_P] * 4 + [_I64, _I, F, _I] + [_P] * 5
+    lib.mhlmoe_layernorm_backward_workspace.argtypes = [_I64, _I, ctypes.POINTER(_SZ)]
+    lib.mhlmoe_layernorm_backward.argtypes = ([_P] * 4 + [_I64, _I, F, _I] + [_P] * 4
+                                              + [_SZ, _P])
+    lib.mhlmoe_expert_counts.argtypes = [_P, _P, _I64, _I, _I, _I, _P, _P]
+    lib.mhlmoe_balance_loss_workspace.argtypes = [_I64, _I, _I, _I, ctypes.POINTER(_SZ)]
+    lib.mhlmoe_balance_loss.argtypes = [_P] * 4 + [_I64] + [_I] * 4 + [_P] * 3 + [_SZ, _P]
+    lib.mhlmoe_balance_loss_backward_workspace.argtypes = [_I64, _I, _I, _I, ctypes.POINTER(_SZ)]
+    lib.mhlmoe_balance_loss_backward.argtypes = ([_P] * 8 + [_I64] + [_I] * 4 + [_P] * 3
+                                                 + [_SZ, _P])
+    lib.mhlmoe_adamw.argtypes = [_P, _I, _P, _P]
     lib.mhlmoe_timing_enable.argtypes = [_I]
     lib.mhlmoe_timing_query.argtypes = [ctypes.c_char_p, ctypes.POINTER(ctypes.c_double),
                                         ctypes.POINTER(_I64)]
@@ -107,7 +133,11 @@ def _declare(lib):
                  "mhlmoe_timing_query", "mhlmoe_timing_reset", "mhlmoe_rmsnorm",
                  "mhlmoe_rmsnorm_backward", "mhlmoe_rmsnorm_backward_workspace",
                  "mhlmoe_quantize", "mhlmoe_gemm_scaled", "mhlmoe_latent_layer_scaled",
-                 "mhlmoe_latent_layer_scaled_workspace"):
+                 "mhlmoe_latent_layer_scaled_workspace", "mhlmoe_layernorm",
+                 "mhlmoe_layernorm_backward", "mhlmoe_layernorm_backward_workspace",
+                 "mhlmoe_expert_counts", "mhlmoe_balance_loss", "mhlmoe_balance_loss_workspace",
+                 "mhlmoe_balance_loss_backward", "mhlmoe_balance_loss_backward_workspace",
+                 "mhlmoe_adamw"):
         getattr(lib, name).restype = _I
     return lib
 
@@ -793,6 +823,227 @@ def mhlmoe_latent_layer_scaled(x, norm_weight, eps, W_in, scale_in, W_router, bi
     if W_r is not None:
         res["R_lat"] = R_lat
     return res
+
+
+# What a training step has around the layer besides.  Devices and streams as above.
+
+def mhlmoe_layernorm(x, weight, eps, *, bias=None, residual=None, quantized=False, sum=None, y=None,
+                     q=None, scales=None, stream=None):
+    """h = x + residual and its layer norm.  x [T, d_model]; weight and bias
+    [d_model] float.  quantized: the norm in 8 bits (q e4m3 and scales per 128
+    columns) instead of y; pass y as well to have both.  Returns a dict with sum
+    (with residual), y, q and scales."""
+    T, d = shape = _rows_cols(x, "x")
+    _int(d, "d_model")
+    dt, dtype, dev, f32 = _dtype_code(x), x.dtype, x.get_device(), torch.float32
+    grid = (T, -(-d // 128))
+    if residual is not None:
+        sum = _new(sum, shape, dtype, x, stream)
+    if quantized:
+        q = _new(q, shape, E4M3, x, stream)
+        scales = _new(scales, grid, f32, x, stream)
+    else:
+        if q is not None or scales is not None:
+            raise ValueError("q and scales are outputs of quantized=True")
+        y = _new(y, shape, dtype, x, stream)
+    _launch(dev, stream, load_library().mhlmoe_layernorm, _at(x, "x", dtype, shape, dev),
+            _at(residual, "residual", dtype, shape, dev), _at(weight, "weight", f32, (d,), dev),
+            _at(bias, "bias", f32, (d,), dev), T, d, eps, dt, _at(sum, "sum", dtype, shape, dev),
+            _at(y, "y", dtype, shape, dev), _at(q, "q", E4M3, shape, dev),
+            _at(scales, "scales", f32, grid, dev))
+    res = {}
+    if sum is not None:
+        res["sum"] = sum
+    if y is not None:
+        res["y"] = y
+    if quantized:
+        res["q"], res["scales"] = q, scales
+    return res
+
+
+def mhlmoe_layernorm_backward_workspace(T: int, d_model: int) -> int:
+    """Workspace bytes of mhlmoe_layernorm_backward."""
+    out = _SZ(0)
+    _check(load_library().mhlmoe_layernorm_backward_workspace(T, _int(d_model, "d_model"),
+                                                              ctypes.byref(out)))
+    return out.value
+
+
+def mhlmoe_layernorm_backward(h, weight, eps, dy, *, dsum=None, dx=None, dweight=None, dbias=None,
+                              workspace=None, stream=None):
+    """Backward of mhlmoe_layernorm from h, the forward's sum (x where there was
+    no residual): returns (dx, dweight, dbias).  dsum: the gradient that reaches h
+    past the norm; dx is the gradient of x and of residual."""
+    T, d = shape = _rows_cols(h, "h")
+    _int(d, "d_model")
+    dt, dtype, dev, f32 = _dtype_code(h), h.dtype, h.get_device(), torch.float32
+    dx = _new(dx, shape, dtype, h, stream)
+    dweight = _new(dweight, (d,), f32, h, stream)
+    dbias = _new(dbias, (d,), f32, h, stream)
+    if workspace is None:
+        n = mhlmoe_layernorm_backward_workspace(T, d)
+        workspace = _new(None, (max(n, 256),), torch.uint8, h, stream)
+    _launch(dev, stream, load_library().mhlmoe_layernorm_backward, _at(h, "h", dtype, shape, dev),
+            _at(weight, "weight", f32, (d,), dev), _at(dy, "dy", dtype, shape, dev),
+            _at(dsum, "dsum", dtype, shape, dev), T, d, eps, dt, _at(dx, "dx", dtype, shape, dev),
+            _at(dweight, "dweight", f32, (d,), dev), _at(dbias, "dbias", f32, (d,), dev),
+            _at(workspace, "workspace", torch.uint8, (workspace.numel(),), dev), workspace.numel())
+    return dx, dweight, dbias
+
+
+def _mask(mask, T, device):
+    """Address of a mask [T] of truth values (None -> NULL)."""
+    return _at(mask, "mask", torch.bool, (T,), device)
+
+
+def _tokens_heads(t, name):
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dim() != 3:
+        raise ValueError(f"{name} must have 3 dimensions (got {t.dim()})")
+    return t.shape
+
+
+def mhlmoe_expert_counts(idx, n_experts, *, mask=None, counts=None, stream=None):
+    """How often each head's experts are in idx [T, Nh, k], over the tokens of mask
+    ([T] bool; None: all): returns counts [Nh, Ne] int32."""
+    T, Nh, k = shape = _tokens_heads(idx, "idx")
+    _int(n_experts, "n_experts")
+    dev, i32 = idx.get_device(), torch.int32
+    if n_experts < 1:
+        raise ValueError(f"n_experts must be >= 1 (got {n_experts})")
+    counts = _new(counts, (Nh, n_experts), i32, idx, stream)
+    _launch(dev, stream, load_library().mhlmoe_expert_counts, _at(idx, "idx", i32, shape, dev),
+            _mask(mask, T, dev), T, Nh, n_experts, k,
+            _at(counts, "counts", i32, (Nh, n_experts), dev))
+    return counts
+
+
+def mhlmoe_balance_loss_workspace(T: int, n_heads: int, d_head: int, n_experts: int) -> int:
+    """Workspace bytes of mhlmoe_balance_loss."""
+    out = _SZ(0)
+    _check(load_library().mhlmoe_balance_loss_workspace(
+        T, _int(n_heads, "n_heads"), _int(d_head, "d_head"), _int(n_experts, "n_experts"),
+        ctypes.byref(out)))
+    return out.value
+
+
+def mhlmoe_balance_loss(X, W_router, counts, *, mask=None, loss=None, stats=None, workspace=None,
+                        stream=None):
+    """The loss that balances the experts: X [T, Nh, dh], counts [Nh, Ne] as
+    mhlmoe_expert_counts gives them.  Returns (loss [Nh], stats [T + 1, Nh, 2]),
+    the latter for mhlmoe_balance_loss_backward."""
+    T, Nh, dh = shape = _tokens_heads(X, "X")
+    Ne = _rows_cols(counts, "counts")[1]
+    dt, dev, f32 = _dtype_code(X), X.get_device(), torch.float32
+    loss = _new(loss, (Nh,), f32, X, stream)
+    stats = _new(stats, (T + 1, Nh, 2), f32, X, stream)
+    if workspace is None:
+        n = mhlmoe_balance_loss_workspace(T, Nh, dh, Ne)
+        workspace = _new(None, (max(n, 256),), torch.uint8, X, stream)
+    _launch(dev, stream, load_library().mhlmoe_balance_loss, _at(X, "X", X.dtype, shape, dev),
+            _at(W_router, "W_router", f32, (Nh, Ne, dh), dev),
+            _at(counts, "counts", torch.int32, (Nh, Ne), dev), _mask(mask, T, dev), T, Nh, dh, Ne, dt,
+            _at(loss, "loss", f32, (Nh,), dev), _at(stats, "stats", f32, (T + 1, Nh, 2), dev),
+            _at(workspace, "workspace", torch.uint8, (workspace.numel(),), dev), workspace.numel())
+    return loss, stats
+
+
+def mhlmoe_balance_loss_backward_workspace(T: int, n_heads: int, d_head: int,
+                                           n_experts: int) -> int:
+    """Workspace bytes of mhlmoe_balance_loss_backward."""
+    out = _SZ(0)
+    _check(load_library().mhlmoe_balance_loss_backward_workspace(
+        T, _int(n_heads, "n_heads"), _int(d_head, "d_head"), _int(n_experts, "n_experts"),
+        ctypes.byref(out)))
+    return out.value
+
+
+def mhlmoe_balance_loss_backward(X, W_router, counts, stats, dloss, *, mask=None, dX_add=None,
+                                 dW_add=None, dX=None, dW_router=None, workspace=None, stream=None):
+    """Backward of mhlmoe_balance_loss from its stats and dloss [Nh]: returns (dX,
+    dW_router), added to the gradients dX_add and dW_add (the layer's, say), which
+    they may replace."""
+    T, Nh, dh = shape = _tokens_heads(X, "X")
+    Ne = _rows_cols(counts, "counts")[1]
+    dt, dtype, dev, f32 = _dtype_code(X), X.dtype, X.get_device(), torch.float32
+    dX = _new(dX, shape, dtype, X, stream)
+    dW_router = _new(dW_router, (Nh, Ne, dh), f32, X, stream)
+    if workspace is None:
+        n = mhlmoe_balance_loss_backward_workspace(T, Nh, dh, Ne)
+        workspace = _new(None, (max(n, 256),), torch.uint8, X, stream)
+    w = (Nh, Ne, dh)
+    _launch(dev, stream, load_library().mhlmoe_balance_loss_backward, _at(X, "X", dtype, shape, dev),
+            _at(W_router, "W_router", f32, w, dev),
+            _at(counts, "counts", torch.int32, (Nh, Ne), dev),
+            _at(stats, "stats", f32, (T + 1, Nh, 2), dev), _at(dloss, "dloss", f32, (Nh,), dev),
+            _mask(mask, T, dev), _at(dX_add, "dX_add", dtype, shape, dev),
+            _at(dW_add, "dW_add", f32, w, dev), T, Nh, dh, Ne, dt, _at(dX, "dX", dtype, shape, dev),
+            _at(dW_router, "dW_router", f32, w, dev),
+            _at(workspace, "workspace", torch.uint8, (workspace.numel(),), dev), workspace.numel())
+    return dX, dW_router
+
+
+class AdamWTensors:
+    """The tensors of mhlmoe_adamw, looked over once and kept for every step.
+
+    tensors: a list of dicts with the tensors param (float32 or bfloat16), grad
+    (float32 or bfloat16), m and v (float32, or float8_e4m3fn together with m_scale
+    and v_scale [ceil(n / 128)] float32, where v is the root of v), all of one
+    shape, and, with a bfloat16 param, master (float32) if there is one; and the
+    numbers weight_decay (0 if left out) and seed (of the 8-bit states' rounding;
+    the tensor's place in the list if left out)."""
+
+    _KEYS = {"param", "master", "grad", "m", "v", "m_scale", "v_scale", "weight_decay", "seed"}
+
+    def __init__(self, tensors):
+        self.tensors = [dict(t) for t in tensors]  # (keeps their memory)
+        self.array = (_AdamWTensor * max(len(self.tensors), 1))()
+        self.device = None
+        f32 = torch.float32
+        for i, (t, c) in enumerate(zip(self.tensors, self.array)):
+            unknown = set(t) - self._KEYS
+            if unknown:
+                raise ValueError(f"tensor {i}: unknown {', '.join(sorted(unknown))}")
+            for name in ("param", "grad", "m", "v"):
+                if not isinstance(t.get(name), torch.Tensor):
+                    raise TypeError(f"tensor {i}: {name} must be a torch.Tensor")
+            param, scaled = t["param"], t.get("m_scale") is not None
+            dev, shape, n = param.get_device(), param.shape, param.numel()
+            if self.device is None:
+                self.device = dev
+            state = E4M3 if scaled else f32
+            grid = (-(-n // 128),)
+            c.param_dtype, c.grad_dtype = _dtype_code(param), _dtype_code(t["grad"])
+            for name, dtype, dims in (
+                    ("param", param.dtype, shape), ("master", f32, shape),
+                    ("grad", t["grad"].dtype, shape), ("m", state, shape), ("v", state, shape),
+                    ("m_scale", f32, grid), ("v_scale", f32, grid)):
+                setattr(c, name, _at(t.get(name), f"tensor {i}: {name}", dtype, dims, self.device))
+            c.n = n
+            c.weight_decay = t.get("weight_decay", 0.0)
+            seed = t.get("seed", i)
+            if not 0 <= seed < 1 << 32:
+                raise ValueError(f"tensor {i}: seed must fit 32 bits (got {seed})")
+            c.seed = seed
+
+
+def mhlmoe_adamw(tensors, lr, *, beta1=0.9, beta2=0.999, eps=1e-8, step, grad_scale=None,
+                 stream=None):
+    """One AdamW step, the step-th from 1, over tensors: an AdamWTensors, or a list
+    of what it takes.  grad_scale: [1] float32 on the GPU that the gradients are
+    multiplied with (of clipping by their norm, say).  Everything is updated in
+    place; lr and step are numbers of the host, which a captured call repeats."""
+    if not isinstance(tensors, AdamWTensors):
+        tensors = AdamWTensors(tensors)
+    n = len(tensors.tensors)
+    if n == 0:
+        return
+    dev = tensors.device
+    s = _AdamWStep(lr, beta1, beta2, eps, step,
+                   _at(grad_scale, "grad_scale", torch.float32, (1,), dev))
+    _launch(dev, stream, load_library().mhlmoe_adamw, ctypes.addressof(tensors.array), n,
+            ctypes.addressof(s))
 
 
 def mhlmoe_timing_enable(on: bool = True) -> None:

@@ -39,9 +39,10 @@ COMMON_FLAGS = [
 SOURCES = ["api.cpp", "api_scaled.cpp", "route.hip", "route_64_bf16.hip", "route_64_f32.hip",
            "route_128_bf16.hip", "route_128_f32.hip", "bucket.hip", "experts.hip", "ffn_ws.hip",
            "backward.hip", "projection.cpp", "static_scratch.hip", "norm.hip", "quantize.hip",
-           "gemm_scaled.hip"]
+           "gemm_scaled.hip", "api_training.cpp", "layernorm.hip", "balance.hip", "adamw.hip"]
 HEADERS = ["api_internal.hpp", "device_common.hpp", "ffn_common.hpp", "launch.hpp",
-           "route_kernel.hpp", "scaled_common.hpp", "scaled_launch.hpp", "sort_networks.hpp"]
+           "norm_rows.hpp", "route_kernel.hpp", "scaled_common.hpp", "scaled_launch.hpp",
+           "sort_networks.hpp", "training_launch.hpp"]
 
 
 def _compile(src: str) -> str:

@@ -159,6 +159,61 @@ __device__ __forceinline__ void barrier_lds() {
   asm volatile("" ::: "memory");
 }
 
+// ds_read_b64_tr_b16: within each group of 16 lanes, lane i receives
+// element i % 4 of the 8-byte pieces addressed by lanes i / 4, 4 + i / 4,
+// 8 + i / 4 and 12 + i / 4 (so four rows of 4 columns, one row per
+// addressing lane quad, come back as one column per lane).
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ u32x2 lds_read_tr16(const uint8_t* p) {
+  const i16x4 r = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+      (__attribute__((address_space(3))) i16x4*)(p));
+  return __builtin_bit_cast(u32x2, r);
+}
+
+// Row swizzle of LDS matrices: 16-byte unit j of row r sits
+// at position swz_tr(j, r) = j ^ mask(r), a linear bijection of the row's
+// place in 16 bank rows.  It keeps three read forms free of bank conflicts:
+//  - 32 rows reading one logical unit with ds_read_b128 (the 32x32 operand
+//    form: 16 lanes served together hold 16 distinct rows mod 16);
+//  - 16 rows reading units u0 + lane / 16 (the 16x16x32 operand form): the
+//    LDS serves a ds_read_b128 in four cycles, to the lanes of equal bit 5
+//    and equal parity of bits 2-4, so for 256-byte rows the mask's images of
+//    row bits 2 and 3 must stay independent of rows 0-1's after adding the
+//    unit bit that lane bit 4 contributes;
+//  - four consecutive rows r0..r0+3 (r0 a multiple of 4) each reading one
+//    aligned 64-byte piece (ds_read_b64_tr_b16 fragments): their masks differ
+//    in the two bits above the piece (256-byte rows) or, two rows to a bank
+//    row, in the bit above it, so the 16 units land in 16 bank groups.
+template <int NJ>
+__device__ __forceinline__ int swz_tr(int j, int r) {
+  static_assert(NJ == 8 || NJ == 16, "rows of 128 or 256 bytes");
+  if constexpr (NJ == 16) {
+    const int m = r & 15;
+    return j ^ (((m & 3) << 2) | ((((m >> 2) ^ (m >> 3)) & 1) << 1) | ((m >> 3) & 1));
+  } else {
+    const int m = (r >> 1) & 7;
+    return j ^ (((m & 1) << 2) | (m >> 1));
+  }
+}
+
+// MFMA operand fragment (eight K of one M / N index per lane) from a matrix
+// in LDS whose rows are K: lane l takes column col0 + l % 32 and, for
+// elements 0-3 and 4-7, rows ra(g) .. ra(g) + 3 and rb(g) .. rb(g) + 3,
+// g = l / 32.  Lane j of each 16-lane group addresses row r + j / 4,
+// columns col + 4 (j % 4) .. + 3 (see lds_read_tr16).  addr(row, col) gives
+// the byte offset of an 8-byte aligned piece of four columns.
+template <typename Addr>
+__device__ __forceinline__ bf16x8 tr_fragment(const uint8_t* base, const Addr& addr, int ra0,
+                                              int ra1, int rb0, int rb1, int col0) {
+  const int lane = lane_id();
+  const int grp = lane >> 4, j = lane & 15;
+  const int col = col0 + 16 * (grp & 1) + 4 * (j & 3);
+  const int ra = (grp >> 1) ? ra1 : ra0, rb = (grp >> 1) ? rb1 : rb0;
+  const u32x2 lo = lds_read_tr16(base + addr(ra + (j >> 2), col));
+  const u32x2 hi = lds_read_tr16(base + addr(rb + (j >> 2), col));
+  return as_bf16x8(u32x4{lo[0], lo[1], hi[0], hi[1]});
+}
+
 // f(std::integral_constant<int, i>{}) for i = I, ..., N - 1, unrolled at
 // compile time (so f can use i in constant expressions).
 template <int I, int N, class F>

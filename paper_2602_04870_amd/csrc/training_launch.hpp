@@ -1,0 +1,110 @@
+// Launch interface of the training step's operators (api_training.cpp) to their
+// kernels: layer norm and its gradient, the experts' counts and balance loss and
+// its gradient, and AdamW.  As in launch.hpp, a launcher only enqueues work on its
+// stream and gets shapes that the ABI layer has validated.
+#pragma once
+
+#include "mhlmoe.h"
+#include "scaled_launch.hpp"
+
+namespace mhl {
+
+// As launch_rmsnorm; b may be NULL.
+hipError_t launch_layernorm(const void* x, const void* residual, const float* w, const float* b,
+                            int64_t T, int d, float eps, bool f32, void* sum, void* y, void* q,
+                            float* scales, hipStream_t s);
+
+// The gradient: dx, and dw and db as rmsnorm_bwd_parts partial rows of 2 d floats,
+// which launch_layernorm_dw adds in order (db may be NULL).  rows:
+// kLayernormRowFloats T floats where rmsnorm_bwd_wide, else unused.
+constexpr int kLayernormRowFloats = 5;
+hipError_t launch_layernorm_bwd(const void* h, const float* w, const void* dy, const void* dsum,
+                                int64_t T, int d, float eps, bool f32, void* dx, float* part,
+                                float* rows, hipStream_t s);
+hipError_t launch_layernorm_dw(const float* part, int64_t n, int d, float* dw, float* db,
+                               hipStream_t s);
+
+// AdamW.  A launch takes up to kAdamTensors tensors, as kernel arguments; its
+// workgroups take `chunk` elements (a multiple of kAdamChunk) of one tensor each,
+// those of tensor i from workgroup first[i] on (2^32 - 1 behind the last).
+constexpr int kAdamTensors = 48;
+constexpr int kAdamChunk = 2048;
+struct AdamTensor {
+  void* param;
+  float* master;  // NULL: the parameter itself
+  const void* grad;
+  void *m, *v;               // float, or e4m3 with scales
+  float *m_scale, *v_scale;  // NULL: 32-bit states
+  int64_t n;
+  float decay;   // lr * weight decay
+  uint32_t key;  // of the random numbers
+  uint8_t param_bf16, grad_bf16;
+};
+struct AdamStep {
+  float beta1, beta2, rest1, rest2;  // rest: 1 - beta
+  float rate, root;                  // lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
+  float eps;
+  const float* grad_scale;  // NULL: 1
+};
+struct AdamLaunch {
+  uint32_t first[kAdamTensors];
+  AdamStep step;
+  int64_t chunk;
+  AdamTensor t[kAdamTensors];
+};
+static_assert(sizeof(AdamLaunch) <= 4096, "kernel arguments");
+// The random numbers' key of (seed, step): a hash of two rounds.
+inline uint32_t adam_mix(uint32_t x) {
+  x = (x ^ (x >> 16)) * 0x6A09E667u;
+  x = (x ^ (x >> 15)) * 0xBB67AE85u;
+  return x ^ (x >> 16);
+}
+inline uint32_t adam_key(uint32_t seed, int64_t step) {
+  return adam_mix(adam_mix(seed) + (uint32_t)step);
+}
+hipError_t launch_adamw(const AdamLaunch& a, unsigned workgroups, hipStream_t s);
+
+// How often each head's experts are in idx [T][Nh][k], over the tokens of mask
+// (NULL: all).
+hipError_t launch_expert_counts(const int32_t* idx, const uint8_t* mask, int64_t T, int Nh, int Ne,
+                                int k, int32_t* counts, hipStream_t s);
+
+// The balance loss and its gradient.  The router's weights are first laid out as
+// operands (balance_weight_bytes), the gradient's dW comes as balance_splits
+// partial results of Nh x (Ne rounded up to 32) x dh floats that
+// launch_balance_dw_sum adds in order.
+inline int balance_blocks(int Ne) { return (int)ceil_div(Ne, 32); }
+inline size_t balance_weight_bytes(int Nh, int dh, int Ne, bool backward) {
+  // three pieces of bf16 for the scores, three more transposed for dX
+  return (size_t)Nh * balance_blocks(Ne) * 32 * dh * 2 * (backward ? 6 : 3);
+}
+constexpr int kBalanceTokens = 128;  // per workgroup of the loss and of dX
+inline int64_t balance_token_blocks(int64_t T) { return ceil_div(T, kBalanceTokens); }
+// Wavefronts (a block of 32 experts each) per workgroup of dW, and the chunks that
+// the tokens are cut into, so that there are about 1024 workgroups.
+inline int balance_dw_waves(int Ne) { return balance_blocks(Ne) < 4 ? balance_blocks(Ne) : 4; }
+inline int64_t balance_splits(int64_t T, int Nh, int Ne) {
+  const int64_t groups = Nh * ceil_div(balance_blocks(Ne), balance_dw_waves(Ne));
+  const int64_t want = ceil_div(1024, groups), most = ceil_div(T, 64);
+  return want < most ? want : most;
+}
+hipError_t launch_balance_weights(const float* W, int Nh, int dh, int Ne, bool backward, void* out,
+                                  hipStream_t s);
+hipError_t launch_balance_loss(const void* X, const void* weights, const int32_t* counts,
+                               const uint8_t* mask, int64_t T, int Nh, int dh, int Ne, bool f32,
+                               float* stats, double* part, hipStream_t s);
+hipError_t launch_balance_loss_sum(const double* part, const int32_t* counts, const uint8_t* mask,
+                                   int64_t T, int Nh, int Ne, float* loss, float* stats,
+                                   hipStream_t s);
+hipError_t launch_balance_dx(const void* X, const void* weights, const int32_t* counts,
+                             const float* stats, const float* dloss, const uint8_t* mask,
+                             const void* dX_add, int64_t T, int Nh, int dh, int Ne, bool f32,
+                             void* dX, hipStream_t s);
+hipError_t launch_balance_dw(const void* X, const void* weights, const int32_t* counts,
+                             const float* stats, const uint8_t* mask, int64_t T, int Nh, int dh,
+                             int Ne, bool f32, float* part, hipStream_t s);
+hipError_t launch_balance_dw_sum(const float* part, const float* stats, const float* dloss,
+                                 const float* dW_add, int64_t T, int Nh, int dh, int Ne, float* dW,
+                                 hipStream_t s);
+
+}  // namespace mhl
