@@ -689,7 +689,7 @@ mhlmoe_status mhlmoe_expert_counts(const int32_t *idx, const uint8_t *mask,
  * What X holds at tokens that do not count is not read, so it may be anything.
  * Scores are of fp32 accuracy (the paper's FP32 router) and never leave the chip.
  * A token with a score that is not finite makes its head's loss NaN.
- * d_head 64 or 128, 1 <= n_heads, n_experts <= 1024, T < 2^30.
+ * d_head 64 or 128, 1 <= n_heads, n_experts <= 1024, (T + 128) * n_heads < 2^31.
  */
 mhlmoe_status mhlmoe_balance_loss_workspace(int64_t T, int n_heads, int d_head,
                                             int n_experts, size_t *bytes);

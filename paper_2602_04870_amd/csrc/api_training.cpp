@@ -63,7 +63,9 @@ mhlmoe_status check_heads(int64_t T, int n_heads, int n_experts) {
 
 mhlmoe_status check_balance(int64_t T, int n_heads, int d_head, int n_experts) {
   MHL_TRY(check_heads(T, n_heads, n_experts));
-  if (T >= int64_t(1) << 30) return fail(MHLMOE_EUNSUPPORTED, "T must be < 2^30");
+  // (also the launches' limit: fewer than 2^24 workgroups of 128 rows)
+  if (T > ((int64_t(1) << 31) - 1) / n_heads - 128)
+    return fail(MHLMOE_EUNSUPPORTED, "(T + 128) * n_heads must be < 2^31");
   if (d_head != 64 && d_head != 128)
     return fail(MHLMOE_EUNSUPPORTED, "d_head %d not in {64, 128}", d_head);
   return MHLMOE_OK;
@@ -75,8 +77,8 @@ struct BalanceLayout {
 BalanceLayout balance_layout(int64_t T, int n_heads, int d_head, int n_experts, bool backward) {
   BalanceLayout L;
   size_t cur = 0;
-  L.weights = bump(cur, mhl::balance_weight_bytes(n_heads, d_head, n_experts, backward));
-  L.part = bump(cur, backward ? sizeof(float) * (size_t)mhl::balance_splits(T, n_heads, n_experts) *
+  L.weights = bump(cur, mhl::balance_weight_bytes(n_heads, d_head, n_experts));
+  L.part = bump(cur, backward ? sizeof(float) * (size_t)mhl::balance_parts(T, n_heads, n_experts) *
                                     n_heads * mhl::balance_blocks(n_experts) * 32 * d_head
                               : sizeof(double) * (size_t)n_heads * mhl::balance_token_blocks(T));
   L.total = cur;
@@ -267,11 +269,11 @@ mhlmoe_status mhlmoe_balance_loss(const void* X, const float* W_router, const in
   double* part = at<double>(workspace, L.part);
   if (T > 0) {
     MHL_TRY(run_kernel("balance_weights", stream, [&] {
-      return mhl::launch_balance_weights(W_router, n_heads, d_head, n_experts, false, weights,
-                                         stream);
+      return mhl::launch_balance_weights(W_router, counts, n_heads, d_head, n_experts,
+                                         dtype == MHLMOE_F32, false, weights, stream);
     }));
     MHL_TRY(run_kernel("balance_loss", stream, [&] {
-      return mhl::launch_balance_loss(X, weights, counts, mask, T, n_heads, d_head, n_experts,
+      return mhl::launch_balance_loss(X, weights, mask, T, n_heads, d_head, n_experts,
                                       dtype == MHLMOE_F32, stats, part, stream);
     }));
   }
@@ -317,16 +319,16 @@ mhlmoe_status mhlmoe_balance_loss_backward(
   const bool f32 = dtype == MHLMOE_F32;
   if (T > 0) {
     MHL_TRY(run_kernel("balance_weights", stream, [&] {
-      return mhl::launch_balance_weights(W_router, n_heads, d_head, n_experts, true, weights,
-                                         stream);
+      return mhl::launch_balance_weights(W_router, counts, n_heads, d_head, n_experts, f32, true,
+                                         weights, stream);
     }));
     MHL_TRY(run_kernel("balance_dx", stream, [&] {
-      return mhl::launch_balance_dx(X, weights, counts, stats, dloss, mask, dX_add, T, n_heads,
-                                    d_head, n_experts, f32, dX, stream);
+      return mhl::launch_balance_dx(X, weights, stats, dloss, mask, dX_add, T, n_heads, d_head,
+                                    n_experts, f32, dX, stream);
     }));
     MHL_TRY(run_kernel("balance_dw", stream, [&] {
-      return mhl::launch_balance_dw(X, weights, counts, stats, mask, T, n_heads, d_head, n_experts,
-                                    f32, part, stream);
+      return mhl::launch_balance_dw(X, weights, stats, mask, T, n_heads, d_head, n_experts, f32,
+                                    part, stream);
     }));
   }
   return run_kernel("balance_sum", stream, [&] {

@@ -14,11 +14,15 @@
 // token; the gradient computes the scores again, once token by token for dX and
 // once expert by expert for dW (a fixed order, no atomics).
 //
-// All products go to the bf16 matrix instructions at fp32 accuracy: an fp32 value
-// is three bf16 ones, w = w0 + w1 + w2 exactly (each the nearest to what is left),
-// and products of pieces w_i x_j with i + j <= 2 are kept: 3 with a bf16 x (exact),
-// 6 with an fp32 x (2^-24 of the product left out); the fp32 matrix instructions
-// take 2.7 times as long as the 6.
+// All products go to the fp16 matrix instructions at fp32 accuracy.  A value scaled
+// by a power of two is two fp16 ones, w = w0 + w1, each the nearest to what is left:
+// off by 2^-23 of itself, or by 2^-39 of the largest of those that share the scale
+// (a token's row of X, 32 experts' rows of W, an expert's ds so far).  A bf16 x is one
+// fp16 value, exactly (down to 2^-31 of its row's largest).  Products of pieces kept:
+// w0 x, w1 x with a bf16 x; w0 x0, w0 x1, w1 x0 with an fp32 x (up to 2^-22 of the
+// product left out).  So a score takes 2 or 3 passes; in three bf16 pieces each it took 3 or 6
+// (gradient at 65536 tokens x 8 heads x 1024 experts: 1855 us so), and one pass of the
+// fp32 matrix instructions lasts as long as 16.
 
 #include "device_common.hpp"
 #include "training_launch.hpp"
@@ -64,7 +68,15 @@ __global__ __launch_bounds__(kCountThreads) void expert_counts_kernel(
 // ---------------------------------------------------------------------------
 // Operands
 // ---------------------------------------------------------------------------
-// Eight values as N bf16 pieces, each the nearest to what the ones before left.
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+
+__device__ __forceinline__ f32x16 mfma32_f16(u32x4 a, u32x4 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a),
+                                                __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+// Eight values as N fp16 pieces, each the nearest to what the ones before left.
 template <int N>
 __device__ __forceinline__ void split8(const float (&f)[8], u32x4 (&out)[N]) {
   float r[8];
@@ -74,102 +86,196 @@ __device__ __forceinline__ void split8(const float (&f)[8], u32x4 (&out)[N]) {
   for (int p = 0; p < N; ++p)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const uint32_t w = pack_bf16x2(r[2 * i], r[2 * i + 1]);
-      out[p][i] = w;
-      r[2 * i] -= bf16_bits_to_f32(w & 0xFFFFu);
-      r[2 * i + 1] -= __uint_as_float(w & 0xFFFF0000u);
+      const f16x2 h = __builtin_convertvector((f32x2{r[2 * i], r[2 * i + 1]}), f16x2);
+      out[p][i] = __builtin_bit_cast(uint32_t, h);
+      if (p + 1 < N) {
+        r[2 * i] -= (float)h[0];
+        r[2 * i + 1] -= (float)h[1];
+      }
     }
 }
 
-// Bytes of a block of 32 experts as operands: fragments of 64 lanes x 16 bytes.
+// The power of two that takes values of magnitude up to `most` (its bits) below 2^15,
+// and its inverse (a row below 2^-112 is not lifted further).
+struct Pow2 {
+  float up, down;
+};
+__device__ __forceinline__ Pow2 pow2_below_2_15(uint32_t most) {
+  uint32_t e = most >> 23;
+  e = e < 15u ? 15u : e > 254u ? 254u : e;
+  return Pow2{__uint_as_float((268u - e) << 23), __uint_as_float((e - 14u) << 23)};
+}
+__device__ __forceinline__ float log2_of(float power) {  // exactly
+  return (float)((int)(__float_as_uint(power) >> 23) - 127);
+}
+__device__ __forceinline__ uint32_t bits_abs(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+__device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
+
+// A block of 32 experts as operands: fragments of 64 lanes x 16 bytes.
 //   scores: piece, k-step s: lane holds expert lane % 32, d = 16 s + 8 (lane / 32) + j
 //   dX (transposed): piece, tile dt of 32 d, k-step s: lane holds d = 32 dt + lane % 32,
 //       experts 16 s + 8 (j / 4) + 4 (lane / 32) + j % 4, in the order in which a score
 //       tile's rows lie in its registers
+// BACK: pieces of the latter (1 for a bf16 dX, 2 for an fp32 one, 0 for none).
 template <int DH>
-constexpr int kScoreFrags = 3 * DH / 16;
+constexpr int kScoreFrags = 2 * DH / 16;
 template <int DH>
-constexpr int kBackFrags = 3 * (DH / 32) * 2;
+constexpr int kBackFrags = (DH / 32) * 2;  // per piece
+template <int DH, int BACK>
+constexpr int kFrags = kScoreFrags<DH> + BACK * kBackFrags<DH>;
 
-template <int DH, bool BWD>
-__global__ __launch_bounds__(256) void balance_weights_kernel(const float* __restrict__ W, int Ne,
-                                                              u32x4* __restrict__ out) {
-  constexpr int kFrags = kScoreFrags<DH> + (BWD ? kBackFrags<DH> : 0);
-  const int e0 = blockIdx.x * 32;
-  const float* w = W + (int64_t)blockIdx.y * Ne * DH;
-  u32x4* o = out + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kFrags * 64;
-  for (int i = threadIdx.x; i < DH / 16 * 64; i += 256) {
-    const int s = i >> 6, lane = i & 63, e = e0 + (lane & 31);
-    float f[8];
-    u32x4 p[3];
+// What lies behind the operands in the workspace, per head: f'_e of the experts
+// (zeros up to the next multiple of 32), the blocks' powers of two (down) and the
+// exponent F that takes ds below 2^14.
+struct HeadInfo {
+  float f[kMaxExperts];
+  float down[kMaxExperts / 32];
+  float F;
+  float pad[31];
+};
+static_assert(sizeof(HeadInfo) == kBalanceHeadBytes, "workspace");
+
+// Grid (blocks of 32 experts, heads).
+template <int DH, int BACK>
+__global__ __launch_bounds__(256) void balance_weights_kernel(const float* __restrict__ W,
+                                                              const int32_t* __restrict__ counts,
+                                                              int Ne, u32x4* __restrict__ out,
+                                                              HeadInfo* __restrict__ info) {
+  constexpr int kStride = DH + 1;
+  __shared__ float w[32 * kStride];
+  __shared__ long long totals[4];
+  __shared__ uint32_t tops[3][4];
+  const int e0 = blockIdx.x * 32, h = blockIdx.y, lane = lane_id(), wave = threadIdx.x >> 6;
+  const float* src = W + ((int64_t)h * Ne + e0) * DH;
+  const int here = Ne - e0 < 32 ? Ne - e0 : 32;
+  uint32_t top = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      f[j] = e < Ne ? w[(int64_t)e * DH + 16 * s + 8 * (lane >> 5) + j] : 0.0f;
-    split8(f, p);
+  for (int i = 0; i < 32 * DH; i += 1024) {
+    const int at = i + threadIdx.x * 4;
+    f32x4 v{0, 0, 0, 0};
+    if (at < here * DH) v = *reinterpret_cast<const f32x4*>(src + at);
 #pragma unroll
-    for (int q = 0; q < 3; ++q) o[(q * (DH / 16) + s) * 64 + lane] = p[q];
-  }
-  if (!BWD) return;
-  o += kScoreFrags<DH> * 64;
-  for (int i = threadIdx.x; i < DH / 32 * 2 * 64; i += 256) {
-    const int dt = i >> 7, s = (i >> 6) & 1, lane = i & 63;
-    float f[8];
-    u32x4 p[3];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int e = e0 + 16 * s + 8 * (j >> 2) + 4 * (lane >> 5) + (j & 3);
-      f[j] = e < Ne ? w[(int64_t)e * DH + 32 * dt + (lane & 31)] : 0.0f;
+    for (int k = 0; k < 4; ++k) {
+      w[at / DH * kStride + at % DH + k] = v[k];
+      top = umax(top, bits_abs(v[k]));
     }
-    split8(f, p);
-#pragma unroll
-    for (int q = 0; q < 3; ++q) o[(q * (DH / 32) * 2 + dt * 2 + s) * 64 + lane] = p[q];
   }
-}
-
-// f'_e of the head's experts (zeros up to the next multiple of 32) in LDS: exact
-// whole numbers, one division.
-template <int THREADS>
-__device__ __forceinline__ void load_excess(const int32_t* __restrict__ counts, int Ne, float* f,
-                                            long long* lds) {
-  long long part = 0;
-  for (int e = threadIdx.x; e < Ne; e += THREADS) part += counts[e];
-#pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) part += __shfl_xor(part, d, kWave);
-  if (lane_id() == 0) lds[threadIdx.x >> 6] = part;
-  __syncthreads();
   long long total = 0;
+  uint32_t most = 0, least = 0xFFFFFFFFu;
+  for (int e = threadIdx.x; e < Ne; e += 256) {
+    const uint32_t c = (uint32_t)counts[(int64_t)h * Ne + e];
+    total += (int32_t)c;
+    most = umax(most, c);
+    least = c < least ? c : least;
+  }
+  least = ~least;
 #pragma unroll
-  for (int w = 0; w < THREADS / kWave; ++w) total += lds[w];
-  const int padded = (Ne + 31) & ~31;
-  for (int e = threadIdx.x; e < padded; e += THREADS)
-    f[e] = e < Ne && total > 0
-               ? (float)((double)((long long)counts[e] * Ne - total) / (double)total)
-               : 0.0f;
+  for (int d = 1; d < kWave; d <<= 1) {
+    total += __shfl_xor(total, d, kWave);
+    top = umax(top, __shfl_xor(top, d, kWave));
+    most = umax(most, __shfl_xor(most, d, kWave));
+    least = umax(least, __shfl_xor(least, d, kWave));
+  }
+  if (lane == 0) {
+    totals[wave] = total;
+    tops[0][wave] = top;
+    tops[1][wave] = most;
+    tops[2][wave] = least;
+  }
   __syncthreads();
-}
-
-// One lane's operand of X: token row, d = 16 s + 8 g + j, as NX pieces.
-template <int DH, bool F32>
-struct XOperand {
-  static constexpr int NX = F32 ? 3 : 1;
-  u32x4 x[NX][DH / 16];
-  __device__ __forceinline__ void load(const void* X, int64_t row, bool ok, int g) {
-#pragma unroll
-    for (int s = 0; s < DH / 16; ++s) {
-      const int64_t at = row * DH + 16 * s + 8 * g;
-      if (F32) {
-        const f32x4* p = reinterpret_cast<const f32x4*>(static_cast<const float*>(X) + at);
-        const f32x4 a = ok ? p[0] : f32x4{0, 0, 0, 0}, b = ok ? p[1] : f32x4{0, 0, 0, 0};
-        const float f[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-        u32x4 o[NX];
-        split8(f, o);
-#pragma unroll
-        for (int p2 = 0; p2 < NX; ++p2) x[p2][s] = o[p2];
-      } else {
-        x[0][s] = ok ? *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(X) + at)
-                     : u32x4{0, 0, 0, 0};
+  total = totals[0] + totals[1] + totals[2] + totals[3];
+  auto over_waves = [&](int k) {
+    return umax(umax(tops[k][0], tops[k][1]), umax(tops[k][2], tops[k][3]));
+  };
+  const Pow2 scale = pow2_below_2_15(over_waves(0));
+  if (threadIdx.x < 32) {
+    // exact whole numbers, one division
+    const int e = e0 + threadIdx.x;
+    float f = 0.0f;
+    if (e < Ne && total > 0)
+      f = (float)((double)((long long)counts[(int64_t)h * Ne + e] * Ne - total) / (double)total);
+    info[h].f[e] = f;
+    if (threadIdx.x == 0) {
+      info[h].down[blockIdx.x] = scale.down;
+      if (blockIdx.x == 0) {
+        // |f' - u| <= max f' - min f' = R: p (f' - u) 2^F < 2^14
+        const double R = total > 0 ? (double)((long long)(over_waves(1) - ~over_waves(2)) * Ne) /
+                                         (double)total
+                                   : 0.0;
+        info[h].F = R > 0.0 ? (float)(13 - ilogb(R)) : 0.0f;
       }
     }
+  }
+  u32x4* o = out + ((int64_t)h * gridDim.x + blockIdx.x) * kFrags<DH, BACK> * 64;
+  for (int i = threadIdx.x; i < DH / 16 * 64; i += 256) {
+    const int s = i >> 6, l = i & 63;
+    float f[8];
+    u32x4 p[2];
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      f[j] = w[(l & 31) * kStride + 16 * s + 8 * (l >> 5) + j] * scale.up;
+    split8(f, p);
+#pragma unroll
+    for (int q = 0; q < 2; ++q) o[(q * (DH / 16) + s) * 64 + l] = p[q];
+  }
+  if constexpr (BACK > 0) {
+    o += kScoreFrags<DH> * 64;
+    for (int i = threadIdx.x; i < DH / 32 * 2 * 64; i += 256) {
+      const int dt = i >> 7, s = (i >> 6) & 1, l = i & 63;
+      float f[8];
+      u32x4 p[BACK];
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        f[j] = w[(16 * s + 8 * (j >> 2) + 4 * (l >> 5) + (j & 3)) * kStride + 32 * dt + (l & 31)] *
+               scale.up;
+      split8(f, p);
+#pragma unroll
+      for (int q = 0; q < BACK; ++q) o[(q * kBackFrags<DH> + dt * 2 + s) * 64 + l] = p[q];
+    }
+  }
+}
+
+// One lane's operand of X: token row, d = 16 s + 8 g + j, as NX pieces of x up, the
+// row's power of two.
+template <int DH, bool F32>
+struct XOperand {
+  static constexpr int NX = F32 ? 2 : 1;
+  u32x4 x[NX][DH / 16];
+  float down;
+  __device__ __forceinline__ void load(const void* X, int64_t row, bool ok, int g) {
+    u32x4 raw[DH / 16][F32 ? 2 : 1];
+    const uint8_t* p = static_cast<const uint8_t*>(X) + (row * DH + 8 * g) * (F32 ? 4 : 2);
+#pragma unroll
+    for (int s = 0; s < DH / 16; ++s)
+#pragma unroll
+      for (int i = 0; i < (F32 ? 2 : 1); ++i)
+        raw[s][i] = ok ? *reinterpret_cast<const u32x4*>(p + 16 * s * (F32 ? 4 : 2) + 16 * i)
+                       : u32x4{0, 0, 0, 0};
+    uint32_t top = 0;
+#pragma unroll
+    for (int s = 0; s < DH / 16; ++s)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = umax(top, bits_abs(value(raw[s], i)));
+    top = umax(top, __shfl_xor(top, 32, kWave));
+    const Pow2 scale = pow2_below_2_15(top);
+    down = scale.down;
+#pragma unroll
+    for (int s = 0; s < DH / 16; ++s) {
+      float f[8];
+      u32x4 o[NX];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] = value(raw[s], i) * scale.up;
+      split8(f, o);
+#pragma unroll
+      for (int q = 0; q < NX; ++q) x[q][s] = o[q];
+    }
+  }
+  // element i of eight as they lie in memory
+  template <int N>
+  static __device__ __forceinline__ float value(const u32x4 (&raw)[N], int i) {
+    if constexpr (F32) return __uint_as_float(raw[i >> 2][i & 3]);
+    const uint32_t w = raw[0][i >> 1];
+    return __uint_as_float((i & 1) ? w & 0xFFFF0000u : w << 16);
   }
 };
 
@@ -182,62 +288,68 @@ __device__ __forceinline__ f32x16 score_start(int e0, int Ne, int g) {
   return z;
 }
 
-// Scores of 32 experts (rows) x 32 tokens (lanes), small products first.
+// Scores of 32 experts (rows) x 32 tokens (lanes), times both powers of two, small
+// products first.
 template <int DH, bool F32>
 __device__ __forceinline__ f32x16 score_tile(const u32x4* w, const XOperand<DH, F32>& x,
                                              f32x16 z) {
   const int lane = lane_id();
 #pragma unroll
-  for (int q = 2; q >= 0; --q)
+  for (int q = 1; q >= 0; --q)
 #pragma unroll
     for (int s = 0; s < DH / 16; ++s) {
-      const bf16x8 a = as_bf16x8(w[(q * (DH / 16) + s) * 64 + lane]);
+      const u32x4 a = w[(q * (DH / 16) + s) * 64 + lane];
 #pragma unroll
       for (int p = XOperand<DH, F32>::NX - 1; p >= 0; --p)
-        if (p + q <= 2) z = mfma32_bf16(a, as_bf16x8(x.x[p][s]), z);
+        if (p + q <= 1) z = mfma32_f16(a, x.x[p][s], z);
     }
   return z;
 }
 
+// Fragments [0, N) of a block to LDS, dealt to the wavefronts, by DMA that the
+// compiler does not track: barrier_vm<0> before they are read.
 template <int N>
-__device__ __forceinline__ void copy_to_lds(const u32x4* __restrict__ src, u32x4* dst) {
+__device__ __forceinline__ void fetch_frags(u32x4 rsrc, uint32_t block_bytes, int b, u32x4* lds) {
+  const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const uint32_t voff = lane_id() * 16;
 #pragma unroll
-  for (int i = 0; i < N; i += kTokenWaves * kWave)
-    if (N % (kTokenWaves * kWave) == 0 || i + (int)threadIdx.x < N)
-      dst[i + threadIdx.x] = src[i + threadIdx.x];
+  for (int i = 0; i < N; i += kTokenWaves)
+    dma_lds16(rsrc, lds + (i + wave) * 64, voff, (uint32_t)b * block_bytes + (i + wave) * 1024u);
 }
 
 // ---------------------------------------------------------------------------
-// The loss: 32 tokens of head blockIdx.y per wavefront, over all experts.
+// The loss: 32 tokens of a head per wavefront, over all experts, whose operands go
+// through LDS in two buffers.  A workgroup's head is blockIdx.x % Nh: workgroups go
+// round the dies, so with 8 heads a die has one head's weights in its L2.
 // ---------------------------------------------------------------------------
 template <int DH, bool F32>
 __global__ __launch_bounds__(kTokenWaves* kWave) void balance_loss_kernel(
     const void* __restrict__ X, const u32x4* __restrict__ weights,
-    const int32_t* __restrict__ counts, const uint8_t* __restrict__ mask, int64_t T, int Nh, int Ne,
+    const HeadInfo* __restrict__ info, const uint8_t* __restrict__ mask, int64_t T, int Nh, int Ne,
     float2* __restrict__ stats, double* __restrict__ part) {
-  constexpr int kFrags = kScoreFrags<DH>;
-  __shared__ u32x4 w[kFrags * 64];
+  constexpr int kN = kFrags<DH, 0>;
+  __shared__ u32x4 w[2][kN * 64];
   __shared__ __align__(16) float fex[kMaxExperts];
-  __shared__ long long sums[kTokenWaves];
   __shared__ double loss[kTokenWaves];
-  const int h = blockIdx.y, lane = lane_id(), g = lane >> 5, wave = threadIdx.x >> 6;
-  const int64_t t = (int64_t)blockIdx.x * kBalanceTokens + wave * 32 + (lane & 31);
+  const int h = blockIdx.x % Nh, lane = lane_id(), g = lane >> 5, wave = threadIdx.x >> 6;
+  const int64_t tb = blockIdx.x / Nh, t = tb * kBalanceTokens + wave * 32 + (lane & 31);
   const bool ok = t < T && (!mask || mask[t < T ? t : 0]);
-  load_excess<kTokenWaves * kWave>(counts + (int64_t)h * Ne, Ne, fex, sums);
+  const int nb = (Ne + 31) / 32;
+  const u32x4 rsrc = buffer_words(weights + (int64_t)h * nb * kN * 64, (uint32_t)nb * kN * 1024u);
+  fetch_frags<kN>(rsrc, kN * 1024u, 0, w[0]);
+  for (int e = threadIdx.x; e < nb * 32; e += kTokenWaves * kWave) fex[e] = info[h].f[e];
   XOperand<DH, F32> x;
   x.load(X, t * Nh + h, ok, g);
-  const int nb = (Ne + 31) / 32;
-  const u32x4* src = weights + (int64_t)h * nb * kFrags * 64;
   float M = -INFINITY, l = 0.0f, u = 0.0f;  // maximum (times log2 e), sum, weighted sum
   for (int b = 0; b < nb; ++b) {
-    __syncthreads();
-    copy_to_lds<kFrags * 64>(src + (int64_t)b * kFrags * 64, w);
-    __syncthreads();
-    const f32x16 z = score_tile<DH, F32>(w, x, score_start(32 * b, Ne, g));
+    const float m = x.down * info[h].down[b] * kLog2e;
+    barrier_vm<0>();
+    if (b + 1 < nb) fetch_frags<kN>(rsrc, kN * 1024u, b + 1, w[(b + 1) & 1]);
+    const f32x16 z = score_tile<DH, F32>(w[b & 1], x, score_start(32 * b, Ne, g));
     float top = z[0];
 #pragma unroll
     for (int v = 1; v < 16; ++v) top = fmaxf(top, z[v]);
-    const float Mn = fmaxf(M, top * kLog2e);
+    const float Mn = fmaxf(M, top * m);
     const float ref = Mn == -INFINITY ? 0.0f : Mn;
     const float old = __builtin_amdgcn_exp2f(M - ref);
     l *= old;
@@ -248,7 +360,7 @@ __global__ __launch_bounds__(kTokenWaves* kWave) void balance_loss_kernel(
       const f32x4 f = *reinterpret_cast<const f32x4*>(&fex[32 * b + 8 * q + 4 * g]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(z[4 * q + i], kLog2e, -ref));
+        const float p = __builtin_amdgcn_exp2f(fmaf(z[4 * q + i], m, -ref));
         l += p;
         u = fmaf(p, f[i], u);
       }
@@ -272,7 +384,7 @@ __global__ __launch_bounds__(kTokenWaves* kWave) void balance_loss_kernel(
   if (threadIdx.x == 0) {
 #pragma unroll
     for (int i = 1; i < kTokenWaves; ++i) sum += loss[i];
-    part[(int64_t)h * gridDim.x + blockIdx.x] = sum;
+    part[h * balance_token_blocks(T) + tb] = sum;
   }
 }
 
@@ -288,8 +400,22 @@ __global__ __launch_bounds__(256) void balance_loss_sum_kernel(
   double s = 0.0;
   for (int64_t i = threadIdx.x; i < blocks; i += 256) s += part[h * blocks + i];
   long long n = 0, c = 0;
-  if (mask)
-    for (int64_t t = threadIdx.x; t < T; t += 256) n += mask[t] != 0;
+  if (mask) {
+    // 16 bytes at once: the number that is not zero, by folding each to its low bit
+#pragma unroll 4
+    for (int64_t i = threadIdx.x; i < T / 16; i += 256) {
+      const u32x4 m = reinterpret_cast<const u32x4*>(mask)[i];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        uint32_t v = m[k];
+        v |= v >> 4;
+        v |= v >> 2;
+        v |= v >> 1;  // (bits from the next byte reach only the upper seven)
+        n += __popc(v & 0x01010101u);
+      }
+    }
+    for (int64_t t = T / 16 * 16 + threadIdx.x; t < T; t += 256) n += mask[t] != 0;
+  }
   for (int e = threadIdx.x; e < Ne; e += 256) c += counts[(int64_t)h * Ne + e];
   sums[threadIdx.x] = s;
   tokens[threadIdx.x] = n;
@@ -312,11 +438,12 @@ __global__ __launch_bounds__(256) void balance_loss_sum_kernel(
 }
 
 // ---------------------------------------------------------------------------
-// dX: 32 tokens of head blockIdx.y per wavefront, over all experts.  Without the
-// factor dloss / n, which comes at the end.
+// dX: 32 tokens of a head per wavefront, over all experts, as in the loss.  A bf16 dX
+// takes ds and W as one fp16 value each (2^-10 of each term off at most; where terms are
+// alike that adds up to a sixth of what bf16's own rounding does), an fp32 one as two.  ds comes out of the
+// exponential as ds 2^(F + K - k_b), with the block's power k_b and the head's smallest
+// K, so that all blocks' products add up alike; the rest of the factors come at the end.
 // ---------------------------------------------------------------------------
-// ds of a score tile, whose 8 rows 8 s .. 8 s + 7 of a lane are the operand of
-// k-step s: p (f' - u) in NP pieces.
 template <int NP>
 __device__ __forceinline__ void split_ds(const f32x16& ds, int s, u32x4 (&out)[NP]) {
   float f[8];
@@ -325,57 +452,68 @@ __device__ __forceinline__ void split_ds(const f32x16& ds, int s, u32x4 (&out)[N
   split8(f, out);
 }
 
+// The largest of the head's blocks' powers down (2^-K), in every lane.
+__device__ __forceinline__ float head_down(const HeadInfo& info, int nb) {
+  float d = lane_id() < nb ? info.down[lane_id()] : 0.0f;
+#pragma unroll
+  for (int i = 1; i < 32; i <<= 1) d = fmaxf(d, __shfl_xor(d, i, kWave));
+  return __shfl(d, 0, kWave);
+}
+
 template <int DH, bool F32>
 __global__ __launch_bounds__(kTokenWaves* kWave) void balance_dx_kernel(
     const void* __restrict__ X, const u32x4* __restrict__ weights,
-    const int32_t* __restrict__ counts, const float2* __restrict__ stats,
+    const HeadInfo* __restrict__ info, const float2* __restrict__ stats,
     const float* __restrict__ dloss, const uint8_t* __restrict__ mask, const void* dX_add,
     int64_t T, int Nh, int Ne, void* dX) {
-  constexpr int kFrags = kScoreFrags<DH> + kBackFrags<DH>;
-  constexpr int kLast = F32 ? 2 : 1;  // products of pieces i + j <= kLast
-  __shared__ u32x4 w[kFrags * 64];
+  constexpr int NP = F32 ? 2 : 1;
+  constexpr int kN = kFrags<DH, NP>;
+  __shared__ u32x4 w[2][kN * 64];
   __shared__ __align__(16) float fex[kMaxExperts];
-  __shared__ long long sums[kTokenWaves];
-  const int h = blockIdx.y, lane = lane_id(), g = lane >> 5, wave = threadIdx.x >> 6;
-  const int64_t t = (int64_t)blockIdx.x * kBalanceTokens + wave * 32 + (lane & 31);
+  const int h = blockIdx.x % Nh, lane = lane_id(), g = lane >> 5, wave = threadIdx.x >> 6;
+  const int64_t t = (int64_t)(blockIdx.x / Nh) * kBalanceTokens + wave * 32 + (lane & 31);
   const int64_t row = t * Nh + h;
   const bool ok = t < T && (!mask || mask[t < T ? t : 0]);
-  load_excess<kTokenWaves * kWave>(counts + (int64_t)h * Ne, Ne, fex, sums);
+  const int nb = (Ne + 31) / 32;
+  const u32x4 rsrc = buffer_words(weights + (int64_t)h * nb * kN * 64, (uint32_t)nb * kN * 1024u);
+  fetch_frags<kN>(rsrc, kN * 1024u, 0, w[0]);
+  for (int e = threadIdx.x; e < nb * 32; e += kTokenWaves * kWave) fex[e] = info[h].f[e];
   XOperand<DH, F32> x;
   x.load(X, row, ok, g);
   // a token that does not count: p = exp2(-infinity) = 0
   const float2 st = ok ? stats[row] : float2{INFINITY, 0.0f};
-  const float lse = st.x * kLog2e, u = st.y;
-  const float c = dloss[h] * stats[T * Nh + h].x;
-  const int nb = (Ne + 31) / 32;
-  const u32x4* src = weights + (int64_t)h * nb * kFrags * 64;
+  const float down = head_down(info[h], nb), F = info[h].F;
+  const float u = st.y, lse = st.x * kLog2e - F;
+  const float c = dloss[h] * stats[T * Nh + h].x * __builtin_amdgcn_ldexpf(down, -(int)F);
   f32x16 dx[DH / 32];
 #pragma unroll
   for (int i = 0; i < DH / 32; ++i) dx[i] = zero16();
   for (int b = 0; b < nb; ++b) {
-    __syncthreads();
-    copy_to_lds<kFrags * 64>(src + (int64_t)b * kFrags * 64, w);
-    __syncthreads();
-    f32x16 z = score_tile<DH, F32>(w, x, score_start(32 * b, Ne, g));
+    const float down_b = info[h].down[b];
+    const float m = x.down * down_b * kLog2e;
+    const float ref = lse - log2_of(down_b / down);
+    barrier_vm<0>();
+    if (b + 1 < nb) fetch_frags<kN>(rsrc, kN * 1024u, b + 1, w[(b + 1) & 1]);
+    const u32x4* wb = w[b & 1];
+    f32x16 z = score_tile<DH, F32>(wb, x, score_start(32 * b, Ne, g));
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const f32x4 f = *reinterpret_cast<const f32x4*>(&fex[32 * b + 8 * q + 4 * g]);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        z[4 * q + i] = __builtin_amdgcn_exp2f(fmaf(z[4 * q + i], kLog2e, -lse)) * (f[i] - u);
+        z[4 * q + i] = __builtin_amdgcn_exp2f(fmaf(z[4 * q + i], m, -ref)) * (f[i] - u);
     }
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      u32x4 ds[kLast + 1];
+      u32x4 ds[NP];
       split_ds(z, s, ds);
 #pragma unroll
       for (int dt = 0; dt < DH / 32; ++dt)
 #pragma unroll
-        for (int q = kLast; q >= 0; --q) {
-          const bf16x8 a = as_bf16x8(
-              w[(kScoreFrags<DH> + q * (DH / 32) * 2 + dt * 2 + s) * 64 + lane]);
+        for (int q = NP - 1; q >= 0; --q) {
+          const u32x4 a = wb[(kScoreFrags<DH> + q * kBackFrags<DH> + dt * 2 + s) * 64 + lane];
 #pragma unroll
-          for (int p = kLast - q; p >= 0; --p) dx[dt] = mfma32_bf16(a, as_bf16x8(ds[p]), dx[dt]);
+          for (int p = NP - 1 - q; p >= 0; --p) dx[dt] = mfma32_f16(a, ds[p], dx[dt]);
         }
     }
   }
@@ -399,7 +537,8 @@ __global__ __launch_bounds__(kTokenWaves* kWave) void balance_dx_kernel(
         if (dX_add) {
           const u32x2 a = *reinterpret_cast<const u32x2*>(static_cast<const uint16_t*>(dX_add) + at);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) f[i] += bf16_bits_to_f32((a[i >> 1] >> (16 * (i & 1))) & 0xFFFFu);
+          for (int i = 0; i < 4; ++i)
+            f[i] += bf16_bits_to_f32((a[i >> 1] >> (16 * (i & 1))) & 0xFFFFu);
         }
         *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(dX) + at) =
             u32x2{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3])};
@@ -408,126 +547,186 @@ __global__ __launch_bounds__(kTokenWaves* kWave) void balance_dx_kernel(
 }
 
 // ---------------------------------------------------------------------------
-// dW: a block of 32 experts per wavefront, whose weights stay in its registers,
-// over a chunk of the tokens, 32 at a time through LDS.
+// dW: a block of 32 experts per wavefront, whose weights stay in its registers, over
+// a chunk of the tokens, 32 SUB at a time through LDS in two buffers (SUB = 4 / EW
+// wavefronts share a block of experts where there are fewer than four blocks, each
+// with 32 tokens of its own).  X lies in LDS as pieces of x up (a token's power of
+// two), read along d for the scores and transposed for dW; what up adds is taken off
+// ds in its exponential.  ds is two fp16 values times S, a power of two that every
+// expert (lane) has for itself: it is lowered, and the sums with it, when a ds does not
+// fit any more, so an expert that gets little weight keeps its digits.
 // ---------------------------------------------------------------------------
-template <int DH, bool F32>
-__global__ __launch_bounds__(256) void balance_dw_kernel(
+constexpr int kDwWaves = 4;
+constexpr float kDwFirst = 0x1p60f;  // S before the first ds: any above 2^-45 lowers it
+
+template <int DH, bool F32, int EW>
+__global__ __launch_bounds__(kDwWaves* kWave) void balance_dw_kernel(
     const void* __restrict__ X, const u32x4* __restrict__ weights, int block_frags,
-    const int32_t* __restrict__ counts, const float2* __restrict__ stats,
-    const uint8_t* __restrict__ mask, int64_t T, int Nh, int Ne, int groups,
+    const HeadInfo* __restrict__ info, const float2* __restrict__ stats,
+    const uint8_t* __restrict__ mask, int64_t T, int Nh, int Ne, int groups, int splits,
     float* __restrict__ part) {
-  constexpr int NX = F32 ? 3 : 1;
-  constexpr int kUnits = DH / 8;  // 16-byte units of a row
-  __shared__ __align__(16) uint8_t xs[NX][32 * DH * 2];
-  __shared__ __align__(16) float lse[32], us[32];
-  __shared__ __align__(16) float fex[kMaxExperts];
-  __shared__ long long sums[4];
-  const int threads = blockDim.x;
-  const int h = blockIdx.x / groups, lane = lane_id(), g = lane >> 5;
-  const int nb = (Ne + 31) / 32;
-  const int b = (blockIdx.x % groups) * (threads / kWave) + (int)(threadIdx.x >> 6);
+  constexpr int NX = F32 ? 2 : 1, SUB = kDwWaves / EW, kTokens = 32 * SUB;
+  constexpr int kUnits = DH / 8;                                  // 16-byte units of a row
+  constexpr int kPer = kTokens * kUnits / (kDwWaves * kWave);     // units per thread
+  constexpr int kRowB = DH * 2;
+  __shared__ __align__(16) uint8_t xs[2][NX][kTokens * kRowB];
+  __shared__ __align__(16) float ms[2][kTokens], refs[2][kTokens], us[2][kTokens];
+  const int lane = lane_id(), g = lane >> 5, wave = threadIdx.x >> 6;
+  // all groups of a (head, chunk) on one die, which then reads its tokens once
+  const int at = blockIdx.x / kXcds, group = at % groups;
+  const int64_t pair = (int64_t)(at / groups) * kXcds + blockIdx.x % kXcds;
+  if (pair >= (int64_t)Nh * splits) return;
+  const int h = (int)(pair % Nh), split = (int)(pair / Nh);
+  const int nb = (Ne + 31) / 32, b = group * EW + wave % EW, sub = wave / EW;
   const bool live = b < nb;
-  // f' of the lane's expert
-  {
-    long long s = 0;
-    for (int e = threadIdx.x; e < Ne; e += threads) s += counts[(int64_t)h * Ne + e];
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) s += __shfl_xor(s, d, kWave);
-    if (lane == 0) sums[threadIdx.x >> 6] = s;
-    __syncthreads();
-  }
-  long long total = 0;
-  for (int i = 0; i < threads / kWave; ++i) total += sums[i];
   const int e = 32 * b + (lane & 31);
-  const float f = e < Ne && total > 0
-                      ? (float)((double)((long long)counts[(int64_t)h * Ne + e] * Ne - total) /
-                                (double)total)
-                      : 0.0f;
-  u32x4 w[3][DH / 16];
-  const u32x4* src = weights + ((int64_t)h * nb + (live ? b : 0)) * block_frags * 64;
+  const float down = head_down(info[h], nb);
+  const float f = live ? info[h].f[e] : 0.0f;
+  u32x4 w[2][DH / 16];
+  {
+    const u32x4* src = weights + ((int64_t)h * nb + (live ? b : 0)) * block_frags * 64;
+    // all blocks by the head's power of two
+    const _Float16 k = (_Float16)(info[h].down[live ? b : 0] / down);
 #pragma unroll
-  for (int q = 0; q < 3; ++q)
+    for (int q = 0; q < 2; ++q)
 #pragma unroll
-    for (int s = 0; s < DH / 16; ++s) w[q][s] = src[(q * (DH / 16) + s) * 64 + lane];
+      for (int s = 0; s < DH / 16; ++s)
+        w[q][s] = __builtin_bit_cast(
+            u32x4, __builtin_bit_cast(f16x8, src[(q * (DH / 16) + s) * 64 + lane]) * k);
+  }
   f32x16 dw[DH / 32];
 #pragma unroll
   for (int i = 0; i < DH / 32; ++i) dw[i] = zero16();
-  const int64_t tiles = (T + 31) / 32;
-  const int64_t begin = tiles * blockIdx.y / gridDim.y, end = tiles * (blockIdx.y + 1) / gridDim.y;
+  float S = kDwFirst;
+  const int64_t tiles = (T + kTokens - 1) / kTokens;
+  const int64_t begin = tiles * split / splits, end = tiles * (split + 1) / splits;
   auto addr = [](int row, int col) {
-    return row * DH * 2 + swz_tr<kUnits>(col >> 3, row) * 16 + (col & 7) * 2;
+    return row * kRowB + swz_tr<kUnits>(col >> 3, row) * 16 + (col & 7) * 2;
   };
-  for (int64_t tile = begin; tile < end; ++tile) {
-    __syncthreads();
-    for (int i = threadIdx.x; i < 32 * kUnits; i += threads) {
-      const int r = i / kUnits, j = i % kUnits;
-      const int64_t t = tile * 32 + r;
+  // a tile's rows on their way, then in LDS
+  u32x4 raw[kPer][F32 ? 2 : 1];
+  auto fetch = [&](int64_t tile) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int unit = i * kDwWaves * kWave + threadIdx.x;
+      const int64_t t = tile * kTokens + unit / kUnits;
       const bool ok = t < T && (!mask || mask[t]);
-      const int64_t at = (t * Nh + h) * DH + 8 * j;
-      u32x4 o[NX];
-      if (F32) {
-        const f32x4* p = reinterpret_cast<const f32x4*>(static_cast<const float*>(X) + at);
-        const f32x4 a = ok ? p[0] : f32x4{0, 0, 0, 0}, c = ok ? p[1] : f32x4{0, 0, 0, 0};
-        const float v[8] = {a[0], a[1], a[2], a[3], c[0], c[1], c[2], c[3]};
-        split8(v, o);
-      } else {
-        o[0] = ok ? *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(X) + at)
-                  : u32x4{0, 0, 0, 0};
+      const uint8_t* p = static_cast<const uint8_t*>(X) +
+                         ((t * Nh + h) * DH + 8 * (unit % kUnits)) * (F32 ? 4 : 2);
+#pragma unroll
+      for (int k = 0; k < (F32 ? 2 : 1); ++k)
+        raw[i][k] = ok ? *reinterpret_cast<const u32x4*>(p + 16 * k) : u32x4{0, 0, 0, 0};
+    }
+  };
+  auto store = [&](int64_t tile, int buf) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int unit = i * kDwWaves * kWave + threadIdx.x, r = unit / kUnits;
+      float v[8];
+      uint32_t top = 0;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        v[k] = XOperand<DH, F32>::value(raw[i], k);
+        top = umax(top, bits_abs(v[k]));
       }
 #pragma unroll
-      for (int p = 0; p < NX; ++p) *reinterpret_cast<u32x4*>(xs[p] + addr(r, 8 * j)) = o[p];
+      for (int d = 1; d < kUnits; d <<= 1) top = umax(top, __shfl_xor(top, d, kWave));
+      const Pow2 scale = pow2_below_2_15(top);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] *= scale.up;
+      u32x4 o[NX];
+      split8(v, o);
+#pragma unroll
+      for (int p = 0; p < NX; ++p)
+        *reinterpret_cast<u32x4*>(xs[buf][p] + addr(r, 8 * (unit % kUnits))) = o[p];
+      if (unit % kUnits == 0) {
+        const int64_t t = tile * kTokens + r;
+        const bool ok = t < T && (!mask || mask[t]);
+        // a token that does not count: p = exp2(-infinity) = 0
+        const float2 s = ok ? stats[t * Nh + h] : float2{INFINITY, 0.0f};
+        ms[buf][r] = scale.down * down * kLog2e;
+        refs[buf][r] = fmaf(s.x, kLog2e, -log2_of(scale.down));
+        us[buf][r] = s.y;
+      }
     }
-    if (threadIdx.x < 32) {
-      const int64_t t = tile * 32 + threadIdx.x;
-      const bool ok = t < T && (!mask || mask[t]);
-      const float2 st = ok ? stats[t * Nh + h] : float2{INFINITY, 0.0f};
-      lse[threadIdx.x] = st.x * kLog2e;
-      us[threadIdx.x] = st.y;
-    }
+  };
+  if (begin < end) {
+    fetch(begin);
+    store(begin, 0);
+  }
+  for (int64_t tile = begin; tile < end; ++tile) {
+    const int buf = (int)(tile - begin) & 1;
     __syncthreads();
+    if (tile + 1 < end) fetch(tile + 1);
+    const uint8_t* xb = xs[buf][0] + 32 * sub * kRowB;
+    constexpr int kPiece = kTokens * kRowB;
     // scores of 32 tokens (rows) x 32 experts (lanes)
     f32x16 z = zero16();
 #pragma unroll
     for (int p = NX - 1; p >= 0; --p)
 #pragma unroll
       for (int s = 0; s < DH / 16; ++s) {
-        const bf16x8 a = as_bf16x8(
-            *reinterpret_cast<const u32x4*>(xs[p] + addr(lane & 31, 16 * s + 8 * g)));
+        const u32x4 a = *reinterpret_cast<const u32x4*>(xb + p * kPiece +
+                                                        addr(lane & 31, 16 * s + 8 * g));
 #pragma unroll
-        for (int q = 2 - p; q >= 0; --q) z = mfma32_bf16(a, as_bf16x8(w[q][s]), z);
+        for (int q = 1 - p; q >= 0; --q) z = mfma32_f16(a, w[q][s], z);
       }
+    float top = 0.0f;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      const f32x4 l4 = *reinterpret_cast<const f32x4*>(&lse[8 * q + 4 * g]);
-      const f32x4 u4 = *reinterpret_cast<const f32x4*>(&us[8 * q + 4 * g]);
+      const int r = 32 * sub + 8 * q + 4 * g;
+      const f32x4 m4 = *reinterpret_cast<const f32x4*>(&ms[buf][r]);
+      const f32x4 r4 = *reinterpret_cast<const f32x4*>(&refs[buf][r]);
+      const f32x4 u4 = *reinterpret_cast<const f32x4*>(&us[buf][r]);
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        z[4 * q + i] = __builtin_amdgcn_exp2f(fmaf(z[4 * q + i], kLog2e, -l4[i])) * (f - u4[i]);
+      for (int i = 0; i < 4; ++i) {
+        z[4 * q + i] =
+            __builtin_amdgcn_exp2f(fmaf(z[4 * q + i], m4[i], -r4[i])) * (f - u4[i]);
+        top = fmaxf(top, fabsf(z[4 * q + i]));
+      }
+    }
+    top = fmaxf(top, __shfl_xor(top, 32, kWave));
+    if (__any(top * S >= 32768.0f)) {
+      // the largest to [2^10, 2^11)
+      uint32_t ex = __float_as_uint(top) >> 23;
+      ex = ex < 20u ? 20u : ex > 254u ? 254u : ex;
+      const float next = top * S >= 32768.0f ? __uint_as_float((264u - ex) << 23) : S;
+      const float k = next / S;
+      S = next;
+#pragma unroll
+      for (int dt = 0; dt < DH / 32; ++dt)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) dw[dt][v] *= k;
     }
 #pragma unroll
+    for (int v = 0; v < 16; ++v) z[v] *= S;
+#pragma unroll
     for (int s = 0; s < 2; ++s) {
-      u32x4 ds[3];
+      u32x4 ds[2];
       split_ds(z, s, ds);
 #pragma unroll
       for (int dt = 0; dt < DH / 32; ++dt)
 #pragma unroll
         for (int p = NX - 1; p >= 0; --p) {
-          const bf16x8 a = tr_fragment(xs[p], addr, 16 * s, 16 * s + 4, 16 * s + 8, 16 * s + 12,
-                                       32 * dt);
+          const u32x4 a = __builtin_bit_cast(
+              u32x4, tr_fragment(xb + p * kPiece, addr, 16 * s, 16 * s + 4, 16 * s + 8, 16 * s + 12,
+                                 32 * dt));
 #pragma unroll
-          for (int q = 2 - p; q >= 0; --q) dw[dt] = mfma32_bf16(a, as_bf16x8(ds[q]), dw[dt]);
+          for (int q = 1 - p; q >= 0; --q) dw[dt] = mfma32_f16(a, ds[q], dw[dt]);
         }
     }
+    if (tile + 1 < end) store(tile + 1, buf ^ 1);
   }
   if (!live) return;
-  float* o = part + (((int64_t)blockIdx.y * Nh + h) * nb * 32 + e) * DH;
+  const float k = 1.0f / S;
+  float* o = part + ((((int64_t)split * SUB + sub) * Nh + h) * nb * 32 + e) * DH;
 #pragma unroll
   for (int dt = 0; dt < DH / 32; ++dt)
 #pragma unroll
     for (int q = 0; q < 4; ++q)
       *reinterpret_cast<f32x4*>(o + 32 * dt + 8 * q + 4 * g) =
-          f32x4{dw[dt][4 * q], dw[dt][4 * q + 1], dw[dt][4 * q + 2], dw[dt][4 * q + 3]};
+          f32x4{dw[dt][4 * q] * k, dw[dt][4 * q + 1] * k, dw[dt][4 * q + 2] * k,
+                dw[dt][4 * q + 3] * k};
 }
 
 // dW = dW_add + dloss / n times the sum of n partial results, in order.
@@ -539,6 +738,7 @@ __global__ __launch_bounds__(256) void balance_dw_sum_kernel(
   if (i >= Ne * dh4) return;
   const f32x4* p = part + (int64_t)h * padded * dh4 + i;
   f32x4 s{0, 0, 0, 0};
+#pragma unroll 8
   for (int64_t r = 0; r < n; ++r) s += p[r * stride];
   const float c = dloss[h] * inv_n[h].x;
   f32x4 o;
@@ -568,22 +768,34 @@ hipError_t launch_expert_counts(const int32_t* idx, const uint8_t* mask, int64_t
   return hipGetLastError();
 }
 
-hipError_t launch_balance_weights(const float* W, int Nh, int dh, int Ne, bool backward, void* out,
-                                  hipStream_t s) {
+// A head's part of the workspace behind the operands.
+static HeadInfo* head_info(const void* weights, int Nh, int dh, int Ne) {
+  return reinterpret_cast<HeadInfo*>(
+      const_cast<uint8_t*>(static_cast<const uint8_t*>(weights)) +
+      balance_operand_bytes(Nh, dh, Ne));
+}
+
+hipError_t launch_balance_weights(const float* W, const int32_t* counts, int Nh, int dh, int Ne,
+                                  bool f32, bool backward, void* out, hipStream_t s) {
   const dim3 grid((unsigned)balance_blocks(Ne), (unsigned)Nh);
-  u32x4* o = static_cast<u32x4*>(out);
-#define MHL_WEIGHTS(DH, BWD) \
-  hipLaunchKernelGGL((balance_weights_kernel<DH, BWD>), grid, dim3(256), 0, s, W, Ne, o)
+#define MHL_WEIGHTS(DH, BACK)                                                                  \
+  hipLaunchKernelGGL((balance_weights_kernel<DH, BACK>), grid, dim3(256), 0, s, W, counts, Ne, \
+                     static_cast<u32x4*>(out), head_info(out, Nh, dh, Ne))
+  const int back = backward ? (f32 ? 2 : 1) : 0;
   if (dh == 128) {
-    if (backward)
-      MHL_WEIGHTS(128, true);
+    if (back == 2)
+      MHL_WEIGHTS(128, 2);
+    else if (back == 1)
+      MHL_WEIGHTS(128, 1);
     else
-      MHL_WEIGHTS(128, false);
+      MHL_WEIGHTS(128, 0);
   } else {
-    if (backward)
-      MHL_WEIGHTS(64, true);
+    if (back == 2)
+      MHL_WEIGHTS(64, 2);
+    else if (back == 1)
+      MHL_WEIGHTS(64, 1);
     else
-      MHL_WEIGHTS(64, false);
+      MHL_WEIGHTS(64, 0);
   }
 #undef MHL_WEIGHTS
   return hipGetLastError();
@@ -602,14 +814,14 @@ hipError_t launch_balance_weights(const float* W, int Nh, int dh, int Ne, bool b
       CALL(64, false);          \
   }
 
-hipError_t launch_balance_loss(const void* X, const void* weights, const int32_t* counts,
-                               const uint8_t* mask, int64_t T, int Nh, int dh, int Ne, bool f32,
-                               float* stats, double* part, hipStream_t s) {
-  const dim3 grid((unsigned)balance_token_blocks(T), (unsigned)Nh);
+hipError_t launch_balance_loss(const void* X, const void* weights, const uint8_t* mask, int64_t T,
+                               int Nh, int dh, int Ne, bool f32, float* stats, double* part,
+                               hipStream_t s) {
+  const dim3 grid((unsigned)(Nh * balance_token_blocks(T)));
 #define MHL_LOSS(DH, F32)                                                                      \
   hipLaunchKernelGGL((balance_loss_kernel<DH, F32>), grid, dim3(kTokenWaves* kWave), 0, s, X,  \
-                     static_cast<const u32x4*>(weights), counts, mask, T, Nh, Ne,              \
-                     reinterpret_cast<float2*>(stats), part)
+                     static_cast<const u32x4*>(weights), head_info(weights, Nh, dh, Ne), mask, \
+                     T, Nh, Ne, reinterpret_cast<float2*>(stats), part)
   MHL_BALANCE_TYPES(MHL_LOSS)
 #undef MHL_LOSS
   return hipGetLastError();
@@ -624,31 +836,42 @@ hipError_t launch_balance_loss_sum(const double* part, const int32_t* counts, co
   return hipGetLastError();
 }
 
-hipError_t launch_balance_dx(const void* X, const void* weights, const int32_t* counts,
-                             const float* stats, const float* dloss, const uint8_t* mask,
-                             const void* dX_add, int64_t T, int Nh, int dh, int Ne, bool f32,
-                             void* dX, hipStream_t s) {
-  const dim3 grid((unsigned)balance_token_blocks(T), (unsigned)Nh);
+hipError_t launch_balance_dx(const void* X, const void* weights, const float* stats,
+                             const float* dloss, const uint8_t* mask, const void* dX_add, int64_t T,
+                             int Nh, int dh, int Ne, bool f32, void* dX, hipStream_t s) {
+  const dim3 grid((unsigned)(Nh * balance_token_blocks(T)));
 #define MHL_DX(DH, F32)                                                                       \
   hipLaunchKernelGGL((balance_dx_kernel<DH, F32>), grid, dim3(kTokenWaves* kWave), 0, s, X,   \
-                     static_cast<const u32x4*>(weights), counts,                              \
+                     static_cast<const u32x4*>(weights), head_info(weights, Nh, dh, Ne),      \
                      reinterpret_cast<const float2*>(stats), dloss, mask, dX_add, T, Nh, Ne, dX)
   MHL_BALANCE_TYPES(MHL_DX)
 #undef MHL_DX
   return hipGetLastError();
 }
 
-hipError_t launch_balance_dw(const void* X, const void* weights, const int32_t* counts,
-                             const float* stats, const uint8_t* mask, int64_t T, int Nh, int dh,
-                             int Ne, bool f32, float* part, hipStream_t s) {
-  const int waves = balance_dw_waves(Ne), groups = (int)ceil_div(balance_blocks(Ne), waves);
-  const dim3 grid((unsigned)(Nh * groups), (unsigned)balance_splits(T, Nh, Ne));
-#define MHL_DW(DH, F32)                                                                          \
-  hipLaunchKernelGGL((balance_dw_kernel<DH, F32>), grid, dim3((unsigned)(waves * kWave)), 0, s,  \
-                     X, static_cast<const u32x4*>(weights), kScoreFrags<DH> + kBackFrags<DH>,    \
-                     counts, reinterpret_cast<const float2*>(stats), mask, T, Nh, Ne, groups, part)
+hipError_t launch_balance_dw(const void* X, const void* weights, const float* stats,
+                             const uint8_t* mask, int64_t T, int Nh, int dh, int Ne, bool f32,
+                             float* part, hipStream_t s) {
+  const int ew = balance_dw_blocks(Ne), groups = (int)ceil_div(balance_blocks(Ne), ew);
+  const int splits = (int)balance_splits(T, Nh, Ne);
+  const dim3 grid((unsigned)(ceil_div((int64_t)Nh * splits, kXcds) * kXcds * groups));
+#define MHL_DW_EW(DH, F32, EW)                                                                  \
+  hipLaunchKernelGGL((balance_dw_kernel<DH, F32, EW>), grid, dim3(kDwWaves* kWave), 0, s, X,    \
+                     static_cast<const u32x4*>(weights), kFrags<DH, F32 ? 2 : 1>,               \
+                     head_info(weights, Nh, dh, Ne), reinterpret_cast<const float2*>(stats),    \
+                     mask, T, Nh, Ne, groups, splits, part)
+#define MHL_DW(DH, F32)         \
+  do {                          \
+    if (ew == 1)                \
+      MHL_DW_EW(DH, F32, 1);    \
+    else if (ew == 2)           \
+      MHL_DW_EW(DH, F32, 2);    \
+    else                        \
+      MHL_DW_EW(DH, F32, 4);    \
+  } while (0)
   MHL_BALANCE_TYPES(MHL_DW)
 #undef MHL_DW
+#undef MHL_DW_EW
   return hipGetLastError();
 }
 
@@ -658,7 +881,7 @@ hipError_t launch_balance_dw_sum(const float* part, const float* stats, const fl
   const int padded = 32 * balance_blocks(Ne), dh4 = dh / 4;
   const dim3 grid((unsigned)ceil_div(Ne * dh4, 256), (unsigned)Nh);
   hipLaunchKernelGGL(balance_dw_sum_kernel, grid, dim3(256), 0, s,
-                     reinterpret_cast<const f32x4*>(part), balance_splits(T, Nh, Ne),
+                     reinterpret_cast<const f32x4*>(part), balance_parts(T, Nh, Ne),
                      (int64_t)Nh * padded * dh4, reinterpret_cast<const float2*>(stats) + T * Nh,
                      dloss, reinterpret_cast<const f32x4*>(dW_add), Ne, padded, dh4,
                      reinterpret_cast<f32x4*>(dW));

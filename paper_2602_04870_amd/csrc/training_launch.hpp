@@ -70,39 +70,49 @@ hipError_t launch_expert_counts(const int32_t* idx, const uint8_t* mask, int64_t
                                 int k, int32_t* counts, hipStream_t s);
 
 // The balance loss and its gradient.  The router's weights are first laid out as
-// operands (balance_weight_bytes), the gradient's dW comes as balance_splits
-// partial results of Nh x (Ne rounded up to 32) x dh floats that
+// operands (up to two fp16 pieces for the scores and two, transposed, for dX), with a
+// head's other numbers (kBalanceHeadBytes) behind them.  The gradient's dW comes as
+// balance_parts partial results of Nh x (Ne rounded up to 32) x dh floats that
 // launch_balance_dw_sum adds in order.
+constexpr size_t kBalanceHeadBytes = 4 * (1024 + 32 + 32);
 inline int balance_blocks(int Ne) { return (int)ceil_div(Ne, 32); }
-inline size_t balance_weight_bytes(int Nh, int dh, int Ne, bool backward) {
-  // three pieces of bf16 for the scores, three more transposed for dX
-  return (size_t)Nh * balance_blocks(Ne) * 32 * dh * 2 * (backward ? 6 : 3);
+inline size_t balance_operand_bytes(int Nh, int dh, int Ne) {
+  return (size_t)Nh * balance_blocks(Ne) * 32 * dh * 2 * 4;
+}
+inline size_t balance_weight_bytes(int Nh, int dh, int Ne) {
+  return balance_operand_bytes(Nh, dh, Ne) + Nh * kBalanceHeadBytes;
 }
 constexpr int kBalanceTokens = 128;  // per workgroup of the loss and of dX
-inline int64_t balance_token_blocks(int64_t T) { return ceil_div(T, kBalanceTokens); }
-// Wavefronts (a block of 32 experts each) per workgroup of dW, and the chunks that
-// the tokens are cut into, so that there are about 1024 workgroups.
-inline int balance_dw_waves(int Ne) { return balance_blocks(Ne) < 4 ? balance_blocks(Ne) : 4; }
+__host__ __device__ inline int64_t balance_token_blocks(int64_t T) {
+  return ceil_div(T, kBalanceTokens);
+}
+// dW: blocks of experts that a workgroup's four wavefronts have (they share them out
+// over the tokens where there are fewer than three), and the chunks that the tokens
+// are cut into, so that there are about 1024 workgroups.
+inline int balance_dw_blocks(int Ne) { return Ne <= 32 ? 1 : Ne <= 64 ? 2 : 4; }
 inline int64_t balance_splits(int64_t T, int Nh, int Ne) {
-  const int64_t groups = Nh * ceil_div(balance_blocks(Ne), balance_dw_waves(Ne));
-  const int64_t want = ceil_div(1024, groups), most = ceil_div(T, 64);
+  const int ew = balance_dw_blocks(Ne);
+  const int64_t groups = Nh * ceil_div(balance_blocks(Ne), ew);
+  const int64_t want = ceil_div(1024, groups), most = ceil_div(T, 256 / ew);
   return want < most ? want : most;
 }
-hipError_t launch_balance_weights(const float* W, int Nh, int dh, int Ne, bool backward, void* out,
-                                  hipStream_t s);
-hipError_t launch_balance_loss(const void* X, const void* weights, const int32_t* counts,
-                               const uint8_t* mask, int64_t T, int Nh, int dh, int Ne, bool f32,
-                               float* stats, double* part, hipStream_t s);
+inline int64_t balance_parts(int64_t T, int Nh, int Ne) {
+  return balance_splits(T, Nh, Ne) * (4 / balance_dw_blocks(Ne));
+}
+hipError_t launch_balance_weights(const float* W, const int32_t* counts, int Nh, int dh, int Ne,
+                                  bool f32, bool backward, void* out, hipStream_t s);
+hipError_t launch_balance_loss(const void* X, const void* weights, const uint8_t* mask, int64_t T,
+                               int Nh, int dh, int Ne, bool f32, float* stats, double* part,
+                               hipStream_t s);
 hipError_t launch_balance_loss_sum(const double* part, const int32_t* counts, const uint8_t* mask,
                                    int64_t T, int Nh, int Ne, float* loss, float* stats,
                                    hipStream_t s);
-hipError_t launch_balance_dx(const void* X, const void* weights, const int32_t* counts,
-                             const float* stats, const float* dloss, const uint8_t* mask,
-                             const void* dX_add, int64_t T, int Nh, int dh, int Ne, bool f32,
-                             void* dX, hipStream_t s);
-hipError_t launch_balance_dw(const void* X, const void* weights, const int32_t* counts,
-                             const float* stats, const uint8_t* mask, int64_t T, int Nh, int dh,
-                             int Ne, bool f32, float* part, hipStream_t s);
+hipError_t launch_balance_dx(const void* X, const void* weights, const float* stats,
+                             const float* dloss, const uint8_t* mask, const void* dX_add, int64_t T,
+                             int Nh, int dh, int Ne, bool f32, void* dX, hipStream_t s);
+hipError_t launch_balance_dw(const void* X, const void* weights, const float* stats,
+                             const uint8_t* mask, int64_t T, int Nh, int dh, int Ne, bool f32,
+                             float* part, hipStream_t s);
 hipError_t launch_balance_dw_sum(const float* part, const float* stats, const float* dloss,
                                  const float* dW_add, int64_t T, int Nh, int dh, int Ne, float* dW,
                                  hipStream_t s);

@@ -63,11 +63,11 @@ int main() {
                       st == MHLMOE_OK ? b : 0);
           // every launch is of fewer than 2^32 threads, the partial results' count is T's
           if (st == MHLMOE_OK) {
-            const int64_t groups = Nh * mhl::ceil_div(mhl::balance_blocks(Ne), mhl::balance_dw_waves(Ne));
-            expect("splits", mhl::balance_splits(T, Nh, Ne) <= 1024 &&
-                                 (T == 0 || mhl::balance_splits(T, Nh, Ne) >= 1), 1);
-            expect("threads", groups * 256 < (int64_t(1) << 32) &&
-                                  mhl::balance_token_blocks(T) * 512 < (int64_t(1) << 33), 1);
+            const int64_t splits = mhl::balance_splits(T, Nh, Ne);
+            const int64_t groups = mhl::ceil_div(mhl::balance_blocks(Ne), mhl::balance_dw_blocks(Ne));
+            expect("splits", splits <= 1024 && (T == 0 || splits >= 1), 1);
+            expect("dw", (Nh * splits + 7) * groups < (int64_t(1) << 24), 1);
+            expect("tokens", Nh * mhl::balance_token_blocks(T) < (int64_t(1) << 24), 1);
           }
         }
   }

@@ -86,10 +86,10 @@ def counts64(idx, mask, Ne):
 class Balance:
     """The loss and its gradient of one problem, and their errors.
 
-    A score is exact products of pieces added in fp32: 6 products per term at most
-    (3 for bf16), each addition off by U of the magnitudes so far, and with an fp32 X
-    three products of pieces left out, together below U: ez = (6 dh + 10) U sum
-    |x w|.  An exponential's argument (z - max) log2 e is rounded where it is up to
+    A score is exact products of pieces added in fp32: 3 products per term at most
+    (2 for bf16), each addition off by U of the magnitudes so far.  Two fp16 pieces are
+    off by 2^-23 = 2 U of the value, and with an fp32 X the product of the second pieces
+    is left out, 2^-22 = 4 U: ez = (6 dh + 10) U sum |x w|.  An exponential's argument (z - max) log2 e is rounded where it is up to
     2.9 |z|, log2 e itself is off by 2^-26, and exp2 by an ulp: ep = (4 |z| + 8) U
     with the row's largest |z|."""
 
@@ -120,9 +120,10 @@ class Balance:
                        + 2 * U * (1 + np.abs(self.loss)))
 
     def backward(self, dloss, dX_add, dW_add, bf16):
-        """dX and dW, and their errors before dX is rounded.  bf16: ds and W meet as
-        two pieces each with the small ones' product left out, below 3 * 2^-18 of
-        the term."""
+        """dX and dW, and their errors before dX is rounded.  bf16: ds and W meet as one
+        fp16 value each, 2^-11 of it off: 2^-10 and 2^-22 of the term.  (It was two
+        bf16 pieces each, 3 * 2^-18, before the kernel's operands were fp16.)  What lies
+        2^-39 below the largest of its scale's values is lost: 2^-20 U."""
         T, Nh, dh = self.X.shape
         Ne = self.W.shape[1]
         c = dloss / self.n
@@ -130,7 +131,7 @@ class Balance:
         e_ds = self.p * ((np.abs(self.f) + np.abs(self.u)[..., None]) * (self.e_p[..., None] + 4 * U)
                          + self.e_u[..., None]) * self.keep[:, None, None]
         dX = np.einsum("the,hed->thd", ds, self.W) * c[:, None]
-        left = 3 * 2.0 ** -18 if bf16 else 0.0
+        left = 2.0 ** -10 + 2.0 ** -22 if bf16 else 0.0
         x_off = (np.einsum("the,hed->thd", e_ds, np.abs(self.W))
                  + ((6 * Ne + 10) * U + left)
                  * np.einsum("the,hed->thd", np.abs(ds), np.abs(self.W))) * np.abs(c)[:, None]
