@@ -686,7 +686,7 @@ mhlmoe_status mhlmoe_expert_counts(const int32_t *idx, const uint8_t *mask,
  *   stats    [T + 1][n_heads][2] float, for the gradient: log sum_e' exp of the
  *            scores and sum_e p_t(e) (n_experts f_e - 1) of every token (zeros
  *            where it does not count), and 1 / max(n, 1) and 0 as row T (out)
- * What X holds at tokens that do not count is not read, so it may be anything.
+ * X may hold anything at tokens that do not count, NaN and infinities too.
  * Scores are of fp32 accuracy (the paper's FP32 router) and never leave the chip.
  * A token with a score that is not finite makes its head's loss NaN.
  * d_head 64 or 128, 1 <= n_heads, n_experts <= 1024, (T + 128) * n_heads < 2^31.

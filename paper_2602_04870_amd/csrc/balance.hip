@@ -242,6 +242,7 @@ struct XOperand {
   static constexpr int NX = F32 ? 2 : 1;
   u32x4 x[NX][DH / 16];
   float down;
+  // row: readable; ok: whether it counts (zeros otherwise).
   __device__ __forceinline__ void load(const void* X, int64_t row, bool ok, int g) {
     u32x4 raw[DH / 16][F32 ? 2 : 1];
     const uint8_t* p = static_cast<const uint8_t*>(X) + (row * DH + 8 * g) * (F32 ? 4 : 2);
@@ -249,8 +250,12 @@ struct XOperand {
     for (int s = 0; s < DH / 16; ++s)
 #pragma unroll
       for (int i = 0; i < (F32 ? 2 : 1); ++i)
-        raw[s][i] = ok ? *reinterpret_cast<const u32x4*>(p + 16 * s * (F32 ? 4 : 2) + 16 * i)
-                       : u32x4{0, 0, 0, 0};
+        raw[s][i] = *reinterpret_cast<const u32x4*>(p + 16 * s * (F32 ? 4 : 2) + 16 * i);
+#pragma unroll
+    for (int s = 0; s < DH / 16; ++s)
+#pragma unroll
+      for (int i = 0; i < (F32 ? 2 : 1); ++i)
+        if (!ok) raw[s][i] = u32x4{0, 0, 0, 0};
     uint32_t top = 0;
 #pragma unroll
     for (int s = 0; s < DH / 16; ++s)
@@ -339,7 +344,7 @@ __global__ __launch_bounds__(kTokenWaves* kWave) void balance_loss_kernel(
   fetch_frags<kN>(rsrc, kN * 1024u, 0, w[0]);
   for (int e = threadIdx.x; e < nb * 32; e += kTokenWaves * kWave) fex[e] = info[h].f[e];
   XOperand<DH, F32> x;
-  x.load(X, t * Nh + h, ok, g);
+  x.load(X, (t < T ? t : T - 1) * Nh + h, ok, g);
   float M = -INFINITY, l = 0.0f, u = 0.0f;  // maximum (times log2 e), sum, weighted sum
   for (int b = 0; b < nb; ++b) {
     const float m = x.down * info[h].down[b] * kLog2e;
@@ -444,6 +449,20 @@ __global__ __launch_bounds__(256) void balance_loss_sum_kernel(
 // exponential as ds 2^(F + K - k_b), with the block's power k_b and the head's smallest
 // K, so that all blocks' products add up alike; the rest of the factors come at the end.
 // ---------------------------------------------------------------------------
+// Maximum over the LANES (8 or 16) lanes that share a row.
+template <int LANES>
+__device__ __forceinline__ uint32_t row_max(uint32_t v) {
+  auto over = [&](auto ctrl) {
+    v = umax(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(ctrl)::value, 0xF, 0xF,
+                                                      true));
+  };
+  over(std::integral_constant<int, 0xB1>{});   // quad_perm [1, 0, 3, 2]
+  over(std::integral_constant<int, 0x4E>{});   // quad_perm [2, 3, 0, 1]
+  over(std::integral_constant<int, 0x141>{});  // row_half_mirror
+  if constexpr (LANES == 16) over(std::integral_constant<int, 0x140>{});  // row_mirror
+  return v;
+}
+
 template <int NP>
 __device__ __forceinline__ void split_ds(const f32x16& ds, int s, u32x4 (&out)[NP]) {
   float f[8];
@@ -479,7 +498,7 @@ __global__ __launch_bounds__(kTokenWaves* kWave) void balance_dx_kernel(
   fetch_frags<kN>(rsrc, kN * 1024u, 0, w[0]);
   for (int e = threadIdx.x; e < nb * 32; e += kTokenWaves * kWave) fex[e] = info[h].f[e];
   XOperand<DH, F32> x;
-  x.load(X, row, ok, g);
+  x.load(X, (t < T ? t : T - 1) * Nh + h, ok, g);
   // a token that does not count: p = exp2(-infinity) = 0
   const float2 st = ok ? stats[row] : float2{INFINITY, 0.0f};
   const float down = head_down(info[h], nb), F = info[h].F;
@@ -597,40 +616,45 @@ __global__ __launch_bounds__(kDwWaves* kWave) void balance_dw_kernel(
   f32x16 dw[DH / 32];
 #pragma unroll
   for (int i = 0; i < DH / 32; ++i) dw[i] = zero16();
-  float S = kDwFirst;
+  float S = kDwFirst, fS = f * kDwFirst;  // S and f' S
   const int64_t tiles = (T + kTokens - 1) / kTokens;
   const int64_t begin = tiles * split / splits, end = tiles * (split + 1) / splits;
   auto addr = [](int row, int col) {
     return row * kRowB + swz_tr<kUnits>(col >> 3, row) * 16 + (col & 7) * 2;
   };
-  // a tile's rows on their way, then in LDS
+  // a tile's rows and their stats on their way (nothing waits for the mask: what a token
+  // that does not count has is read and dropped), then in LDS
   u32x4 raw[kPer][F32 ? 2 : 1];
+  float2 st[kPer];
+  uint8_t counted[kPer];
   auto fetch = [&](int64_t tile) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int unit = i * kDwWaves * kWave + threadIdx.x;
-      const int64_t t = tile * kTokens + unit / kUnits;
-      const bool ok = t < T && (!mask || mask[t]);
+      int64_t t = tile * kTokens + unit / kUnits;
+      t = t < T ? t : T - 1;
       const uint8_t* p = static_cast<const uint8_t*>(X) +
                          ((t * Nh + h) * DH + 8 * (unit % kUnits)) * (F32 ? 4 : 2);
 #pragma unroll
       for (int k = 0; k < (F32 ? 2 : 1); ++k)
-        raw[i][k] = ok ? *reinterpret_cast<const u32x4*>(p + 16 * k) : u32x4{0, 0, 0, 0};
+        raw[i][k] = *reinterpret_cast<const u32x4*>(p + 16 * k);
+      st[i] = stats[t * Nh + h];
+      counted[i] = mask ? mask[t] : 1;
     }
   };
   auto store = [&](int64_t tile, int buf) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int unit = i * kDwWaves * kWave + threadIdx.x, r = unit / kUnits;
+      const bool ok = tile * kTokens + r < T && counted[i];
       float v[8];
       uint32_t top = 0;
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        v[k] = XOperand<DH, F32>::value(raw[i], k);
+        v[k] = ok ? XOperand<DH, F32>::value(raw[i], k) : 0.0f;
         top = umax(top, bits_abs(v[k]));
       }
-#pragma unroll
-      for (int d = 1; d < kUnits; d <<= 1) top = umax(top, __shfl_xor(top, d, kWave));
+      top = row_max<kUnits>(top);
       const Pow2 scale = pow2_below_2_15(top);
 #pragma unroll
       for (int k = 0; k < 8; ++k) v[k] *= scale.up;
@@ -640,13 +664,10 @@ __global__ __launch_bounds__(kDwWaves* kWave) void balance_dw_kernel(
       for (int p = 0; p < NX; ++p)
         *reinterpret_cast<u32x4*>(xs[buf][p] + addr(r, 8 * (unit % kUnits))) = o[p];
       if (unit % kUnits == 0) {
-        const int64_t t = tile * kTokens + r;
-        const bool ok = t < T && (!mask || mask[t]);
         // a token that does not count: p = exp2(-infinity) = 0
-        const float2 s = ok ? stats[t * Nh + h] : float2{INFINITY, 0.0f};
         ms[buf][r] = scale.down * down * kLog2e;
-        refs[buf][r] = fmaf(s.x, kLog2e, -log2_of(scale.down));
-        us[buf][r] = s.y;
+        refs[buf][r] = ok ? fmaf(st[i].x, kLog2e, -log2_of(scale.down)) : INFINITY;
+        us[buf][r] = ok ? st[i].y : 0.0f;
       }
     }
   };
@@ -681,25 +702,26 @@ __global__ __launch_bounds__(kDwWaves* kWave) void balance_dw_kernel(
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         z[4 * q + i] =
-            __builtin_amdgcn_exp2f(fmaf(z[4 * q + i], m4[i], -r4[i])) * (f - u4[i]);
+            __builtin_amdgcn_exp2f(fmaf(z[4 * q + i], m4[i], -r4[i])) * fmaf(-S, u4[i], fS);
         top = fmaxf(top, fabsf(z[4 * q + i]));
       }
     }
-    top = fmaxf(top, __shfl_xor(top, 32, kWave));
-    if (__any(top * S >= 32768.0f)) {
-      // the largest to [2^10, 2^11)
+    const u32x2 both = permlane32_swap(__float_as_uint(top), __float_as_uint(top));
+    top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+    if (__any(top >= 32768.0f)) {
+      // those down by a power of two that takes their largest to [2^10, 2^11)
       uint32_t ex = __float_as_uint(top) >> 23;
-      ex = ex < 20u ? 20u : ex > 254u ? 254u : ex;
-      const float next = top * S >= 32768.0f ? __uint_as_float((264u - ex) << 23) : S;
-      const float k = next / S;
-      S = next;
+      ex = ex > 254u ? 254u : ex;
+      const float k = top >= 32768.0f ? __uint_as_float((264u - ex) << 23) : 1.0f;
+      S *= k;
+      fS = f * S;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) z[v] *= k;
 #pragma unroll
       for (int dt = 0; dt < DH / 32; ++dt)
 #pragma unroll
         for (int v = 0; v < 16; ++v) dw[dt][v] *= k;
     }
-#pragma unroll
-    for (int v = 0; v < 16; ++v) z[v] *= S;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       u32x4 ds[2];
