@@ -76,6 +76,17 @@ __device__ __forceinline__ f32x16 mfma32_f16(u32x4 a, u32x4 b, f32x16 c) {
                                                 __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
+// v less one half of a register of two fp16 values, in one instruction.
+template <int HALF>
+__device__ __forceinline__ float minus_half(float v, uint32_t pair) {
+  float r;
+  if (HALF == 0)
+    asm("v_fma_mix_f32 %0, -%1, 1.0, %2 op_sel:[0,0,0] op_sel_hi:[1,0,0]" : "=v"(r) : "v"(pair), "v"(v));
+  else
+    asm("v_fma_mix_f32 %0, -%1, 1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(r) : "v"(pair), "v"(v));
+  return r;
+}
+
 // Eight values as N fp16 pieces, each the nearest to what the ones before left.
 template <int N>
 __device__ __forceinline__ void split8(const float (&f)[8], u32x4 (&out)[N]) {
@@ -89,8 +100,8 @@ __device__ __forceinline__ void split8(const float (&f)[8], u32x4 (&out)[N]) {
       const f16x2 h = __builtin_convertvector((f32x2{r[2 * i], r[2 * i + 1]}), f16x2);
       out[p][i] = __builtin_bit_cast(uint32_t, h);
       if (p + 1 < N) {
-        r[2 * i] -= (float)h[0];
-        r[2 * i + 1] -= (float)h[1];
+        r[2 * i] = minus_half<0>(r[2 * i], out[p][i]);
+        r[2 * i + 1] = minus_half<1>(r[2 * i + 1], out[p][i]);
       }
     }
 }
@@ -107,6 +118,9 @@ __device__ __forceinline__ Pow2 pow2_below_2_15(uint32_t most) {
 }
 __device__ __forceinline__ float log2_of(float power) {  // exactly
   return (float)((int)(__float_as_uint(power) >> 23) - 127);
+}
+__device__ __forceinline__ float uniform(float v) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_readfirstlane((int)__float_as_uint(v)));
 }
 __device__ __forceinline__ uint32_t bits_abs(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 __device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
@@ -284,21 +298,13 @@ struct XOperand {
   }
 };
 
-// Rows of a score tile past the last expert begin at -infinity: no weight.
-__device__ __forceinline__ f32x16 score_start(int e0, int Ne, int g) {
-  f32x16 z;
-#pragma unroll
-  for (int v = 0; v < 16; ++v)
-    z[v] = e0 + 8 * (v >> 2) + 4 * g + (v & 3) < Ne ? 0.0f : -INFINITY;
-  return z;
-}
-
 // Scores of 32 experts (rows) x 32 tokens (lanes), times both powers of two, small
-// products first.
+// products first.  e0: the block's first expert; rows past the last one have no weight.
 template <int DH, bool F32>
-__device__ __forceinline__ f32x16 score_tile(const u32x4* w, const XOperand<DH, F32>& x,
-                                             f32x16 z) {
+__device__ __forceinline__ f32x16 score_tile(const u32x4* w, const XOperand<DH, F32>& x, int e0,
+                                             int Ne) {
   const int lane = lane_id();
+  f32x16 z = zero16();
 #pragma unroll
   for (int q = 1; q >= 0; --q)
 #pragma unroll
@@ -308,6 +314,12 @@ __device__ __forceinline__ f32x16 score_tile(const u32x4* w, const XOperand<DH, 
       for (int p = XOperand<DH, F32>::NX - 1; p >= 0; --p)
         if (p + q <= 1) z = mfma32_f16(a, x.x[p][s], z);
     }
+  if (e0 + 32 > Ne) {
+    asm volatile("");  // a branch, not 48 instructions for every block
+#pragma unroll
+    for (int v = 0; v < 16; ++v)
+      z[v] = e0 + mfma32_row(v, lane) < Ne ? z[v] : -INFINITY;
+  }
   return z;
 }
 
@@ -350,7 +362,7 @@ __global__ __launch_bounds__(kTokenWaves* kWave) void balance_loss_kernel(
     const float m = x.down * info[h].down[b] * kLog2e;
     barrier_vm<0>();
     if (b + 1 < nb) fetch_frags<kN>(rsrc, kN * 1024u, b + 1, w[(b + 1) & 1]);
-    const f32x16 z = score_tile<DH, F32>(w[b & 1], x, score_start(32 * b, Ne, g));
+    const f32x16 z = score_tile<DH, F32>(w[b & 1], x, 32 * b, Ne);
     float top = z[0];
 #pragma unroll
     for (int v = 1; v < 16; ++v) top = fmaxf(top, z[v]);
@@ -476,7 +488,7 @@ __device__ __forceinline__ float head_down(const HeadInfo& info, int nb) {
   float d = lane_id() < nb ? info.down[lane_id()] : 0.0f;
 #pragma unroll
   for (int i = 1; i < 32; i <<= 1) d = fmaxf(d, __shfl_xor(d, i, kWave));
-  return __shfl(d, 0, kWave);
+  return uniform(d);
 }
 
 template <int DH, bool F32>
@@ -510,11 +522,11 @@ __global__ __launch_bounds__(kTokenWaves* kWave) void balance_dx_kernel(
   for (int b = 0; b < nb; ++b) {
     const float down_b = info[h].down[b];
     const float m = x.down * down_b * kLog2e;
-    const float ref = lse - log2_of(down_b / down);
+    const float ref = lse - (log2_of(down_b) - log2_of(down));
     barrier_vm<0>();
     if (b + 1 < nb) fetch_frags<kN>(rsrc, kN * 1024u, b + 1, w[(b + 1) & 1]);
     const u32x4* wb = w[b & 1];
-    f32x16 z = score_tile<DH, F32>(wb, x, score_start(32 * b, Ne, g));
+    f32x16 z = score_tile<DH, F32>(wb, x, 32 * b, Ne);
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const f32x4 f = *reinterpret_cast<const f32x4*>(&fex[32 * b + 8 * q + 4 * g]);
@@ -671,6 +683,15 @@ __global__ __launch_bounds__(kDwWaves* kWave) void balance_dw_kernel(
       }
     }
   };
+  // a lane's places in a tile, kept: the swizzle is linear (a row's mask repeats after 16
+  // rows), so the rest is an exclusive or or an offset
+  const int sub_row = 32 * sub;
+  const int z_at = addr(sub_row + (lane & 31), 8 * g);
+  int t_at[2];  // rows of k-step 0's two halves
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+    t_at[k] = addr(sub_row + 4 * g + 8 * k + ((lane & 15) >> 2),
+                   16 * ((lane >> 4) & 1) + 4 * (lane & 3));
   if (begin < end) {
     fetch(begin);
     store(begin, 0);
@@ -679,7 +700,7 @@ __global__ __launch_bounds__(kDwWaves* kWave) void balance_dw_kernel(
     const int buf = (int)(tile - begin) & 1;
     __syncthreads();
     if (tile + 1 < end) fetch(tile + 1);
-    const uint8_t* xb = xs[buf][0] + 32 * sub * kRowB;
+    const uint8_t* xb = xs[buf][0];
     constexpr int kPiece = kTokens * kRowB;
     // scores of 32 tokens (rows) x 32 experts (lanes)
     f32x16 z = zero16();
@@ -687,8 +708,8 @@ __global__ __launch_bounds__(kDwWaves* kWave) void balance_dw_kernel(
     for (int p = NX - 1; p >= 0; --p)
 #pragma unroll
       for (int s = 0; s < DH / 16; ++s) {
-        const u32x4 a = *reinterpret_cast<const u32x4*>(xb + p * kPiece +
-                                                        addr(lane & 31, 16 * s + 8 * g));
+        const u32x4 a =
+            *reinterpret_cast<const u32x4*>(xb + p * kPiece + (z_at ^ (s * 32)));
 #pragma unroll
         for (int q = 1 - p; q >= 0; --q) z = mfma32_f16(a, w[q][s], z);
       }
@@ -730,9 +751,10 @@ __global__ __launch_bounds__(kDwWaves* kWave) void balance_dw_kernel(
       for (int dt = 0; dt < DH / 32; ++dt)
 #pragma unroll
         for (int p = NX - 1; p >= 0; --p) {
-          const u32x4 a = __builtin_bit_cast(
-              u32x4, tr_fragment(xb + p * kPiece, addr, 16 * s, 16 * s + 4, 16 * s + 8, 16 * s + 12,
-                                 32 * dt));
+          const uint8_t* rows = xb + p * kPiece + 16 * s * kRowB;
+          const u32x2 lo = lds_read_tr16(rows + (t_at[0] ^ (dt * 64)));
+          const u32x2 hi = lds_read_tr16(rows + (t_at[1] ^ (dt * 64)));
+          const u32x4 a{lo[0], lo[1], hi[0], hi[1]};
 #pragma unroll
           for (int q = 1 - p; q >= 0; --q) dw[dt] = mfma32_f16(a, ds[q], dw[dt]);
         }
