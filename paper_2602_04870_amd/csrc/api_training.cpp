@@ -78,7 +78,7 @@ BalanceLayout balance_layout(int64_t T, int n_heads, int d_head, int n_experts, 
   BalanceLayout L;
   size_t cur = 0;
   L.weights = bump(cur, mhl::balance_weight_bytes(n_heads, d_head, n_experts));
-  L.part = bump(cur, backward ? sizeof(float) * (size_t)mhl::balance_parts(T, n_heads, n_experts) *
+  L.part = bump(cur, backward ? sizeof(float) * (size_t)mhl::balance_splits(T, n_heads, n_experts) *
                                     n_heads * mhl::balance_blocks(n_experts) * 32 * d_head
                               : sizeof(double) * (size_t)n_heads * mhl::balance_token_blocks(T));
   L.total = cur;
@@ -269,8 +269,8 @@ mhlmoe_status mhlmoe_balance_loss(const void* X, const float* W_router, const in
   double* part = at<double>(workspace, L.part);
   if (T > 0) {
     MHL_TRY(run_kernel("balance_weights", stream, [&] {
-      return mhl::launch_balance_weights(W_router, counts, n_heads, d_head, n_experts,
-                                         dtype == MHLMOE_F32, false, weights, stream);
+      return mhl::launch_balance_weights(W_router, counts, n_heads, d_head, n_experts, weights,
+                                         stream);
     }));
     MHL_TRY(run_kernel("balance_loss", stream, [&] {
       return mhl::launch_balance_loss(X, weights, mask, T, n_heads, d_head, n_experts,
@@ -319,18 +319,19 @@ mhlmoe_status mhlmoe_balance_loss_backward(
   const bool f32 = dtype == MHLMOE_F32;
   if (T > 0) {
     MHL_TRY(run_kernel("balance_weights", stream, [&] {
-      return mhl::launch_balance_weights(W_router, counts, n_heads, d_head, n_experts, f32, true,
-                                         weights, stream);
+      return mhl::launch_balance_weights(W_router, counts, n_heads, d_head, n_experts, weights,
+                                         stream);
     }));
     MHL_TRY(run_kernel("balance_dx", stream, [&] {
       return mhl::launch_balance_dx(X, weights, stats, dloss, mask, dX_add, T, n_heads, d_head,
                                     n_experts, f32, dX, stream);
     }));
     MHL_TRY(run_kernel("balance_dw", stream, [&] {
-      return mhl::launch_balance_dw(X, weights, stats, mask, T, n_heads, d_head, n_experts, f32,
-                                    part, stream);
+      return mhl::launch_balance_dw(X, W_router, counts, stats, dloss, mask, dW_add, T, n_heads,
+                                    d_head, n_experts, f32, dW_router, part, stream);
     }));
   }
+  if (mhl::balance_splits(T, n_heads, n_experts) == 1) return MHLMOE_OK;
   return run_kernel("balance_sum", stream, [&] {
     return mhl::launch_balance_dw_sum(part, stats, dloss, dW_add, T, n_heads, d_head, n_experts,
                                       dW_router, stream);

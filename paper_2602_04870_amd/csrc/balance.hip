@@ -125,22 +125,74 @@ __device__ __forceinline__ float uniform(float v) {
 __device__ __forceinline__ uint32_t bits_abs(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 __device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
 
-// A block of 32 experts as operands: fragments of 64 lanes x 16 bytes.
-//   scores: piece, k-step s: lane holds expert lane % 32, d = 16 s + 8 (lane / 32) + j
-//   dX (transposed): piece, tile dt of 32 d, k-step s: lane holds d = 32 dt + lane % 32,
-//       experts 16 s + 8 (j / 4) + 4 (lane / 32) + j % 4, in the order in which a score
-//       tile's rows lie in its registers
-// BACK: pieces of the latter (1 for a bf16 dX, 2 for an fp32 one, 0 for none).
-template <int DH>
-constexpr int kScoreFrags = 2 * DH / 16;
-template <int DH>
-constexpr int kBackFrags = (DH / 32) * 2;  // per piece
-template <int DH, int BACK>
-constexpr int kFrags = kScoreFrags<DH> + BACK * kBackFrags<DH>;
+// Maximum over the LANES (8 or 16) lanes that share a row.
+template <int LANES>
+__device__ __forceinline__ uint32_t row_max(uint32_t v) {
+  auto over = [&](auto ctrl) {
+    v = umax(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(ctrl)::value, 0xF, 0xF,
+                                                      true));
+  };
+  over(std::integral_constant<int, 0xB1>{});   // quad_perm [1, 0, 3, 2]
+  over(std::integral_constant<int, 0x4E>{});   // quad_perm [2, 3, 0, 1]
+  over(std::integral_constant<int, 0x141>{});  // row_half_mirror
+  if constexpr (LANES == 16) over(std::integral_constant<int, 0x140>{});  // row_mirror
+  return v;
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+  v = row_max<16>(v);
+  v = umax(v, __shfl_xor(v, 16, kWave));
+  return umax(v, __shfl_xor(v, 32, kWave));
+}
+__device__ __forceinline__ long long wave_sum(long long v) {
+#pragma unroll
+  for (int d = 1; d < kWave; d <<= 1) v += __shfl_xor(v, d, kWave);
+  return v;
+}
 
-// What lies behind the operands in the workspace, per head: f'_e of the experts
-// (zeros up to the next multiple of 32), the blocks' powers of two (down) and the
-// exponent F that takes ds below 2^14.
+// f' = E c / total - 1 from exact whole numbers, with one division.
+__device__ __forceinline__ float excess(int32_t c, int Ne, long long total) {
+  return total > 0 ? (float)((double)((long long)c * Ne - total) / (double)total) : 0.0f;
+}
+// |f' - u| <= max f' - min f': the exponent F with |f' - u| 2^F < 2^14.
+__device__ __forceinline__ float ds_exponent(uint32_t most, uint32_t least, int Ne,
+                                             long long total) {
+  const double R = total > 0 ? (double)((long long)(most - least) * Ne) / (double)total : 0.0;
+  return R > 0.0 ? (float)(13 - ilogb(R)) : 0.0f;
+}
+
+// A matrix of rows of DH fp16 values in LDS, 16-byte units swizzled (swz_tr), and a lane's
+// places in 32 of its rows as an operand: with the rows as the operand's rows (lane: row
+// lane % 32, columns 16 s + 8 (lane / 32) + j), and transposed (lane: column 32 dt + lane
+// % 32, rows 16 s + 8 (j / 4) + 4 (lane / 32) + j % 4, the order in which the rows of a
+// 32 x 32 product lie in a lane's registers).  The swizzle is linear and repeats after
+// 16 rows, so everything but the lane's base is an exclusive or or an offset.
+template <int DH>
+struct Tile {
+  static constexpr int kRow = DH * 2;
+  static constexpr int kBytes = 32 * kRow;
+  static __device__ __forceinline__ int unit(int row, int j) {
+    return row * kRow + swz_tr<DH / 8>(j, row) * 16;
+  }
+  int rows, cols[2];
+  __device__ __forceinline__ Tile() {
+    const int lane = lane_id(), g = lane >> 5, c = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+    rows = unit(lane & 31, g);
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      cols[k] = unit(4 * g + 8 * k + ((lane & 15) >> 2), c >> 3) + (c & 7) * 2;
+  }
+  __device__ __forceinline__ u32x4 row_operand(const uint8_t* p, int s) const {
+    return *reinterpret_cast<const u32x4*>(p + (rows ^ (s * 32)));
+  }
+  __device__ __forceinline__ u32x4 col_operand(const uint8_t* p, int dt, int s) const {
+    const u32x2 lo = lds_read_tr16(p + 16 * s * kRow + (cols[0] ^ (dt * 64)));
+    const u32x2 hi = lds_read_tr16(p + 16 * s * kRow + (cols[1] ^ (dt * 64)));
+    return u32x4{lo[0], lo[1], hi[0], hi[1]};
+  }
+};
+
+// What lies behind the weights in the workspace, per head: f'_e of the experts (zeros up
+// to the next multiple of 32), the blocks' powers of two (down) and F.
 struct HeadInfo {
   float f[kMaxExperts];
   float down[kMaxExperts / 32];
@@ -149,29 +201,32 @@ struct HeadInfo {
 };
 static_assert(sizeof(HeadInfo) == kBalanceHeadBytes, "workspace");
 
-// Grid (blocks of 32 experts, heads).
-template <int DH, int BACK>
+// The router's weights, grid (blocks of 32 experts, heads): two Tiles per block, the
+// pieces of w up.
+template <int DH>
 __global__ __launch_bounds__(256) void balance_weights_kernel(const float* __restrict__ W,
                                                               const int32_t* __restrict__ counts,
-                                                              int Ne, u32x4* __restrict__ out,
+                                                              int Ne, uint8_t* __restrict__ out,
                                                               HeadInfo* __restrict__ info) {
-  constexpr int kStride = DH + 1;
-  __shared__ float w[32 * kStride];
+  constexpr int kUnits = DH / 8, kPer = 32 * kUnits / 256;
   __shared__ long long totals[4];
   __shared__ uint32_t tops[3][4];
   const int e0 = blockIdx.x * 32, h = blockIdx.y, lane = lane_id(), wave = threadIdx.x >> 6;
   const float* src = W + ((int64_t)h * Ne + e0) * DH;
-  const int here = Ne - e0 < 32 ? Ne - e0 : 32;
+  float v[kPer][8];
   uint32_t top = 0;
 #pragma unroll
-  for (int i = 0; i < 32 * DH; i += 1024) {
-    const int at = i + threadIdx.x * 4;
-    f32x4 v{0, 0, 0, 0};
-    if (at < here * DH) v = *reinterpret_cast<const f32x4*>(src + at);
+  for (int i = 0; i < kPer; ++i) {
+    const int unit = i * 256 + threadIdx.x;
+    const bool ok = e0 + unit / kUnits < Ne;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      w[at / DH * kStride + at % DH + k] = v[k];
-      top = umax(top, bits_abs(v[k]));
+    for (int k = 0; k < 2; ++k) {
+      const f32x4 x = ok ? *reinterpret_cast<const f32x4*>(src + unit * 8 + 4 * k) : f32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        v[i][4 * k + j] = x[j];
+        top = umax(top, bits_abs(x[j]));
+      }
     }
   }
   long long total = 0;
@@ -182,19 +237,15 @@ __global__ __launch_bounds__(256) void balance_weights_kernel(const float* __res
     most = umax(most, c);
     least = c < least ? c : least;
   }
-  least = ~least;
-#pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) {
-    total += __shfl_xor(total, d, kWave);
-    top = umax(top, __shfl_xor(top, d, kWave));
-    most = umax(most, __shfl_xor(most, d, kWave));
-    least = umax(least, __shfl_xor(least, d, kWave));
-  }
+  total = wave_sum(total);
+  top = wave_max(top);
+  most = wave_max(most);
+  least = ~wave_max(~least);
   if (lane == 0) {
     totals[wave] = total;
     tops[0][wave] = top;
     tops[1][wave] = most;
-    tops[2][wave] = least;
+    tops[2][wave] = ~least;
   }
   __syncthreads();
   total = totals[0] + totals[1] + totals[2] + totals[3];
@@ -203,49 +254,25 @@ __global__ __launch_bounds__(256) void balance_weights_kernel(const float* __res
   };
   const Pow2 scale = pow2_below_2_15(over_waves(0));
   if (threadIdx.x < 32) {
-    // exact whole numbers, one division
     const int e = e0 + threadIdx.x;
-    float f = 0.0f;
-    if (e < Ne && total > 0)
-      f = (float)((double)((long long)counts[(int64_t)h * Ne + e] * Ne - total) / (double)total);
-    info[h].f[e] = f;
+    info[h].f[e] = e < Ne ? excess(counts[(int64_t)h * Ne + e], Ne, total) : 0.0f;
     if (threadIdx.x == 0) {
       info[h].down[blockIdx.x] = scale.down;
-      if (blockIdx.x == 0) {
-        // |f' - u| <= max f' - min f' = R: p (f' - u) 2^F < 2^14
-        const double R = total > 0 ? (double)((long long)(over_waves(1) - ~over_waves(2)) * Ne) /
-                                         (double)total
-                                   : 0.0;
-        info[h].F = R > 0.0 ? (float)(13 - ilogb(R)) : 0.0f;
-      }
+      if (blockIdx.x == 0) info[h].F = ds_exponent(over_waves(1), ~over_waves(2), Ne, total);
     }
   }
-  u32x4* o = out + ((int64_t)h * gridDim.x + blockIdx.x) * kFrags<DH, BACK> * 64;
-  for (int i = threadIdx.x; i < DH / 16 * 64; i += 256) {
-    const int s = i >> 6, l = i & 63;
-    float f[8];
+  uint8_t* o = out + ((int64_t)h * gridDim.x + blockIdx.x) * 2 * Tile<DH>::kBytes;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int unit = i * 256 + threadIdx.x;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[i][j] *= scale.up;
     u32x4 p[2];
+    split8(v[i], p);
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      f[j] = w[(l & 31) * kStride + 16 * s + 8 * (l >> 5) + j] * scale.up;
-    split8(f, p);
-#pragma unroll
-    for (int q = 0; q < 2; ++q) o[(q * (DH / 16) + s) * 64 + l] = p[q];
-  }
-  if constexpr (BACK > 0) {
-    o += kScoreFrags<DH> * 64;
-    for (int i = threadIdx.x; i < DH / 32 * 2 * 64; i += 256) {
-      const int dt = i >> 7, s = (i >> 6) & 1, l = i & 63;
-      float f[8];
-      u32x4 p[BACK];
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        f[j] = w[(16 * s + 8 * (j >> 2) + 4 * (l >> 5) + (j & 3)) * kStride + 32 * dt + (l & 31)] *
-               scale.up;
-      split8(f, p);
-#pragma unroll
-      for (int q = 0; q < BACK; ++q) o[(q * kBackFrags<DH> + dt * 2 + s) * 64 + l] = p[q];
-    }
+    for (int q = 0; q < 2; ++q)
+      *reinterpret_cast<u32x4*>(o + q * Tile<DH>::kBytes +
+                                Tile<DH>::unit(unit / kUnits, unit % kUnits)) = p[q];
   }
 }
 
@@ -301,15 +328,14 @@ struct XOperand {
 // Scores of 32 experts (rows) x 32 tokens (lanes), times both powers of two, small
 // products first.  e0: the block's first expert; rows past the last one have no weight.
 template <int DH, bool F32>
-__device__ __forceinline__ f32x16 score_tile(const u32x4* w, const XOperand<DH, F32>& x, int e0,
-                                             int Ne) {
-  const int lane = lane_id();
+__device__ __forceinline__ f32x16 score_tile(const uint8_t* w, const Tile<DH>& at,
+                                             const XOperand<DH, F32>& x, int e0, int Ne) {
   f32x16 z = zero16();
 #pragma unroll
   for (int q = 1; q >= 0; --q)
 #pragma unroll
     for (int s = 0; s < DH / 16; ++s) {
-      const u32x4 a = w[(q * (DH / 16) + s) * 64 + lane];
+      const u32x4 a = at.row_operand(w + q * Tile<DH>::kBytes, s);
 #pragma unroll
       for (int p = XOperand<DH, F32>::NX - 1; p >= 0; --p)
         if (p + q <= 1) z = mfma32_f16(a, x.x[p][s], z);
@@ -318,20 +344,21 @@ __device__ __forceinline__ f32x16 score_tile(const u32x4* w, const XOperand<DH, 
     asm volatile("");  // a branch, not 48 instructions for every block
 #pragma unroll
     for (int v = 0; v < 16; ++v)
-      z[v] = e0 + mfma32_row(v, lane) < Ne ? z[v] : -INFINITY;
+      z[v] = e0 + mfma32_row(v, lane_id()) < Ne ? z[v] : -INFINITY;
   }
   return z;
 }
 
-// Fragments [0, N) of a block to LDS, dealt to the wavefronts, by DMA that the
-// compiler does not track: barrier_vm<0> before they are read.
-template <int N>
-__device__ __forceinline__ void fetch_frags(u32x4 rsrc, uint32_t block_bytes, int b, u32x4* lds) {
+// A block's weights to LDS, a KB per wavefront in turn, by DMA that the compiler does not
+// track: barrier_vm<0> before they are read.
+template <int DH>
+__device__ __forceinline__ void fetch_block(u32x4 rsrc, int b, uint8_t* lds) {
+  constexpr uint32_t kBlock = 2 * Tile<DH>::kBytes;
   const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const uint32_t voff = lane_id() * 16;
 #pragma unroll
-  for (int i = 0; i < N; i += kTokenWaves)
-    dma_lds16(rsrc, lds + (i + wave) * 64, voff, (uint32_t)b * block_bytes + (i + wave) * 1024u);
+  for (uint32_t i = 0; i < kBlock; i += kTokenWaves * 1024u)
+    dma_lds16(rsrc, lds + i + wave * 1024u, voff, (uint32_t)b * kBlock + i + wave * 1024u);
 }
 
 // ---------------------------------------------------------------------------
@@ -341,19 +368,20 @@ __device__ __forceinline__ void fetch_frags(u32x4 rsrc, uint32_t block_bytes, in
 // ---------------------------------------------------------------------------
 template <int DH, bool F32>
 __global__ __launch_bounds__(kTokenWaves* kWave) void balance_loss_kernel(
-    const void* __restrict__ X, const u32x4* __restrict__ weights,
+    const void* __restrict__ X, const uint8_t* __restrict__ weights,
     const HeadInfo* __restrict__ info, const uint8_t* __restrict__ mask, int64_t T, int Nh, int Ne,
     float2* __restrict__ stats, double* __restrict__ part) {
-  constexpr int kN = kFrags<DH, 0>;
-  __shared__ u32x4 w[2][kN * 64];
+  constexpr uint32_t kBlock = 2 * Tile<DH>::kBytes;
+  __shared__ __align__(16) uint8_t w[2][kBlock];
   __shared__ __align__(16) float fex[kMaxExperts];
   __shared__ double loss[kTokenWaves];
   const int h = blockIdx.x % Nh, lane = lane_id(), g = lane >> 5, wave = threadIdx.x >> 6;
   const int64_t tb = blockIdx.x / Nh, t = tb * kBalanceTokens + wave * 32 + (lane & 31);
   const bool ok = t < T && (!mask || mask[t < T ? t : 0]);
   const int nb = (Ne + 31) / 32;
-  const u32x4 rsrc = buffer_words(weights + (int64_t)h * nb * kN * 64, (uint32_t)nb * kN * 1024u);
-  fetch_frags<kN>(rsrc, kN * 1024u, 0, w[0]);
+  const u32x4 rsrc = buffer_words(weights + (int64_t)h * nb * kBlock, (uint32_t)nb * kBlock);
+  fetch_block<DH>(rsrc, 0, w[0]);
+  const Tile<DH> at;
   for (int e = threadIdx.x; e < nb * 32; e += kTokenWaves * kWave) fex[e] = info[h].f[e];
   XOperand<DH, F32> x;
   x.load(X, (t < T ? t : T - 1) * Nh + h, ok, g);
@@ -361,8 +389,8 @@ __global__ __launch_bounds__(kTokenWaves* kWave) void balance_loss_kernel(
   for (int b = 0; b < nb; ++b) {
     const float m = x.down * info[h].down[b] * kLog2e;
     barrier_vm<0>();
-    if (b + 1 < nb) fetch_frags<kN>(rsrc, kN * 1024u, b + 1, w[(b + 1) & 1]);
-    const f32x16 z = score_tile<DH, F32>(w[b & 1], x, 32 * b, Ne);
+    if (b + 1 < nb) fetch_block<DH>(rsrc, b + 1, w[(b + 1) & 1]);
+    const f32x16 z = score_tile<DH, F32>(w[b & 1], at, x, 32 * b, Ne);
     float top = z[0];
 #pragma unroll
     for (int v = 1; v < 16; ++v) top = fmaxf(top, z[v]);
@@ -461,20 +489,6 @@ __global__ __launch_bounds__(256) void balance_loss_sum_kernel(
 // exponential as ds 2^(F + K - k_b), with the block's power k_b and the head's smallest
 // K, so that all blocks' products add up alike; the rest of the factors come at the end.
 // ---------------------------------------------------------------------------
-// Maximum over the LANES (8 or 16) lanes that share a row.
-template <int LANES>
-__device__ __forceinline__ uint32_t row_max(uint32_t v) {
-  auto over = [&](auto ctrl) {
-    v = umax(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(ctrl)::value, 0xF, 0xF,
-                                                      true));
-  };
-  over(std::integral_constant<int, 0xB1>{});   // quad_perm [1, 0, 3, 2]
-  over(std::integral_constant<int, 0x4E>{});   // quad_perm [2, 3, 0, 1]
-  over(std::integral_constant<int, 0x141>{});  // row_half_mirror
-  if constexpr (LANES == 16) over(std::integral_constant<int, 0x140>{});  // row_mirror
-  return v;
-}
-
 template <int NP>
 __device__ __forceinline__ void split_ds(const f32x16& ds, int s, u32x4 (&out)[NP]) {
   float f[8];
@@ -493,21 +507,22 @@ __device__ __forceinline__ float head_down(const HeadInfo& info, int nb) {
 
 template <int DH, bool F32>
 __global__ __launch_bounds__(kTokenWaves* kWave) void balance_dx_kernel(
-    const void* __restrict__ X, const u32x4* __restrict__ weights,
+    const void* __restrict__ X, const uint8_t* __restrict__ weights,
     const HeadInfo* __restrict__ info, const float2* __restrict__ stats,
     const float* __restrict__ dloss, const uint8_t* __restrict__ mask, const void* dX_add,
     int64_t T, int Nh, int Ne, void* dX) {
   constexpr int NP = F32 ? 2 : 1;
-  constexpr int kN = kFrags<DH, NP>;
-  __shared__ u32x4 w[2][kN * 64];
+  constexpr uint32_t kBlock = 2 * Tile<DH>::kBytes;
+  __shared__ __align__(16) uint8_t w[2][kBlock];
   __shared__ __align__(16) float fex[kMaxExperts];
   const int h = blockIdx.x % Nh, lane = lane_id(), g = lane >> 5, wave = threadIdx.x >> 6;
   const int64_t t = (int64_t)(blockIdx.x / Nh) * kBalanceTokens + wave * 32 + (lane & 31);
   const int64_t row = t * Nh + h;
   const bool ok = t < T && (!mask || mask[t < T ? t : 0]);
   const int nb = (Ne + 31) / 32;
-  const u32x4 rsrc = buffer_words(weights + (int64_t)h * nb * kN * 64, (uint32_t)nb * kN * 1024u);
-  fetch_frags<kN>(rsrc, kN * 1024u, 0, w[0]);
+  const u32x4 rsrc = buffer_words(weights + (int64_t)h * nb * kBlock, (uint32_t)nb * kBlock);
+  fetch_block<DH>(rsrc, 0, w[0]);
+  const Tile<DH> at;
   for (int e = threadIdx.x; e < nb * 32; e += kTokenWaves * kWave) fex[e] = info[h].f[e];
   XOperand<DH, F32> x;
   x.load(X, (t < T ? t : T - 1) * Nh + h, ok, g);
@@ -524,9 +539,9 @@ __global__ __launch_bounds__(kTokenWaves* kWave) void balance_dx_kernel(
     const float m = x.down * down_b * kLog2e;
     const float ref = lse - (log2_of(down_b) - log2_of(down));
     barrier_vm<0>();
-    if (b + 1 < nb) fetch_frags<kN>(rsrc, kN * 1024u, b + 1, w[(b + 1) & 1]);
-    const u32x4* wb = w[b & 1];
-    f32x16 z = score_tile<DH, F32>(wb, x, 32 * b, Ne);
+    if (b + 1 < nb) fetch_block<DH>(rsrc, b + 1, w[(b + 1) & 1]);
+    const uint8_t* wb = w[b & 1];
+    f32x16 z = score_tile<DH, F32>(wb, at, x, 32 * b, Ne);
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const f32x4 f = *reinterpret_cast<const f32x4*>(&fex[32 * b + 8 * q + 4 * g]);
@@ -542,7 +557,7 @@ __global__ __launch_bounds__(kTokenWaves* kWave) void balance_dx_kernel(
       for (int dt = 0; dt < DH / 32; ++dt)
 #pragma unroll
         for (int q = NP - 1; q >= 0; --q) {
-          const u32x4 a = wb[(kScoreFrags<DH> + q * kBackFrags<DH> + dt * 2 + s) * 64 + lane];
+          const u32x4 a = at.col_operand(wb + q * Tile<DH>::kBytes, dt, s);
 #pragma unroll
           for (int p = NP - 1 - q; p >= 0; --p) dx[dt] = mfma32_f16(a, ds[p], dx[dt]);
         }
@@ -553,25 +568,25 @@ __global__ __launch_bounds__(kTokenWaves* kWave) void balance_dx_kernel(
   for (int dt = 0; dt < DH / 32; ++dt)
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      const int64_t at = row * DH + 32 * dt + 8 * q + 4 * g;
+      const int64_t to = row * DH + 32 * dt + 8 * q + 4 * g;
       float f[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) f[i] = ok ? dx[dt][4 * q + i] * c : 0.0f;
       if (F32) {
         if (dX_add) {
-          const f32x4 a = *reinterpret_cast<const f32x4*>(static_cast<const float*>(dX_add) + at);
+          const f32x4 a = *reinterpret_cast<const f32x4*>(static_cast<const float*>(dX_add) + to);
 #pragma unroll
           for (int i = 0; i < 4; ++i) f[i] += a[i];
         }
-        *reinterpret_cast<f32x4*>(static_cast<float*>(dX) + at) = f32x4{f[0], f[1], f[2], f[3]};
+        *reinterpret_cast<f32x4*>(static_cast<float*>(dX) + to) = f32x4{f[0], f[1], f[2], f[3]};
       } else {
         if (dX_add) {
-          const u32x2 a = *reinterpret_cast<const u32x2*>(static_cast<const uint16_t*>(dX_add) + at);
+          const u32x2 a = *reinterpret_cast<const u32x2*>(static_cast<const uint16_t*>(dX_add) + to);
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             f[i] += bf16_bits_to_f32((a[i >> 1] >> (16 * (i & 1))) & 0xFFFFu);
         }
-        *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(dX) + at) =
+        *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(dX) + to) =
             u32x2{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3])};
       }
     }
@@ -592,48 +607,31 @@ constexpr float kDwFirst = 0x1p60f;  // S before the first ds: any above 2^-45 l
 
 template <int DH, bool F32, int EW>
 __global__ __launch_bounds__(kDwWaves* kWave) void balance_dw_kernel(
-    const void* __restrict__ X, const u32x4* __restrict__ weights, int block_frags,
-    const HeadInfo* __restrict__ info, const float2* __restrict__ stats,
-    const uint8_t* __restrict__ mask, int64_t T, int Nh, int Ne, int groups, int splits,
-    float* __restrict__ part) {
+    const void* __restrict__ X, const float* __restrict__ W, const int32_t* __restrict__ counts,
+    const float2* __restrict__ stats, const float* __restrict__ dloss,
+    const uint8_t* __restrict__ mask, const float* dW_add, int64_t T, int Nh, int Ne, int groups,
+    int splits, float* dW, float* __restrict__ part) {
   constexpr int NX = F32 ? 2 : 1, SUB = kDwWaves / EW, kTokens = 32 * SUB;
-  constexpr int kUnits = DH / 8;                                  // 16-byte units of a row
-  constexpr int kPer = kTokens * kUnits / (kDwWaves * kWave);     // units per thread
-  constexpr int kRowB = DH * 2;
-  __shared__ __align__(16) uint8_t xs[2][NX][kTokens * kRowB];
+  constexpr int kUnits = DH / 8;                               // 16-byte units of a row
+  constexpr int kPer = kTokens * kUnits / (kDwWaves * kWave);  // units per thread
+  constexpr int kPiece = SUB * Tile<DH>::kBytes;
+  constexpr int kSums = (SUB - 1) * EW * 32 * DH * 4;  // of all but the first wavefront of a block
+  constexpr int kLds = 2 * NX * kPiece > kSums ? 2 * NX * kPiece : kSums;
+  __shared__ __align__(16) uint8_t xs[kLds];
   __shared__ __align__(16) float ms[2][kTokens], refs[2][kTokens], us[2][kTokens];
+  __shared__ long long totals[kDwWaves];
+  __shared__ uint32_t tops[kDwWaves];
   const int lane = lane_id(), g = lane >> 5, wave = threadIdx.x >> 6;
   // all groups of a (head, chunk) on one die, which then reads its tokens once
-  const int at = blockIdx.x / kXcds, group = at % groups;
-  const int64_t pair = (int64_t)(at / groups) * kXcds + blockIdx.x % kXcds;
+  const int slot = blockIdx.x / kXcds, group = slot % groups;
+  const int64_t pair = (int64_t)(slot / groups) * kXcds + blockIdx.x % kXcds;
   if (pair >= (int64_t)Nh * splits) return;
   const int h = (int)(pair % Nh), split = (int)(pair / Nh);
   const int nb = (Ne + 31) / 32, b = group * EW + wave % EW, sub = wave / EW;
-  const bool live = b < nb;
   const int e = 32 * b + (lane & 31);
-  const float down = head_down(info[h], nb);
-  const float f = live ? info[h].f[e] : 0.0f;
-  u32x4 w[2][DH / 16];
-  {
-    const u32x4* src = weights + ((int64_t)h * nb + (live ? b : 0)) * block_frags * 64;
-    // all blocks by the head's power of two
-    const _Float16 k = (_Float16)(info[h].down[live ? b : 0] / down);
-#pragma unroll
-    for (int q = 0; q < 2; ++q)
-#pragma unroll
-      for (int s = 0; s < DH / 16; ++s)
-        w[q][s] = __builtin_bit_cast(
-            u32x4, __builtin_bit_cast(f16x8, src[(q * (DH / 16) + s) * 64 + lane]) * k);
-  }
-  f32x16 dw[DH / 32];
-#pragma unroll
-  for (int i = 0; i < DH / 32; ++i) dw[i] = zero16();
-  float S = kDwFirst, fS = f * kDwFirst;  // S and f' S
+  const bool live = e < Ne;
   const int64_t tiles = (T + kTokens - 1) / kTokens;
   const int64_t begin = tiles * split / splits, end = tiles * (split + 1) / splits;
-  auto addr = [](int row, int col) {
-    return row * kRowB + swz_tr<kUnits>(col >> 3, row) * 16 + (col & 7) * 2;
-  };
   // a tile's rows and their stats on their way (nothing waits for the mask: what a token
   // that does not count has is read and dropped), then in LDS
   u32x4 raw[kPer][F32 ? 2 : 1];
@@ -654,6 +652,54 @@ __global__ __launch_bounds__(kDwWaves* kWave) void balance_dw_kernel(
       counted[i] = mask ? mask[t] : 1;
     }
   };
+  if (begin < end) fetch(begin);
+  // the lane's expert: f' and, scaled alike for all of the workgroup's experts, its weights
+  u32x4 w[2][DH / 16];
+  float f, down;
+  {
+    float v[DH / 16][8];
+    const float* src = W + ((int64_t)h * Ne + (live ? e : 0)) * DH + 8 * g;
+    uint32_t top = 0;
+#pragma unroll
+    for (int s = 0; s < DH / 16; ++s)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(src + 16 * s + 4 * k);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          v[s][4 * k + j] = live ? x[j] : 0.0f;
+          top = umax(top, bits_abs(v[s][4 * k + j]));
+        }
+      }
+    long long total = 0;
+    for (int i = threadIdx.x; i < Ne; i += kDwWaves * kWave) total += counts[(int64_t)h * Ne + i];
+    total = wave_sum(total);
+    top = wave_max(top);
+    if (lane == 0) {
+      totals[wave] = total;
+      tops[wave] = top;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kDwWaves; ++i) top = umax(top, tops[i]);
+    total = totals[0] + totals[1] + totals[2] + totals[3];
+    f = live ? excess(counts[(int64_t)h * Ne + e], Ne, total) : 0.0f;
+    const Pow2 scale = pow2_below_2_15(top);
+    down = scale.down;
+#pragma unroll
+    for (int s = 0; s < DH / 16; ++s) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[s][j] *= scale.up;
+      u32x4 o[2];
+      split8(v[s], o);
+      w[0][s] = o[0];
+      w[1][s] = o[1];
+    }
+  }
+  f32x16 dw[DH / 32];
+#pragma unroll
+  for (int i = 0; i < DH / 32; ++i) dw[i] = zero16();
+  float S = kDwFirst, fS = f * kDwFirst;  // S and f' S
   auto store = [&](int64_t tile, int buf) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
@@ -674,7 +720,8 @@ __global__ __launch_bounds__(kDwWaves* kWave) void balance_dw_kernel(
       split8(v, o);
 #pragma unroll
       for (int p = 0; p < NX; ++p)
-        *reinterpret_cast<u32x4*>(xs[buf][p] + addr(r, 8 * (unit % kUnits))) = o[p];
+        *reinterpret_cast<u32x4*>(xs + (buf * NX + p) * kPiece +
+                                  Tile<DH>::unit(r, unit % kUnits)) = o[p];
       if (unit % kUnits == 0) {
         // a token that does not count: p = exp2(-infinity) = 0
         ms[buf][r] = scale.down * down * kLog2e;
@@ -683,33 +730,20 @@ __global__ __launch_bounds__(kDwWaves* kWave) void balance_dw_kernel(
       }
     }
   };
-  // a lane's places in a tile, kept: the swizzle is linear (a row's mask repeats after 16
-  // rows), so the rest is an exclusive or or an offset
-  const int sub_row = 32 * sub;
-  const int z_at = addr(sub_row + (lane & 31), 8 * g);
-  int t_at[2];  // rows of k-step 0's two halves
-#pragma unroll
-  for (int k = 0; k < 2; ++k)
-    t_at[k] = addr(sub_row + 4 * g + 8 * k + ((lane & 15) >> 2),
-                   16 * ((lane >> 4) & 1) + 4 * (lane & 3));
-  if (begin < end) {
-    fetch(begin);
-    store(begin, 0);
-  }
+  const Tile<DH> at;
+  if (begin < end) store(begin, 0);
   for (int64_t tile = begin; tile < end; ++tile) {
     const int buf = (int)(tile - begin) & 1;
     __syncthreads();
     if (tile + 1 < end) fetch(tile + 1);
-    const uint8_t* xb = xs[buf][0];
-    constexpr int kPiece = kTokens * kRowB;
+    const uint8_t* xb = xs + buf * NX * kPiece + sub * Tile<DH>::kBytes;
     // scores of 32 tokens (rows) x 32 experts (lanes)
     f32x16 z = zero16();
 #pragma unroll
     for (int p = NX - 1; p >= 0; --p)
 #pragma unroll
       for (int s = 0; s < DH / 16; ++s) {
-        const u32x4 a =
-            *reinterpret_cast<const u32x4*>(xb + p * kPiece + (z_at ^ (s * 32)));
+        const u32x4 a = at.row_operand(xb + p * kPiece, s);
 #pragma unroll
         for (int q = 1 - p; q >= 0; --q) z = mfma32_f16(a, w[q][s], z);
       }
@@ -751,26 +785,56 @@ __global__ __launch_bounds__(kDwWaves* kWave) void balance_dw_kernel(
       for (int dt = 0; dt < DH / 32; ++dt)
 #pragma unroll
         for (int p = NX - 1; p >= 0; --p) {
-          const uint8_t* rows = xb + p * kPiece + 16 * s * kRowB;
-          const u32x2 lo = lds_read_tr16(rows + (t_at[0] ^ (dt * 64)));
-          const u32x2 hi = lds_read_tr16(rows + (t_at[1] ^ (dt * 64)));
-          const u32x4 a{lo[0], lo[1], hi[0], hi[1]};
+          const u32x4 a = at.col_operand(xb + p * kPiece, dt, s);
 #pragma unroll
           for (int q = 1 - p; q >= 0; --q) dw[dt] = mfma32_f16(a, ds[q], dw[dt]);
         }
     }
     if (tile + 1 < end) store(tile + 1, buf ^ 1);
   }
-  if (!live) return;
   const float k = 1.0f / S;
-  float* o = part + ((((int64_t)split * SUB + sub) * Nh + h) * nb * 32 + e) * DH;
 #pragma unroll
   for (int dt = 0; dt < DH / 32; ++dt)
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-      *reinterpret_cast<f32x4*>(o + 32 * dt + 8 * q + 4 * g) =
-          f32x4{dw[dt][4 * q] * k, dw[dt][4 * q + 1] * k, dw[dt][4 * q + 2] * k,
-                dw[dt][4 * q + 3] * k};
+    for (int v = 0; v < 16; ++v) dw[dt][v] *= k;
+  // the wavefronts that share a block, in order
+  if constexpr (SUB > 1) {
+    f32x4* sums = reinterpret_cast<f32x4*>(xs);
+    auto place = [&](int w, int i) { return ((w - EW) * (DH / 8) + i) * kWave + lane; };
+    __syncthreads();
+    if (sub > 0) {
+#pragma unroll
+      for (int i = 0; i < DH / 8; ++i)
+        sums[place(wave, i)] = f32x4{dw[i / 4][4 * (i % 4)], dw[i / 4][4 * (i % 4) + 1],
+                                     dw[i / 4][4 * (i % 4) + 2], dw[i / 4][4 * (i % 4) + 3]};
+    }
+    __syncthreads();
+    if (sub > 0) return;
+#pragma unroll
+    for (int r = 1; r < SUB; ++r)
+#pragma unroll
+      for (int i = 0; i < DH / 8; ++i) {
+        const f32x4 v = sums[place(wave + r * EW, i)];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) dw[i / 4][4 * (i % 4) + j] += v[j];
+      }
+  }
+  if (!live) return;
+  // one chunk: the result; else a partial one
+  const float c = splits == 1 ? dloss[h] * stats[T * Nh + h].x : 1.0f;
+  const int64_t row = ((int64_t)h * Ne + e) * DH;
+  float* o = splits == 1 ? dW + row : part + (((int64_t)split * Nh + h) * nb * 32 + e) * DH;
+#pragma unroll
+  for (int dt = 0; dt < DH / 32; ++dt)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int d = 32 * dt + 8 * q + 4 * g;
+      f32x4 v;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = dw[dt][4 * q + i] * c;
+      if (splits == 1 && dW_add) v += *reinterpret_cast<const f32x4*>(dW_add + row + d);
+      *reinterpret_cast<f32x4*>(o + d) = v;
+    }
 }
 
 // dW = dW_add + dloss / n times the sum of n partial results, in order.
@@ -820,27 +884,15 @@ static HeadInfo* head_info(const void* weights, int Nh, int dh, int Ne) {
 }
 
 hipError_t launch_balance_weights(const float* W, const int32_t* counts, int Nh, int dh, int Ne,
-                                  bool f32, bool backward, void* out, hipStream_t s) {
+                                  void* out, hipStream_t s) {
   const dim3 grid((unsigned)balance_blocks(Ne), (unsigned)Nh);
-#define MHL_WEIGHTS(DH, BACK)                                                                  \
-  hipLaunchKernelGGL((balance_weights_kernel<DH, BACK>), grid, dim3(256), 0, s, W, counts, Ne, \
-                     static_cast<u32x4*>(out), head_info(out, Nh, dh, Ne))
-  const int back = backward ? (f32 ? 2 : 1) : 0;
-  if (dh == 128) {
-    if (back == 2)
-      MHL_WEIGHTS(128, 2);
-    else if (back == 1)
-      MHL_WEIGHTS(128, 1);
-    else
-      MHL_WEIGHTS(128, 0);
-  } else {
-    if (back == 2)
-      MHL_WEIGHTS(64, 2);
-    else if (back == 1)
-      MHL_WEIGHTS(64, 1);
-    else
-      MHL_WEIGHTS(64, 0);
-  }
+#define MHL_WEIGHTS(DH)                                                                  \
+  hipLaunchKernelGGL((balance_weights_kernel<DH>), grid, dim3(256), 0, s, W, counts, Ne, \
+                     static_cast<uint8_t*>(out), head_info(out, Nh, dh, Ne))
+  if (dh == 128)
+    MHL_WEIGHTS(128);
+  else
+    MHL_WEIGHTS(64);
 #undef MHL_WEIGHTS
   return hipGetLastError();
 }
@@ -864,7 +916,7 @@ hipError_t launch_balance_loss(const void* X, const void* weights, const uint8_t
   const dim3 grid((unsigned)(Nh * balance_token_blocks(T)));
 #define MHL_LOSS(DH, F32)                                                                      \
   hipLaunchKernelGGL((balance_loss_kernel<DH, F32>), grid, dim3(kTokenWaves* kWave), 0, s, X,  \
-                     static_cast<const u32x4*>(weights), head_info(weights, Nh, dh, Ne), mask, \
+                     static_cast<const uint8_t*>(weights), head_info(weights, Nh, dh, Ne), mask, \
                      T, Nh, Ne, reinterpret_cast<float2*>(stats), part)
   MHL_BALANCE_TYPES(MHL_LOSS)
 #undef MHL_LOSS
@@ -886,24 +938,24 @@ hipError_t launch_balance_dx(const void* X, const void* weights, const float* st
   const dim3 grid((unsigned)(Nh * balance_token_blocks(T)));
 #define MHL_DX(DH, F32)                                                                       \
   hipLaunchKernelGGL((balance_dx_kernel<DH, F32>), grid, dim3(kTokenWaves* kWave), 0, s, X,   \
-                     static_cast<const u32x4*>(weights), head_info(weights, Nh, dh, Ne),      \
+                     static_cast<const uint8_t*>(weights), head_info(weights, Nh, dh, Ne),      \
                      reinterpret_cast<const float2*>(stats), dloss, mask, dX_add, T, Nh, Ne, dX)
   MHL_BALANCE_TYPES(MHL_DX)
 #undef MHL_DX
   return hipGetLastError();
 }
 
-hipError_t launch_balance_dw(const void* X, const void* weights, const float* stats,
-                             const uint8_t* mask, int64_t T, int Nh, int dh, int Ne, bool f32,
-                             float* part, hipStream_t s) {
+hipError_t launch_balance_dw(const void* X, const float* W, const int32_t* counts,
+                             const float* stats, const float* dloss, const uint8_t* mask,
+                             const float* dW_add, int64_t T, int Nh, int dh, int Ne, bool f32,
+                             float* dW, float* part, hipStream_t s) {
   const int ew = balance_dw_blocks(Ne), groups = (int)ceil_div(balance_blocks(Ne), ew);
   const int splits = (int)balance_splits(T, Nh, Ne);
   const dim3 grid((unsigned)(ceil_div((int64_t)Nh * splits, kXcds) * kXcds * groups));
 #define MHL_DW_EW(DH, F32, EW)                                                                  \
-  hipLaunchKernelGGL((balance_dw_kernel<DH, F32, EW>), grid, dim3(kDwWaves* kWave), 0, s, X,    \
-                     static_cast<const u32x4*>(weights), kFrags<DH, F32 ? 2 : 1>,               \
-                     head_info(weights, Nh, dh, Ne), reinterpret_cast<const float2*>(stats),    \
-                     mask, T, Nh, Ne, groups, splits, part)
+  hipLaunchKernelGGL((balance_dw_kernel<DH, F32, EW>), grid, dim3(kDwWaves* kWave), 0, s, X, W, \
+                     counts, reinterpret_cast<const float2*>(stats), dloss, mask, dW_add, T,    \
+                     Nh, Ne, groups, splits, dW, part)
 #define MHL_DW(DH, F32)         \
   do {                          \
     if (ew == 1)                \
@@ -925,7 +977,7 @@ hipError_t launch_balance_dw_sum(const float* part, const float* stats, const fl
   const int padded = 32 * balance_blocks(Ne), dh4 = dh / 4;
   const dim3 grid((unsigned)ceil_div(Ne * dh4, 256), (unsigned)Nh);
   hipLaunchKernelGGL(balance_dw_sum_kernel, grid, dim3(256), 0, s,
-                     reinterpret_cast<const f32x4*>(part), balance_parts(T, Nh, Ne),
+                     reinterpret_cast<const f32x4*>(part), balance_splits(T, Nh, Ne),
                      (int64_t)Nh * padded * dh4, reinterpret_cast<const float2*>(stats) + T * Nh,
                      dloss, reinterpret_cast<const f32x4*>(dW_add), Ne, padded, dh4,
                      reinterpret_cast<f32x4*>(dW));

@@ -69,15 +69,15 @@ hipError_t launch_adamw(const AdamLaunch& a, unsigned workgroups, hipStream_t s)
 hipError_t launch_expert_counts(const int32_t* idx, const uint8_t* mask, int64_t T, int Nh, int Ne,
                                 int k, int32_t* counts, hipStream_t s);
 
-// The balance loss and its gradient.  The router's weights are first laid out as
-// operands (up to two fp16 pieces for the scores and two, transposed, for dX), with a
-// head's other numbers (kBalanceHeadBytes) behind them.  The gradient's dW comes as
-// balance_parts partial results of Nh x (Ne rounded up to 32) x dh floats that
-// launch_balance_dw_sum adds in order.
+// The balance loss and its gradient.  The router's weights are first laid out as two
+// fp16 pieces, with a head's other numbers (kBalanceHeadBytes) behind them, for the
+// loss and dX.  dW comes from W itself, in balance_splits partial results of Nh x (Ne
+// rounded up to 32) x dh floats that launch_balance_dw_sum adds in order, or, where
+// there is one, at once.
 constexpr size_t kBalanceHeadBytes = 4 * (1024 + 32 + 32);
 inline int balance_blocks(int Ne) { return (int)ceil_div(Ne, 32); }
 inline size_t balance_operand_bytes(int Nh, int dh, int Ne) {
-  return (size_t)Nh * balance_blocks(Ne) * 32 * dh * 2 * 4;
+  return (size_t)Nh * balance_blocks(Ne) * 32 * dh * 2 * 2;
 }
 inline size_t balance_weight_bytes(int Nh, int dh, int Ne) {
   return balance_operand_bytes(Nh, dh, Ne) + Nh * kBalanceHeadBytes;
@@ -88,19 +88,16 @@ __host__ __device__ inline int64_t balance_token_blocks(int64_t T) {
 }
 // dW: blocks of experts that a workgroup's four wavefronts have (they share them out
 // over the tokens where there are fewer than three), and the chunks that the tokens
-// are cut into, so that there are about 1024 workgroups.
+// are cut into, of at least four tiles, so that there are about 1024 workgroups.
 inline int balance_dw_blocks(int Ne) { return Ne <= 32 ? 1 : Ne <= 64 ? 2 : 4; }
 inline int64_t balance_splits(int64_t T, int Nh, int Ne) {
   const int ew = balance_dw_blocks(Ne);
   const int64_t groups = Nh * ceil_div(balance_blocks(Ne), ew);
-  const int64_t want = ceil_div(1024, groups), most = ceil_div(T, 256 / ew);
+  const int64_t want = ceil_div(1024, groups), most = ceil_div(T, 4 * 32 * (4 / ew));
   return want < most ? want : most;
 }
-inline int64_t balance_parts(int64_t T, int Nh, int Ne) {
-  return balance_splits(T, Nh, Ne) * (4 / balance_dw_blocks(Ne));
-}
 hipError_t launch_balance_weights(const float* W, const int32_t* counts, int Nh, int dh, int Ne,
-                                  bool f32, bool backward, void* out, hipStream_t s);
+                                  void* out, hipStream_t s);
 hipError_t launch_balance_loss(const void* X, const void* weights, const uint8_t* mask, int64_t T,
                                int Nh, int dh, int Ne, bool f32, float* stats, double* part,
                                hipStream_t s);
@@ -110,9 +107,10 @@ hipError_t launch_balance_loss_sum(const double* part, const int32_t* counts, co
 hipError_t launch_balance_dx(const void* X, const void* weights, const float* stats,
                              const float* dloss, const uint8_t* mask, const void* dX_add, int64_t T,
                              int Nh, int dh, int Ne, bool f32, void* dX, hipStream_t s);
-hipError_t launch_balance_dw(const void* X, const void* weights, const float* stats,
-                             const uint8_t* mask, int64_t T, int Nh, int dh, int Ne, bool f32,
-                             float* part, hipStream_t s);
+hipError_t launch_balance_dw(const void* X, const float* W, const int32_t* counts,
+                             const float* stats, const float* dloss, const uint8_t* mask,
+                             const float* dW_add, int64_t T, int Nh, int dh, int Ne, bool f32,
+                             float* dW, float* part, hipStream_t s);
 hipError_t launch_balance_dw_sum(const float* part, const float* stats, const float* dloss,
                                  const float* dW_add, int64_t T, int Nh, int dh, int Ne, float* dW,
                                  hipStream_t s);
