@@ -791,7 +791,8 @@ mhlmoe_status mhlmoe_adamw(const mhlmoe_adamw_tensor *tensors, int n_tensors,
  * "proj_bwd" (the projection GEMMs of the latent layer), "rmsnorm",
  * "rmsnorm_bwd", "rmsnorm_dw", "quantize" and "gemm_scaled"; "layernorm",
  * "layernorm_bwd", "layernorm_dw", "expert_counts", "balance_weights",
- * "balance_loss", "balance_sum", "balance_dx", "balance_dw" and "adamw".
+ * "balance_loss", "balance_sum", "balance_dx", "balance_dw", "balance_dx_dw" and
+ * "adamw".
  *
  * mhlmoe_timing_enable(on)   start (on != 0) or stop recording; records
  *                            already taken are kept.

@@ -80,7 +80,8 @@ BalanceLayout balance_layout(int64_t T, int n_heads, int d_head, int n_experts, 
   L.weights = bump(cur, mhl::balance_weight_bytes(n_heads, d_head, n_experts));
   L.part = bump(cur, backward ? sizeof(float) * (size_t)mhl::balance_splits(T, n_heads, n_experts) *
                                     n_heads * mhl::balance_blocks(n_experts) * 32 * d_head
-                              : sizeof(double) * (size_t)n_heads * mhl::balance_token_blocks(T));
+                              : sizeof(double) * (size_t)n_heads *
+                                    mhl::balance_token_blocks(T, n_heads, n_experts));
   L.total = cur;
   return L;
 }
@@ -267,16 +268,18 @@ mhlmoe_status mhlmoe_balance_loss(const void* X, const float* W_router, const in
   MHL_TRY(check_workspace(workspace, workspace_bytes, L.total));
   void* weights = at<void>(workspace, L.weights);
   double* part = at<double>(workspace, L.part);
-  if (T > 0) {
+  const bool few = mhl::balance_few(T, n_heads, n_experts);
+  if (T > 0 && !few)
     MHL_TRY(run_kernel("balance_weights", stream, [&] {
       return mhl::launch_balance_weights(W_router, counts, n_heads, d_head, n_experts, weights,
                                          stream);
     }));
+  if (T > 0)
     MHL_TRY(run_kernel("balance_loss", stream, [&] {
-      return mhl::launch_balance_loss(X, weights, mask, T, n_heads, d_head, n_experts,
-                                      dtype == MHLMOE_F32, stats, part, stream);
+      return mhl::launch_balance_loss(X, W_router, weights, counts, mask, T, n_heads, d_head,
+                                      n_experts, dtype == MHLMOE_F32, stats, part, loss, stream);
     }));
-  }
+  if (mhl::balance_loss_at_once(T, n_heads, n_experts)) return MHLMOE_OK;
   return run_kernel("balance_sum", stream, [&] {
     return mhl::launch_balance_loss_sum(part, counts, mask, T, n_heads, n_experts, loss, stats,
                                         stream);
@@ -317,7 +320,13 @@ mhlmoe_status mhlmoe_balance_loss_backward(
   void* weights = at<void>(workspace, L.weights);
   float* part = at<float>(workspace, L.part);
   const bool f32 = dtype == MHLMOE_F32;
-  if (T > 0) {
+  if (T > 0 && mhl::balance_few(T, n_heads, n_experts)) {
+    MHL_TRY(run_kernel("balance_dx_dw", stream, [&] {
+      return mhl::launch_balance_bwd_few(X, W_router, counts, stats, dloss, mask, dX_add, dW_add, T,
+                                         n_heads, d_head, n_experts, f32, dX, dW_router, part,
+                                         stream);
+    }));
+  } else if (T > 0) {
     MHL_TRY(run_kernel("balance_weights", stream, [&] {
       return mhl::launch_balance_weights(W_router, counts, n_heads, d_head, n_experts, weights,
                                          stream);

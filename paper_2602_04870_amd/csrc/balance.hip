@@ -44,6 +44,37 @@ __global__ __launch_bounds__(kCountThreads) void counts_zero_kernel(int32_t* cou
   if (i < n) counts[i] = 0;
 }
 
+// All of head blockIdx.x's slots, where they are few: no launch in front to clear the
+// counts.
+constexpr int kCountAllThreads = 1024;
+constexpr int64_t kCountAllSlots = 1 << 15;
+
+__global__ __launch_bounds__(kCountAllThreads) void expert_counts_all_kernel(
+    const int32_t* __restrict__ idx, const uint8_t* __restrict__ mask, int64_t T, int Nh, int Ne,
+    int k, DivMagic by_k, int32_t* __restrict__ counts) {
+  __shared__ int32_t hist[kMaxExperts];
+  if ((int)threadIdx.x < Ne) hist[threadIdx.x] = 0;
+  __syncthreads();
+  const int n = (int)T * k;
+  for (int i0 = threadIdx.x; i0 < n; i0 += 8 * kCountAllThreads) {
+    int e[8];
+    uint8_t counted[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int i = i0 + j * kCountAllThreads < n ? i0 + j * kCountAllThreads : i0;
+      const int t = div_by_magic(i, by_k);
+      e[j] = idx[((int64_t)t * Nh + blockIdx.x) * k + (i - t * k)];
+      counted[j] = mask ? mask[t] : 1;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (i0 + j * kCountAllThreads < n && counted[j] && (unsigned)e[j] < (unsigned)Ne)
+        atomicAdd(&hist[e[j]], 1);
+  }
+  __syncthreads();
+  if ((int)threadIdx.x < Ne) counts[(int64_t)blockIdx.x * Ne + threadIdx.x] = hist[threadIdx.x];
+}
+
 // Head blockIdx.y, tokens [blockIdx.x tokens, + tokens): a histogram in LDS, added
 // to the counts (whole numbers, so in any order).
 __global__ __launch_bounds__(kCountThreads) void expert_counts_kernel(
@@ -325,6 +356,81 @@ struct XOperand {
   }
 };
 
+// One lane's operand of W, straight from memory: expert e, d = 16 s + 8 g + j, as two
+// pieces of w up, the power of two of its wavefront's (or workgroup's) experts.
+template <int DH>
+struct WOperand {
+  float v[DH / 16][8];
+  u32x4 w[2][DH / 16];
+  float down;
+  // Head's weights Wh; zeros past the last expert.  Returns the lane's largest magnitude.
+  __device__ __forceinline__ uint32_t load(const float* __restrict__ Wh, int e, int Ne, int g) {
+    const float* src = Wh + (int64_t)(e < Ne ? e : Ne - 1) * DH + 8 * g;
+    uint32_t top = 0;
+#pragma unroll
+    for (int s = 0; s < DH / 16; ++s)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(src + 16 * s + 4 * k);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          v[s][4 * k + j] = e < Ne ? x[j] : 0.0f;
+          top = umax(top, bits_abs(v[s][4 * k + j]));
+        }
+      }
+    return top;
+  }
+  __device__ __forceinline__ void split(uint32_t top) {
+    const Pow2 scale = pow2_below_2_15(top);
+    down = scale.down;
+#pragma unroll
+    for (int s = 0; s < DH / 16; ++s) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[s][j] *= scale.up;
+      u32x4 o[2];
+      split8(v[s], o);
+      w[0][s] = o[0];
+      w[1][s] = o[1];
+    }
+  }
+};
+
+// What a head's counts give: their sum, and whether the head has any; all of a
+// workgroup of THREADS.
+struct HeadCounts {
+  long long total;
+  uint32_t most, least;
+};
+template <int THREADS>
+__device__ __forceinline__ HeadCounts head_counts(const int32_t* __restrict__ counts, int Ne,
+                                                  long long* totals, uint32_t (*tops)[2]) {
+  const int wave = threadIdx.x >> 6;
+  HeadCounts c{0, 0u, 0xFFFFFFFFu};
+  for (int e = threadIdx.x; e < Ne; e += THREADS) {
+    const uint32_t n = (uint32_t)counts[e];
+    c.total += (int32_t)n;
+    c.most = umax(c.most, n);
+    c.least = n < c.least ? n : c.least;
+  }
+  c.total = wave_sum(c.total);
+  c.most = wave_max(c.most);
+  c.least = wave_max(~c.least);
+  if (lane_id() == 0) {
+    totals[wave] = c.total;
+    tops[wave][0] = c.most;
+    tops[wave][1] = c.least;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < THREADS / kWave; ++w) {
+    if (w != wave) c.total += totals[w];
+    c.most = umax(c.most, tops[w][0]);
+    c.least = umax(c.least, tops[w][1]);
+  }
+  c.least = ~c.least;
+  return c;
+}
+
 // Scores of 32 experts (rows) x 32 tokens (lanes), times both powers of two, small
 // products first.  e0: the block's first expert; rows past the last one have no weight.
 template <int DH, bool F32>
@@ -348,6 +454,68 @@ __device__ __forceinline__ f32x16 score_tile(const uint8_t* w, const Tile<DH>& a
   }
   return z;
 }
+
+// The same with the weights in registers.
+template <int DH, bool F32>
+__device__ __forceinline__ f32x16 score_tile(const WOperand<DH>& w, const XOperand<DH, F32>& x,
+                                             int e0, int Ne) {
+  f32x16 z = zero16();
+#pragma unroll
+  for (int q = 1; q >= 0; --q)
+#pragma unroll
+    for (int s = 0; s < DH / 16; ++s)
+#pragma unroll
+      for (int p = XOperand<DH, F32>::NX - 1; p >= 0; --p)
+        if (p + q <= 1) z = mfma32_f16(w.w[q][s], x.x[p][s], z);
+  if (e0 + 32 > Ne) {
+    asm volatile("");
+#pragma unroll
+    for (int v = 0; v < 16; ++v)
+      z[v] = e0 + mfma32_row(v, lane_id()) < Ne ? z[v] : -INFINITY;
+  }
+  return z;
+}
+
+// The running maximum (times log2 e), sum and weighted sum of a token's softmax.
+struct Running {
+  float M = -INFINITY, l = 0.0f, u = 0.0f;
+  // 32 experts' scores times m = log2 e over their power of two; f: their f'.
+  __device__ __forceinline__ void add(const f32x16& z, float m, const float* f, int g) {
+    float top = z[0];
+#pragma unroll
+    for (int v = 1; v < 16; ++v) top = fmaxf(top, z[v]);
+    const float Mn = fmaxf(M, top * m);
+    const float ref = Mn == -INFINITY ? 0.0f : Mn;
+    const float old = __builtin_amdgcn_exp2f(M - ref);
+    l *= old;
+    u *= old;
+    M = Mn;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const f32x4 f4 = *reinterpret_cast<const f32x4*>(f + 8 * q + 4 * g);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(z[4 * q + i], m, -ref));
+        l += p;
+        u = fmaf(p, f4[i], u);
+      }
+    }
+  }
+  // Together with another part of the token's experts, one of which has a weight.
+  __device__ __forceinline__ void join(float Mo, float lo, float uo) {
+    const float Mt = fmaxf(M, Mo);
+    const float a = __builtin_amdgcn_exp2f(M - Mt), c = __builtin_amdgcn_exp2f(Mo - Mt);
+    l = l * a + lo * c;
+    u = u * a + uo * c;
+    M = Mt;
+  }
+  __device__ __forceinline__ void join_halves() {
+    join(__shfl_xor(M, 32, kWave), __shfl_xor(l, 32, kWave), __shfl_xor(u, 32, kWave));
+  }
+  __device__ __forceinline__ float2 stats(bool ok) const {
+    return float2{ok ? (M + __builtin_amdgcn_logf(l)) * kLn2 : 0.0f, ok ? u / l : 0.0f};
+  }
+};
 
 // A block's weights to LDS, a KB per wavefront in turn, by DMA that the compiler does not
 // track: barrier_vm<0> before they are read.
@@ -385,43 +553,17 @@ __global__ __launch_bounds__(kTokenWaves* kWave) void balance_loss_kernel(
   for (int e = threadIdx.x; e < nb * 32; e += kTokenWaves * kWave) fex[e] = info[h].f[e];
   XOperand<DH, F32> x;
   x.load(X, (t < T ? t : T - 1) * Nh + h, ok, g);
-  float M = -INFINITY, l = 0.0f, u = 0.0f;  // maximum (times log2 e), sum, weighted sum
+  Running run;
   for (int b = 0; b < nb; ++b) {
     const float m = x.down * info[h].down[b] * kLog2e;
     barrier_vm<0>();
     if (b + 1 < nb) fetch_block<DH>(rsrc, b + 1, w[(b + 1) & 1]);
-    const f32x16 z = score_tile<DH, F32>(w[b & 1], at, x, 32 * b, Ne);
-    float top = z[0];
-#pragma unroll
-    for (int v = 1; v < 16; ++v) top = fmaxf(top, z[v]);
-    const float Mn = fmaxf(M, top * m);
-    const float ref = Mn == -INFINITY ? 0.0f : Mn;
-    const float old = __builtin_amdgcn_exp2f(M - ref);
-    l *= old;
-    u *= old;
-    M = Mn;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const f32x4 f = *reinterpret_cast<const f32x4*>(&fex[32 * b + 8 * q + 4 * g]);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(z[4 * q + i], m, -ref));
-        l += p;
-        u = fmaf(p, f[i], u);
-      }
-    }
+    run.add(score_tile<DH, F32>(w[b & 1], at, x, 32 * b, Ne), m, fex + 32 * b, g);
   }
-  // the two lanes of a token
-  const float Mo = __shfl_xor(M, 32, kWave), lo = __shfl_xor(l, 32, kWave),
-              uo = __shfl_xor(u, 32, kWave);
-  const float Mt = fmaxf(M, Mo);
-  const float a = __builtin_amdgcn_exp2f(M - Mt), c = __builtin_amdgcn_exp2f(Mo - Mt);
-  l = l * a + lo * c;
-  u = u * a + uo * c;
-  const float lse = ok ? (Mt + __builtin_amdgcn_logf(l)) * kLn2 : 0.0f;
-  const float share = ok ? u / l : 0.0f;
-  if (g == 0 && t < T) stats[t * Nh + h] = float2{lse, share};
-  double sum = g == 0 ? (double)share : 0.0;
+  run.join_halves();
+  const float2 st = run.stats(ok);
+  if (g == 0 && t < T) stats[t * Nh + h] = st;
+  double sum = g == 0 ? (double)st.y : 0.0;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) sum += __shfl_xor(sum, d, kWave);
   if (lane == 0) loss[wave] = sum;
@@ -429,7 +571,92 @@ __global__ __launch_bounds__(kTokenWaves* kWave) void balance_loss_kernel(
   if (threadIdx.x == 0) {
 #pragma unroll
     for (int i = 1; i < kTokenWaves; ++i) sum += loss[i];
-    part[h * balance_token_blocks(T) + tb] = sum;
+    part[h * ceil_div(T, kBalanceTokens) + tb] = sum;
+  }
+}
+
+// The loss where there are few tokens: eight wavefronts, EG of them for the blocks of
+// experts in turn, the others for as many groups of 32 tokens; weights straight from
+// memory, no launch in front.  A head's tokens in one workgroup: also its loss, with no
+// launch behind.
+constexpr int kFewThreads = kBalanceFewWaves * kWave;
+
+template <int DH, bool F32, int EG>
+__global__ __launch_bounds__(kFewThreads) void balance_loss_few_kernel(
+    const void* __restrict__ X, const float* __restrict__ W, const int32_t* __restrict__ counts,
+    const uint8_t* __restrict__ mask, int64_t T, int Nh, int Ne, float2* __restrict__ stats,
+    double* __restrict__ part, float* __restrict__ loss) {
+  constexpr int TG = kBalanceFewWaves / EG;
+  __shared__ __align__(16) float fex[kMaxExperts];
+  __shared__ long long totals[kBalanceFewWaves];
+  __shared__ uint32_t tops[kBalanceFewWaves][2];
+  __shared__ float runs[EG][3][TG * 32];
+  __shared__ double sums[TG];
+  __shared__ int tokens[TG];
+  const int h = blockIdx.x % Nh, lane = lane_id(), g = lane >> 5, wave = threadIdx.x >> 6;
+  const int eg = wave % EG, tg = wave / EG;
+  const int64_t tb = blockIdx.x / Nh, t = tb * (TG * 32) + tg * 32 + (lane & 31);
+  const int64_t near = t < T ? t : T - 1;
+  const bool counted = mask ? mask[near] != 0 : true;
+  const float* Wh = W + (int64_t)h * Ne * DH;
+  WOperand<DH> w;
+  uint32_t top = w.load(Wh, 32 * eg + (lane & 31), Ne, g);
+  const HeadCounts c = head_counts<kFewThreads>(counts + (int64_t)h * Ne, Ne, totals, tops);
+  for (int e = threadIdx.x; e < ((Ne + 31) & ~31); e += kFewThreads)
+    fex[e] = e < Ne ? excess(counts[(int64_t)h * Ne + e], Ne, c.total) : 0.0f;
+  const bool ok = t < T && counted;
+  XOperand<DH, F32> x;
+  x.load(X, near * Nh + h, ok, g);
+  __syncthreads();
+  Running run;
+  for (int b = eg; b * 32 < Ne; b += EG) {
+    w.split(wave_max(top));
+    const float m = x.down * w.down * kLog2e;
+    const f32x16 z = score_tile<DH, F32>(w, x, 32 * b, Ne);
+    if ((b + EG) * 32 < Ne) top = w.load(Wh, 32 * (b + EG) + (lane & 31), Ne, g);
+    run.add(z, m, fex + 32 * b, g);
+  }
+  // (a wavefront without experts has M = -infinity, which join_halves would make NaN)
+  if (eg * 32 < Ne) run.join_halves();
+  if constexpr (EG > 1) {
+    if (g == 0) {
+      runs[eg][0][tg * 32 + lane] = run.M;
+      runs[eg][1][tg * 32 + lane] = run.l;
+      runs[eg][2][tg * 32 + lane] = run.u;
+    }
+    __syncthreads();
+    if (eg == 0) {
+      const int at = tg * 32 + (lane & 31);
+#pragma unroll
+      for (int i = 1; i < EG; ++i) run.join(runs[i][0][at], runs[i][1][at], runs[i][2][at]);
+    }
+  }
+  if (eg == 0) {
+    const float2 st = run.stats(ok);
+    if (g == 0 && t < T) stats[t * Nh + h] = st;
+    double sum = g == 0 ? (double)st.y : 0.0;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) sum += __shfl_xor(sum, d, kWave);
+    if (lane == 0) sums[tg] = sum;
+    const int n = __popcll(__ballot(ok && g == 0));
+    if (lane == 0) tokens[tg] = n;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    double sum = sums[0];
+    int n = tokens[0];
+#pragma unroll
+    for (int i = 1; i < TG; ++i) {
+      sum += sums[i];
+      n += tokens[i];
+    }
+    if (T > TG * 32) {
+      part[h * ceil_div(T, TG * 32) + tb] = sum;
+    } else {
+      const double m = n > 0 ? (double)n : 1.0;
+      loss[h] = c.total > 0 ? (float)(1.0 + sum / m) : 0.0f;
+      stats[T * Nh + h] = float2{(float)(1.0 / m), 0.0f};
+    }
   }
 }
 
@@ -497,6 +724,59 @@ __device__ __forceinline__ void split_ds(const f32x16& ds, int s, u32x4 (&out)[N
   split8(f, out);
 }
 
+// dX^T += W^T ds of 32 experts x 32 tokens.
+template <int DH, int NP>
+__device__ __forceinline__ void add_dx(const f32x16& z, const uint8_t* w, const Tile<DH>& at,
+                                       f32x16 (&dx)[DH / 32]) {
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    u32x4 ds[NP];
+    split_ds(z, s, ds);
+#pragma unroll
+    for (int dt = 0; dt < DH / 32; ++dt)
+#pragma unroll
+      for (int q = NP - 1; q >= 0; --q) {
+        const u32x4 a = at.col_operand(w + q * Tile<DH>::kBytes, dt, s);
+#pragma unroll
+        for (int p = NP - 1 - q; p >= 0; --p) dx[dt] = mfma32_f16(a, ds[p], dx[dt]);
+      }
+  }
+}
+
+// A lane's part of its token's row of dX, times c, added to dX_add's.  c = 0 is for a
+// token that does not count, whose sums are dropped.
+template <int DH, bool F32>
+__device__ __forceinline__ void store_dx(const f32x16 (&dx)[DH / 32], float c, int64_t row,
+                                         const void* dX_add, void* dX) {
+  const int g = lane_id() >> 5;
+#pragma unroll
+  for (int dt = 0; dt < DH / 32; ++dt)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int64_t to = row * DH + 32 * dt + 8 * q + 4 * g;
+      float f[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) f[i] = c != 0.0f ? dx[dt][4 * q + i] * c : 0.0f;
+      if (F32) {
+        if (dX_add) {
+          const f32x4 a = *reinterpret_cast<const f32x4*>(static_cast<const float*>(dX_add) + to);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) f[i] += a[i];
+        }
+        *reinterpret_cast<f32x4*>(static_cast<float*>(dX) + to) = f32x4{f[0], f[1], f[2], f[3]};
+      } else {
+        if (dX_add) {
+          const u32x2 a = *reinterpret_cast<const u32x2*>(static_cast<const uint16_t*>(dX_add) + to);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            f[i] += bf16_bits_to_f32((a[i >> 1] >> (16 * (i & 1))) & 0xFFFFu);
+        }
+        *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(dX) + to) =
+            u32x2{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3])};
+      }
+    }
+}
+
 // The largest of the head's blocks' powers down (2^-K), in every lane.
 __device__ __forceinline__ float head_down(const HeadInfo& info, int nb) {
   float d = lane_id() < nb ? info.down[lane_id()] : 0.0f;
@@ -549,47 +829,9 @@ __global__ __launch_bounds__(kTokenWaves* kWave) void balance_dx_kernel(
       for (int i = 0; i < 4; ++i)
         z[4 * q + i] = __builtin_amdgcn_exp2f(fmaf(z[4 * q + i], m, -ref)) * (f[i] - u);
     }
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      u32x4 ds[NP];
-      split_ds(z, s, ds);
-#pragma unroll
-      for (int dt = 0; dt < DH / 32; ++dt)
-#pragma unroll
-        for (int q = NP - 1; q >= 0; --q) {
-          const u32x4 a = at.col_operand(wb + q * Tile<DH>::kBytes, dt, s);
-#pragma unroll
-          for (int p = NP - 1 - q; p >= 0; --p) dx[dt] = mfma32_f16(a, ds[p], dx[dt]);
-        }
-    }
+    add_dx<DH, NP>(z, wb, at, dx);
   }
-  if (t >= T) return;
-#pragma unroll
-  for (int dt = 0; dt < DH / 32; ++dt)
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int64_t to = row * DH + 32 * dt + 8 * q + 4 * g;
-      float f[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) f[i] = ok ? dx[dt][4 * q + i] * c : 0.0f;
-      if (F32) {
-        if (dX_add) {
-          const f32x4 a = *reinterpret_cast<const f32x4*>(static_cast<const float*>(dX_add) + to);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) f[i] += a[i];
-        }
-        *reinterpret_cast<f32x4*>(static_cast<float*>(dX) + to) = f32x4{f[0], f[1], f[2], f[3]};
-      } else {
-        if (dX_add) {
-          const u32x2 a = *reinterpret_cast<const u32x2*>(static_cast<const uint16_t*>(dX_add) + to);
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            f[i] += bf16_bits_to_f32((a[i >> 1] >> (16 * (i & 1))) & 0xFFFFu);
-        }
-        *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(dX) + to) =
-            u32x2{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3])};
-      }
-    }
+  if (t < T) store_dx<DH, F32>(dx, ok ? c : 0.0f, row, dX_add, dX);
 }
 
 // ---------------------------------------------------------------------------
@@ -606,25 +848,52 @@ constexpr int kDwWaves = 4;
 constexpr float kDwFirst = 0x1p60f;  // S before the first ds: any above 2^-45 lowers it
 
 template <int DH, bool F32, int EW>
-__global__ __launch_bounds__(kDwWaves* kWave) void balance_dw_kernel(
-    const void* __restrict__ X, const float* __restrict__ W, const int32_t* __restrict__ counts,
-    const float2* __restrict__ stats, const float* __restrict__ dloss,
-    const uint8_t* __restrict__ mask, const float* dW_add, int64_t T, int Nh, int Ne, int groups,
-    int splits, float* dW, float* __restrict__ part) {
+struct DwShared {
+  static constexpr int NX = F32 ? 2 : 1, SUB = kDwWaves / EW;
+  static constexpr int kTiles = 2 * NX * SUB * Tile<DH>::kBytes;
+  static constexpr int kSums = (SUB - 1) * EW * 32 * DH * 4;  // of all but a block's first wavefront
+  __align__(16) uint8_t xs[kTiles > kSums ? kTiles : kSums];
+  __align__(16) float ms[2][32 * SUB], refs[2][32 * SUB], us[2][32 * SUB];
+  long long totals[kDwWaves];
+  uint32_t tops[kDwWaves][2];
+};
+
+struct DwArgs {
+  const void* X;
+  const float* W;
+  const int32_t* counts;
+  const float2* stats;
+  const float* dloss;
+  const uint8_t* mask;
+  const float* dW_add;
+  int64_t T;
+  int Nh, Ne, groups, splits;
+  float *dW, *part;
+};
+
+template <int DH, bool F32, int EW>
+__device__ __forceinline__ void balance_dw(const DwArgs& a, unsigned block,
+                                           DwShared<DH, F32, EW>& sm) {
   constexpr int NX = F32 ? 2 : 1, SUB = kDwWaves / EW, kTokens = 32 * SUB;
   constexpr int kUnits = DH / 8;                               // 16-byte units of a row
   constexpr int kPer = kTokens * kUnits / (kDwWaves * kWave);  // units per thread
   constexpr int kPiece = SUB * Tile<DH>::kBytes;
-  constexpr int kSums = (SUB - 1) * EW * 32 * DH * 4;  // of all but the first wavefront of a block
-  constexpr int kLds = 2 * NX * kPiece > kSums ? 2 * NX * kPiece : kSums;
-  __shared__ __align__(16) uint8_t xs[kLds];
-  __shared__ __align__(16) float ms[2][kTokens], refs[2][kTokens], us[2][kTokens];
-  __shared__ long long totals[kDwWaves];
-  __shared__ uint32_t tops[kDwWaves];
+  const void* __restrict__ X = a.X;
+  const float* __restrict__ W = a.W;
+  const int32_t* __restrict__ counts = a.counts;
+  const float2* __restrict__ stats = a.stats;
+  const uint8_t* __restrict__ mask = a.mask;
+  const float* dW_add = a.dW_add;
+  const int64_t T = a.T;
+  const int Nh = a.Nh, Ne = a.Ne, groups = a.groups, splits = a.splits;
+  uint8_t* const xs = sm.xs;
+  auto& ms = sm.ms;
+  auto& refs = sm.refs;
+  auto& us = sm.us;
   const int lane = lane_id(), g = lane >> 5, wave = threadIdx.x >> 6;
   // all groups of a (head, chunk) on one die, which then reads its tokens once
-  const int slot = blockIdx.x / kXcds, group = slot % groups;
-  const int64_t pair = (int64_t)(slot / groups) * kXcds + blockIdx.x % kXcds;
+  const int slot = block / kXcds, group = slot % groups;
+  const int64_t pair = (int64_t)(slot / groups) * kXcds + block % kXcds;
   if (pair >= (int64_t)Nh * splits) return;
   const int h = (int)(pair % Nh), split = (int)(pair / Nh);
   const int nb = (Ne + 31) / 32, b = group * EW + wave % EW, sub = wave / EW;
@@ -654,48 +923,20 @@ __global__ __launch_bounds__(kDwWaves* kWave) void balance_dw_kernel(
   };
   if (begin < end) fetch(begin);
   // the lane's expert: f' and, scaled alike for all of the workgroup's experts, its weights
-  u32x4 w[2][DH / 16];
-  float f, down;
+  WOperand<DH> w;
+  const uint32_t top = w.load(W + (int64_t)h * Ne * DH, e, Ne, g);
+  const HeadCounts hc = head_counts<kDwWaves * kWave>(counts + (int64_t)h * Ne, Ne, sm.totals, sm.tops);
+  const float f = live ? excess(counts[(int64_t)h * Ne + e], Ne, hc.total) : 0.0f;
   {
-    float v[DH / 16][8];
-    const float* src = W + ((int64_t)h * Ne + (live ? e : 0)) * DH + 8 * g;
-    uint32_t top = 0;
-#pragma unroll
-    for (int s = 0; s < DH / 16; ++s)
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const f32x4 x = *reinterpret_cast<const f32x4*>(src + 16 * s + 4 * k);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          v[s][4 * k + j] = live ? x[j] : 0.0f;
-          top = umax(top, bits_abs(v[s][4 * k + j]));
-        }
-      }
-    long long total = 0;
-    for (int i = threadIdx.x; i < Ne; i += kDwWaves * kWave) total += counts[(int64_t)h * Ne + i];
-    total = wave_sum(total);
-    top = wave_max(top);
-    if (lane == 0) {
-      totals[wave] = total;
-      tops[wave] = top;
-    }
+    uint32_t most = wave_max(top);
+    __syncthreads();  // the readers of tops
+    if (lane == 0) sm.tops[wave][0] = most;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kDwWaves; ++i) top = umax(top, tops[i]);
-    total = totals[0] + totals[1] + totals[2] + totals[3];
-    f = live ? excess(counts[(int64_t)h * Ne + e], Ne, total) : 0.0f;
-    const Pow2 scale = pow2_below_2_15(top);
-    down = scale.down;
-#pragma unroll
-    for (int s = 0; s < DH / 16; ++s) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[s][j] *= scale.up;
-      u32x4 o[2];
-      split8(v[s], o);
-      w[0][s] = o[0];
-      w[1][s] = o[1];
-    }
+    for (int i = 0; i < kDwWaves; ++i) most = umax(most, sm.tops[i][0]);
+    w.split(most);
   }
+  const float down = w.down;
   f32x16 dw[DH / 32];
 #pragma unroll
   for (int i = 0; i < DH / 32; ++i) dw[i] = zero16();
@@ -745,7 +986,7 @@ __global__ __launch_bounds__(kDwWaves* kWave) void balance_dw_kernel(
       for (int s = 0; s < DH / 16; ++s) {
         const u32x4 a = at.row_operand(xb + p * kPiece, s);
 #pragma unroll
-        for (int q = 1 - p; q >= 0; --q) z = mfma32_f16(a, w[q][s], z);
+        for (int q = 1 - p; q >= 0; --q) z = mfma32_f16(a, w.w[q][s], z);
       }
     float top = 0.0f;
 #pragma unroll
@@ -821,9 +1062,9 @@ __global__ __launch_bounds__(kDwWaves* kWave) void balance_dw_kernel(
   }
   if (!live) return;
   // one chunk: the result; else a partial one
-  const float c = splits == 1 ? dloss[h] * stats[T * Nh + h].x : 1.0f;
+  const float c = splits == 1 ? a.dloss[h] * stats[T * Nh + h].x : 1.0f;
   const int64_t row = ((int64_t)h * Ne + e) * DH;
-  float* o = splits == 1 ? dW + row : part + (((int64_t)split * Nh + h) * nb * 32 + e) * DH;
+  float* o = splits == 1 ? a.dW + row : a.part + (((int64_t)split * Nh + h) * nb * 32 + e) * DH;
 #pragma unroll
   for (int dt = 0; dt < DH / 32; ++dt)
 #pragma unroll
@@ -835,6 +1076,140 @@ __global__ __launch_bounds__(kDwWaves* kWave) void balance_dw_kernel(
       if (splits == 1 && dW_add) v += *reinterpret_cast<const f32x4*>(dW_add + row + d);
       *reinterpret_cast<f32x4*>(o + d) = v;
     }
+}
+
+template <int DH, bool F32, int EW>
+__global__ __launch_bounds__(kDwWaves* kWave) void balance_dw_kernel(const DwArgs a) {
+  __shared__ DwShared<DH, F32, EW> sm;
+  balance_dw<DH, F32, EW>(a, blockIdx.x, sm);
+}
+
+// ---------------------------------------------------------------------------
+// The gradient where there are few tokens, in one launch: the first workgroups make dX,
+// the others dW.  For dX four wavefronts, EG of them for the blocks of experts in turn,
+// the others for as many groups of 32 tokens; weights straight from memory, and through
+// a Tile of the wavefront's own to be read transposed.  The products add up in the unit
+// of the largest weights so far (down), to which both are lowered when larger ones come.
+// ---------------------------------------------------------------------------
+constexpr int kDxFewWaves = kDwWaves;
+
+template <int DH, bool F32, int EG>
+struct DxFewShared {
+  static constexpr int NP = F32 ? 2 : 1;
+  static constexpr int kTiles = kDxFewWaves * NP * Tile<DH>::kBytes;
+  static constexpr int kSums = (kDxFewWaves - kDxFewWaves / EG) * 32 * DH * 4;
+  __align__(16) uint8_t ws[kTiles > kSums ? kTiles : kSums];
+  __align__(16) float fex[kMaxExperts];
+  long long totals[kDxFewWaves];
+  uint32_t tops[kDxFewWaves][2];
+};
+
+template <int DH, bool F32, int EG>
+__device__ __forceinline__ void balance_dx_few(const DwArgs& a, const void* dX_add, void* dX,
+                                               unsigned block, DxFewShared<DH, F32, EG>& sm) {
+  constexpr int NP = F32 ? 2 : 1, TG = kDxFewWaves / EG;
+  const int64_t T = a.T;
+  const int Nh = a.Nh, Ne = a.Ne;
+  const int h = block % Nh, lane = lane_id(), g = lane >> 5, wave = threadIdx.x >> 6;
+  const int eg = wave % EG, tg = wave / EG;
+  const int64_t t = (int64_t)(block / Nh) * (TG * 32) + tg * 32 + (lane & 31);
+  const int64_t near = t < T ? t : T - 1;
+  const bool counted = a.mask ? a.mask[near] != 0 : true;
+  const float* Wh = a.W + (int64_t)h * Ne * DH;
+  const int32_t* counts = a.counts + (int64_t)h * Ne;
+  WOperand<DH> w;
+  uint32_t top = w.load(Wh, 32 * eg + (lane & 31), Ne, g);
+  float2 st = a.stats[near * Nh + h];
+  const HeadCounts hc = head_counts<kDxFewWaves * kWave>(counts, Ne, sm.totals, sm.tops);
+  for (int e = threadIdx.x; e < ((Ne + 31) & ~31); e += kDxFewWaves * kWave)
+    sm.fex[e] = e < Ne ? excess(counts[e], Ne, hc.total) : 0.0f;
+  const float F = ds_exponent(hc.most, hc.least, Ne, hc.total);
+  const bool ok = t < T && counted;
+  if (!ok) st = float2{INFINITY, 0.0f};  // p = exp2(-infinity) = 0
+  XOperand<DH, F32> x;
+  x.load(a.X, near * Nh + h, ok, g);
+  const float lse = st.x * kLog2e - F;
+  f32x16 dx[DH / 32];
+#pragma unroll
+  for (int i = 0; i < DH / 32; ++i) dx[i] = zero16();
+  const Tile<DH> at;
+  uint8_t* const ws = sm.ws + wave * NP * Tile<DH>::kBytes;
+  float down = 0x1p-126f;
+  __syncthreads();
+  for (int b = eg; b * 32 < Ne; b += EG) {
+    w.split(wave_max(top));
+    const float down_b = uniform(w.down);
+    wave_lds_order();  // the readers of the block before
+#pragma unroll
+    for (int q = 0; q < NP; ++q)
+#pragma unroll
+      for (int s = 0; s < DH / 16; ++s)
+        *reinterpret_cast<u32x4*>(ws + q * Tile<DH>::kBytes + (at.rows ^ (s * 32))) = w.w[q][s];
+    wave_lds_order();
+    const float m = x.down * down_b * kLog2e;
+    f32x16 z = score_tile<DH, F32>(w, x, 32 * b, Ne);
+    if ((b + EG) * 32 < Ne) top = w.load(Wh, 32 * (b + EG) + (lane & 31), Ne, g);
+    if (down_b > down) {
+      const float k = down / down_b;
+      down = down_b;
+#pragma unroll
+      for (int i = 0; i < DH / 32; ++i)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) dx[i][v] *= k;
+    }
+    const float ref = lse - (log2_of(down_b) - log2_of(down));
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const f32x4 f = *reinterpret_cast<const f32x4*>(&sm.fex[32 * b + 8 * q + 4 * g]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        z[4 * q + i] = __builtin_amdgcn_exp2f(fmaf(z[4 * q + i], m, -ref)) * (f[i] - st.y);
+    }
+    add_dx<DH, NP>(z, ws, at, dx);
+  }
+  const float c = a.dloss[h] * a.stats[T * Nh + h].x * __builtin_amdgcn_ldexpf(down, -(int)F);
+#pragma unroll
+  for (int i = 0; i < DH / 32; ++i)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) dx[i][v] *= c;
+  if constexpr (EG > 1) {
+    // the wavefronts that share tokens, in order
+    f32x4* sums = reinterpret_cast<f32x4*>(sm.ws);
+    auto place = [&](int e, int i) { return (((e - 1) * TG + tg) * (DH / 8) + i) * kWave + lane; };
+    __syncthreads();
+    if (eg > 0) {
+#pragma unroll
+      for (int i = 0; i < DH / 8; ++i)
+        sums[place(eg, i)] = f32x4{dx[i / 4][4 * (i % 4)], dx[i / 4][4 * (i % 4) + 1],
+                                   dx[i / 4][4 * (i % 4) + 2], dx[i / 4][4 * (i % 4) + 3]};
+    }
+    __syncthreads();
+    if (eg > 0) return;
+#pragma unroll
+    for (int r = 1; r < EG; ++r)
+#pragma unroll
+      for (int i = 0; i < DH / 8; ++i) {
+        const f32x4 v = sums[place(r, i)];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) dx[i / 4][4 * (i % 4) + j] += v[j];
+      }
+  }
+  if (t < T) store_dx<DH, F32>(dx, ok ? 1.0f : 0.0f, t * Nh + h, dX_add, dX);
+}
+
+template <int DH, bool F32, int EG>
+__global__ __launch_bounds__(kDwWaves* kWave) void balance_bwd_few_kernel(
+    const DwArgs a, const void* dX_add, void* dX, unsigned dx_blocks) {
+  // as many blocks of experts per workgroup of dW as wavefronts share them for dX
+  __shared__ union Shared {
+    DxFewShared<DH, F32, EG> dx;
+    DwShared<DH, F32, EG> dw;
+    __device__ Shared() {}
+  } sm;
+  if (blockIdx.x < dx_blocks)
+    balance_dx_few<DH, F32, EG>(a, dX_add, dX, blockIdx.x, sm.dx);
+  else
+    balance_dw<DH, F32, EG>(a, blockIdx.x - dx_blocks, sm.dw);
 }
 
 // dW = dW_add + dloss / n times the sum of n partial results, in order.
@@ -861,10 +1236,14 @@ __global__ __launch_bounds__(256) void balance_dw_sum_kernel(
 
 hipError_t launch_expert_counts(const int32_t* idx, const uint8_t* mask, int64_t T, int Nh, int Ne,
                                 int k, int32_t* counts, hipStream_t s) {
+  if (T * k <= kCountAllSlots) {
+    hipLaunchKernelGGL(expert_counts_all_kernel, dim3((unsigned)Nh), dim3(kCountAllThreads), 0, s,
+                       idx, mask, T, Nh, Ne, k, div_magic(k), counts);
+    return hipGetLastError();
+  }
   const int n = Nh * Ne;
   hipLaunchKernelGGL(counts_zero_kernel, dim3((unsigned)ceil_div(n, kCountThreads)),
                      dim3(kCountThreads), 0, s, counts, n);
-  if (T == 0) return hipGetLastError();
   // about 1024 workgroups, of at least 128 tokens
   int64_t blocks = ceil_div(1024, Nh);
   if (blocks > ceil_div(T, 128)) blocks = ceil_div(T, 128);
@@ -910,14 +1289,37 @@ hipError_t launch_balance_weights(const float* W, const int32_t* counts, int Nh,
       CALL(64, false);          \
   }
 
-hipError_t launch_balance_loss(const void* X, const void* weights, const uint8_t* mask, int64_t T,
-                               int Nh, int dh, int Ne, bool f32, float* stats, double* part,
+hipError_t launch_balance_loss(const void* X, const float* W, const void* weights,
+                               const int32_t* counts, const uint8_t* mask, int64_t T, int Nh,
+                               int dh, int Ne, bool f32, float* stats, double* part, float* loss,
                                hipStream_t s) {
-  const dim3 grid((unsigned)(Nh * balance_token_blocks(T)));
+  const dim3 grid((unsigned)(Nh * balance_token_blocks(T, Nh, Ne)));
+  float2* st = reinterpret_cast<float2*>(stats);
+  if (balance_few(T, Nh, Ne)) {
+    const int eg = balance_few_groups(Ne, kBalanceFewWaves);
+#define MHL_LOSS_EG(DH, F32, EG)                                                                 \
+  hipLaunchKernelGGL((balance_loss_few_kernel<DH, F32, EG>), grid, dim3(kFewThreads), 0, s, X,   \
+                     W, counts, mask, T, Nh, Ne, st, part, loss)
+#define MHL_LOSS(DH, F32)          \
+  do {                             \
+    if (eg == 1)                   \
+      MHL_LOSS_EG(DH, F32, 1);     \
+    else if (eg == 2)              \
+      MHL_LOSS_EG(DH, F32, 2);     \
+    else if (eg == 4)              \
+      MHL_LOSS_EG(DH, F32, 4);     \
+    else                           \
+      MHL_LOSS_EG(DH, F32, 8);     \
+  } while (0)
+    MHL_BALANCE_TYPES(MHL_LOSS)
+#undef MHL_LOSS
+#undef MHL_LOSS_EG
+    return hipGetLastError();
+  }
 #define MHL_LOSS(DH, F32)                                                                      \
   hipLaunchKernelGGL((balance_loss_kernel<DH, F32>), grid, dim3(kTokenWaves* kWave), 0, s, X,  \
                      static_cast<const uint8_t*>(weights), head_info(weights, Nh, dh, Ne), mask, \
-                     T, Nh, Ne, reinterpret_cast<float2*>(stats), part)
+                     T, Nh, Ne, st, part)
   MHL_BALANCE_TYPES(MHL_LOSS)
 #undef MHL_LOSS
   return hipGetLastError();
@@ -927,7 +1329,7 @@ hipError_t launch_balance_loss_sum(const double* part, const int32_t* counts, co
                                    int64_t T, int Nh, int Ne, float* loss, float* stats,
                                    hipStream_t s) {
   hipLaunchKernelGGL(balance_loss_sum_kernel, dim3((unsigned)Nh), dim3(256), 0, s, part,
-                     balance_token_blocks(T), counts, mask, T, Nh, Ne, loss,
+                     balance_token_blocks(T, Nh, Ne), counts, mask, T, Nh, Ne, loss,
                      reinterpret_cast<float2*>(stats));
   return hipGetLastError();
 }
@@ -935,7 +1337,7 @@ hipError_t launch_balance_loss_sum(const double* part, const int32_t* counts, co
 hipError_t launch_balance_dx(const void* X, const void* weights, const float* stats,
                              const float* dloss, const uint8_t* mask, const void* dX_add, int64_t T,
                              int Nh, int dh, int Ne, bool f32, void* dX, hipStream_t s) {
-  const dim3 grid((unsigned)(Nh * balance_token_blocks(T)));
+  const dim3 grid((unsigned)(Nh * ceil_div(T, kBalanceTokens)));
 #define MHL_DX(DH, F32)                                                                       \
   hipLaunchKernelGGL((balance_dx_kernel<DH, F32>), grid, dim3(kTokenWaves* kWave), 0, s, X,   \
                      static_cast<const uint8_t*>(weights), head_info(weights, Nh, dh, Ne),      \
@@ -945,29 +1347,68 @@ hipError_t launch_balance_dx(const void* X, const void* weights, const float* st
   return hipGetLastError();
 }
 
+static DwArgs dw_args(const void* X, const float* W, const int32_t* counts, const float* stats,
+                      const float* dloss, const uint8_t* mask, const float* dW_add, int64_t T,
+                      int Nh, int Ne, float* dW, float* part) {
+  return DwArgs{X, W, counts, reinterpret_cast<const float2*>(stats), dloss, mask, dW_add, T, Nh,
+                Ne, (int)ceil_div(balance_blocks(Ne), balance_dw_blocks(Ne)),
+                (int)balance_splits(T, Nh, Ne), dW, part};
+}
+static unsigned dw_workgroups(const DwArgs& a) {
+  return (unsigned)(ceil_div((int64_t)a.Nh * a.splits, kXcds) * kXcds * a.groups);
+}
+
+// CALL(DH, F32, blocks of experts per workgroup of dW)
+#define MHL_BALANCE_DW(CALL)      \
+  do {                            \
+    const int ew = balance_dw_blocks(Ne); \
+    if (ew == 1) {                \
+      MHL_BALANCE_TYPES(CALL##_1) \
+    } else if (ew == 2) {         \
+      MHL_BALANCE_TYPES(CALL##_2) \
+    } else {                      \
+      MHL_BALANCE_TYPES(CALL##_4) \
+    }                             \
+  } while (0)
+
 hipError_t launch_balance_dw(const void* X, const float* W, const int32_t* counts,
                              const float* stats, const float* dloss, const uint8_t* mask,
                              const float* dW_add, int64_t T, int Nh, int dh, int Ne, bool f32,
                              float* dW, float* part, hipStream_t s) {
-  const int ew = balance_dw_blocks(Ne), groups = (int)ceil_div(balance_blocks(Ne), ew);
-  const int splits = (int)balance_splits(T, Nh, Ne);
-  const dim3 grid((unsigned)(ceil_div((int64_t)Nh * splits, kXcds) * kXcds * groups));
-#define MHL_DW_EW(DH, F32, EW)                                                                  \
-  hipLaunchKernelGGL((balance_dw_kernel<DH, F32, EW>), grid, dim3(kDwWaves* kWave), 0, s, X, W, \
-                     counts, reinterpret_cast<const float2*>(stats), dloss, mask, dW_add, T,    \
-                     Nh, Ne, groups, splits, dW, part)
-#define MHL_DW(DH, F32)         \
-  do {                          \
-    if (ew == 1)                \
-      MHL_DW_EW(DH, F32, 1);    \
-    else if (ew == 2)           \
-      MHL_DW_EW(DH, F32, 2);    \
-    else                        \
-      MHL_DW_EW(DH, F32, 4);    \
-  } while (0)
-  MHL_BALANCE_TYPES(MHL_DW)
+  const DwArgs a = dw_args(X, W, counts, stats, dloss, mask, dW_add, T, Nh, Ne, dW, part);
+#define MHL_DW(DH, F32, EW)                                                                      \
+  hipLaunchKernelGGL((balance_dw_kernel<DH, F32, EW>), dim3(dw_workgroups(a)),                   \
+                     dim3(kDwWaves* kWave), 0, s, a)
+#define MHL_DW_1(DH, F32) MHL_DW(DH, F32, 1)
+#define MHL_DW_2(DH, F32) MHL_DW(DH, F32, 2)
+#define MHL_DW_4(DH, F32) MHL_DW(DH, F32, 4)
+  MHL_BALANCE_DW(MHL_DW);
+#undef MHL_DW_1
+#undef MHL_DW_2
+#undef MHL_DW_4
 #undef MHL_DW
-#undef MHL_DW_EW
+  return hipGetLastError();
+}
+
+hipError_t launch_balance_bwd_few(const void* X, const float* W, const int32_t* counts,
+                                  const float* stats, const float* dloss, const uint8_t* mask,
+                                  const void* dX_add, const float* dW_add, int64_t T, int Nh,
+                                  int dh, int Ne, bool f32, void* dX, float* dW, float* part,
+                                  hipStream_t s) {
+  const DwArgs a = dw_args(X, W, counts, stats, dloss, mask, dW_add, T, Nh, Ne, dW, part);
+  const unsigned dx_blocks =
+      (unsigned)(Nh * ceil_div(T, 32 * (kDxFewWaves / balance_dw_blocks(Ne))));
+#define MHL_FEW(DH, F32, EW)                                                                       \
+  hipLaunchKernelGGL((balance_bwd_few_kernel<DH, F32, EW>), dim3(dx_blocks + dw_workgroups(a)),    \
+                     dim3(kDwWaves* kWave), 0, s, a, dX_add, dX, dx_blocks)
+#define MHL_FEW_1(DH, F32) MHL_FEW(DH, F32, 1)
+#define MHL_FEW_2(DH, F32) MHL_FEW(DH, F32, 2)
+#define MHL_FEW_4(DH, F32) MHL_FEW(DH, F32, 4)
+  MHL_BALANCE_DW(MHL_FEW);
+#undef MHL_FEW_1
+#undef MHL_FEW_2
+#undef MHL_FEW_4
+#undef MHL_FEW
   return hipGetLastError();
 }
 

@@ -82,9 +82,32 @@ inline size_t balance_operand_bytes(int Nh, int dh, int Ne) {
 inline size_t balance_weight_bytes(int Nh, int dh, int Ne) {
   return balance_operand_bytes(Nh, dh, Ne) + Nh * kBalanceHeadBytes;
 }
+constexpr int64_t kBalanceFew = 512;
 constexpr int kBalanceTokens = 128;  // per workgroup of the loss and of dX
-__host__ __device__ inline int64_t balance_token_blocks(int64_t T) {
-  return ceil_div(T, kBalanceTokens);
+// Few tokens: no launch in front that lays the weights out (every group of 32 tokens
+// splits them itself), and the wavefronts of a workgroup share out the experts, too.
+constexpr int kBalanceFewWaves = 8;
+inline bool balance_few(int64_t T, int Nh, int Ne) {
+  return Nh * ceil_div(T, 32) <= kBalanceFew;
+}
+// Of so many wavefronts, those that have experts of their own: a power of two.
+inline int balance_few_groups(int Ne, int waves) {
+  int n = 1;
+  while (n < balance_blocks(Ne) && n < waves) n *= 2;
+  return n;
+}
+// Tokens and workgroups per head of the loss.
+inline int64_t balance_loss_tokens(int64_t T, int Nh, int Ne) {
+  return balance_few(T, Nh, Ne)
+             ? 32 * (kBalanceFewWaves / balance_few_groups(Ne, kBalanceFewWaves))
+             : kBalanceTokens;
+}
+inline int64_t balance_token_blocks(int64_t T, int Nh, int Ne) {
+  return ceil_div(T, balance_loss_tokens(T, Nh, Ne));
+}
+// Whether launch_balance_loss writes the loss itself.
+inline bool balance_loss_at_once(int64_t T, int Nh, int Ne) {
+  return T > 0 && balance_few(T, Nh, Ne) && balance_token_blocks(T, Nh, Ne) == 1;
 }
 // dW: blocks of experts that a workgroup's four wavefronts have (they share them out
 // over the tokens where there are fewer than three), and the chunks that the tokens
@@ -98,8 +121,9 @@ inline int64_t balance_splits(int64_t T, int Nh, int Ne) {
 }
 hipError_t launch_balance_weights(const float* W, const int32_t* counts, int Nh, int dh, int Ne,
                                   void* out, hipStream_t s);
-hipError_t launch_balance_loss(const void* X, const void* weights, const uint8_t* mask, int64_t T,
-                               int Nh, int dh, int Ne, bool f32, float* stats, double* part,
+hipError_t launch_balance_loss(const void* X, const float* W, const void* weights,
+                               const int32_t* counts, const uint8_t* mask, int64_t T, int Nh,
+                               int dh, int Ne, bool f32, float* stats, double* part, float* loss,
                                hipStream_t s);
 hipError_t launch_balance_loss_sum(const double* part, const int32_t* counts, const uint8_t* mask,
                                    int64_t T, int Nh, int Ne, float* loss, float* stats,
@@ -111,6 +135,12 @@ hipError_t launch_balance_dw(const void* X, const float* W, const int32_t* count
                              const float* stats, const float* dloss, const uint8_t* mask,
                              const float* dW_add, int64_t T, int Nh, int dh, int Ne, bool f32,
                              float* dW, float* part, hipStream_t s);
+// dX and dW where balance_few.
+hipError_t launch_balance_bwd_few(const void* X, const float* W, const int32_t* counts,
+                                  const float* stats, const float* dloss, const uint8_t* mask,
+                                  const void* dX_add, const float* dW_add, int64_t T, int Nh,
+                                  int dh, int Ne, bool f32, void* dX, float* dW, float* part,
+                                  hipStream_t s);
 hipError_t launch_balance_dw_sum(const float* part, const float* stats, const float* dloss,
                                  const float* dW_add, int64_t T, int Nh, int dh, int Ne, float* dW,
                                  hipStream_t s);

@@ -191,7 +191,7 @@ def test_kernel_names_are_declared():
     """Every kernel these entry points time is named in the header."""
     header = open(m.HEADER).read()
     names = re.findall(r'run_kernel\("(\w+)"', open(os.path.join(CSRC, "api_training.cpp")).read())
-    assert len(set(names)) == 10
+    assert len(set(names)) == 11
     for name in names:
         assert f'"{name}"' in header, name
 

@@ -67,7 +67,7 @@ int main() {
             const int64_t groups = mhl::ceil_div(mhl::balance_blocks(Ne), mhl::balance_dw_blocks(Ne));
             expect("splits", splits <= 1024 && (T == 0 || splits >= 1), 1);
             expect("dw", (Nh * splits + 7) * groups < (int64_t(1) << 24), 1);
-            expect("tokens", Nh * mhl::balance_token_blocks(T) < (int64_t(1) << 24), 1);
+            expect("tokens", Nh * mhl::balance_token_blocks(T, Nh, Ne) < (int64_t(1) << 24), 1);
           }
         }
   }
