@@ -47,7 +47,7 @@ __global__ __launch_bounds__(kCountThreads) void counts_zero_kernel(int32_t* cou
 // All of head blockIdx.x's slots, where they are few: no launch in front to clear the
 // counts.
 constexpr int kCountAllThreads = 1024;
-constexpr int64_t kCountAllSlots = 1 << 15;
+constexpr int64_t kCountAllSlots = 1 << 13;  // 32768 of them take 19 us, in two launches 8
 
 __global__ __launch_bounds__(kCountAllThreads) void expert_counts_all_kernel(
     const int32_t* __restrict__ idx, const uint8_t* __restrict__ mask, int64_t T, int Nh, int Ne,
@@ -777,6 +777,67 @@ __device__ __forceinline__ void store_dx(const f32x16 (&dx)[DH / 32], float c, i
     }
 }
 
+// The same for a wavefront's 32 tokens from t0 on, through a Tile of LDS, so that whole
+// rows are read and written (by lanes' own pieces of 8 bytes the kernel took 80 us where
+// it takes 55: 16384 x 16 heads x 16 experts).
+template <int DH, bool F32>
+__device__ __forceinline__ void store_dx_rows(const f32x16 (&dx)[DH / 32], bool ok, float c,
+                                              int64_t t0, int64_t T, int Nh, int h, uint8_t* tile,
+                                              const void* dX_add, void* dX) {
+  constexpr int kUnits = DH / 8, kRows = kWave / kUnits;  // 16-byte units, rows per access
+  constexpr int kPasses = F32 ? 2 : 1;                    // fp32: half a row at a time
+  const int lane = lane_id(), g = lane >> 5, r0 = lane / kUnits, j = lane % kUnits;
+#pragma unroll
+  for (int pass = 0; pass < kPasses; ++pass) {
+    auto row = [&](int i) { return t0 + r0 + kRows * i; };
+    auto address = [&](int i) {
+      return ((row(i) * Nh + h) * DH) * (F32 ? 4 : 2) + pass * DH * 2 + 16 * j;
+    };
+    auto place = [&](int i) {
+      return reinterpret_cast<u32x4*>(tile + Tile<DH>::unit(r0 + kRows * i, j));
+    };
+    if (dX_add) {
+      u32x4 add[32 / kRows];
+#pragma unroll
+      for (int i = 0; i < 32 / kRows; ++i)
+        add[i] = row(i) < T ? *reinterpret_cast<const u32x4*>(
+                                  static_cast<const uint8_t*>(dX_add) + address(i))
+                            : u32x4{0, 0, 0, 0};
+      wave_lds_order();  // the readers of what was there
+#pragma unroll
+      for (int i = 0; i < 32 / kRows; ++i) *place(i) = add[i];
+    }
+    wave_lds_order();
+#pragma unroll
+    for (int i = 0; i < DH / 8 / kPasses; ++i) {
+      const int dt = i / 4 + pass * (DH / 32 / kPasses), q = i % 4;
+      float f[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) f[k] = ok ? dx[dt][4 * q + k] * c : 0.0f;
+      if constexpr (F32) {
+        f32x4* p = reinterpret_cast<f32x4*>(tile + Tile<DH>::unit(lane & 31, 2 * i + g));
+        f32x4 v{f[0], f[1], f[2], f[3]};
+        if (dX_add) v += *p;
+        *p = v;
+      } else {
+        u32x2* p = reinterpret_cast<u32x2*>(tile + Tile<DH>::unit(lane & 31, i) + 8 * g);
+        if (dX_add) {
+          const u32x2 a = *p;
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            f[k] += bf16_bits_to_f32((a[k >> 1] >> (16 * (k & 1))) & 0xFFFFu);
+        }
+        *p = u32x2{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3])};
+      }
+    }
+    wave_lds_order();
+#pragma unroll
+    for (int i = 0; i < 32 / kRows; ++i)
+      if (row(i) < T)
+        *reinterpret_cast<u32x4*>(static_cast<uint8_t*>(dX) + address(i)) = *place(i);
+  }
+}
+
 // The largest of the head's blocks' powers down (2^-K), in every lane.
 __device__ __forceinline__ float head_down(const HeadInfo& info, int nb) {
   float d = lane_id() < nb ? info.down[lane_id()] : 0.0f;
@@ -831,7 +892,9 @@ __global__ __launch_bounds__(kTokenWaves* kWave) void balance_dx_kernel(
     }
     add_dx<DH, NP>(z, wb, at, dx);
   }
-  if (t < T) store_dx<DH, F32>(dx, ok ? c : 0.0f, row, dX_add, dX);
+  __syncthreads();  // the weights' LDS is the rows' now
+  store_dx_rows<DH, F32>(dx, ok, c, t - (lane & 31), T, Nh, h, &w[0][0] + wave * Tile<DH>::kBytes,
+                         dX_add, dX);
 }
 
 // ---------------------------------------------------------------------------

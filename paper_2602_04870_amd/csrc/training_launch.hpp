@@ -82,13 +82,22 @@ inline size_t balance_operand_bytes(int Nh, int dh, int Ne) {
 inline size_t balance_weight_bytes(int Nh, int dh, int Ne) {
   return balance_operand_bytes(Nh, dh, Ne) + Nh * kBalanceHeadBytes;
 }
-constexpr int64_t kBalanceFew = 512;
 constexpr int kBalanceTokens = 128;  // per workgroup of the loss and of dX
 // Few tokens: no launch in front that lays the weights out (every group of 32 tokens
 // splits them itself), and the wavefronts of a workgroup share out the experts, too.
+// us at 8 heads, d_h 128, bf16, so / with the weights laid out (a call of the loss and
+// the counts, of the gradient):
+//   tokens  experts   loss       gradient
+//      512    1024   28 / 40     35 / 71
+//     1024    1024   29 / 40     64 / 79
+//     2048      64   21 / 24     30 / 32
+//     2048     256   26 / 24     50 / 42
+//     4096      16   21 / 25     33 / 37
+//     4096      64   21 / 25     41 / 35
 constexpr int kBalanceFewWaves = 8;
 inline bool balance_few(int64_t T, int Nh, int Ne) {
-  return Nh * ceil_div(T, 32) <= kBalanceFew;
+  const int64_t groups = Nh * ceil_div(T, 32);
+  return groups <= 256 || groups * balance_blocks(Ne) <= 1024;
 }
 // Of so many wavefronts, those that have experts of their own: a power of two.
 inline int balance_few_groups(int Ne, int waves) {
@@ -111,12 +120,14 @@ inline bool balance_loss_at_once(int64_t T, int Nh, int Ne) {
 }
 // dW: blocks of experts that a workgroup's four wavefronts have (they share them out
 // over the tokens where there are fewer than three), and the chunks that the tokens
-// are cut into, of at least four tiles, so that there are about 1024 workgroups.
+// are cut into, of at least four tiles, so that there are about 512 workgroups, two per
+// CU at once (us of the gradient in bf16 with 512 and 1024: 122 and 138 at 16384 x 16
+// heads x 128 experts, 63 and 76 at 8192 x 8 x 256, 1024 and 1029 at 65536 x 8 x 1024).
 inline int balance_dw_blocks(int Ne) { return Ne <= 32 ? 1 : Ne <= 64 ? 2 : 4; }
 inline int64_t balance_splits(int64_t T, int Nh, int Ne) {
   const int ew = balance_dw_blocks(Ne);
   const int64_t groups = Nh * ceil_div(balance_blocks(Ne), ew);
-  const int64_t want = ceil_div(1024, groups), most = ceil_div(T, 4 * 32 * (4 / ew));
+  const int64_t want = ceil_div(512, groups), most = ceil_div(T, 4 * 32 * (4 / ew));
   return want < most ? want : most;
 }
 hipError_t launch_balance_weights(const float* W, const int32_t* counts, int Nh, int dh, int Ne,
