@@ -78,7 +78,7 @@ BalanceLayout balance_layout(int64_t T, int n_heads, int d_head, int n_experts, 
   BalanceLayout L;
   size_t cur = 0;
   L.weights = bump(cur, mhl::balance_weight_bytes(n_heads, d_head, n_experts));
-  L.part = bump(cur, backward ? sizeof(float) * (size_t)mhl::balance_splits(T, n_heads, n_experts) *
+  L.part = bump(cur, backward ? sizeof(float) * (size_t)mhl::balance_splits(T, n_heads, d_head, n_experts) *
                                     n_heads * mhl::balance_blocks(n_experts) * 32 * d_head
                               : sizeof(double) * (size_t)n_heads *
                                     mhl::balance_token_blocks(T, n_heads, n_experts));
@@ -340,7 +340,7 @@ mhlmoe_status mhlmoe_balance_loss_backward(
                                     d_head, n_experts, f32, dW_router, part, stream);
     }));
   }
-  if (mhl::balance_splits(T, n_heads, n_experts) == 1) return MHLMOE_OK;
+  if (mhl::balance_splits(T, n_heads, d_head, n_experts) == 1) return MHLMOE_OK;
   return run_kernel("balance_sum", stream, [&] {
     return mhl::launch_balance_dw_sum(part, stats, dloss, dW_add, T, n_heads, d_head, n_experts,
                                       dW_router, stream);

@@ -44,6 +44,30 @@ __global__ __launch_bounds__(kCountThreads) void counts_zero_kernel(int32_t* cou
   if (i < n) counts[i] = 0;
 }
 
+// A head's slots of T tokens into a histogram in LDS, eight of a thread on their way at
+// once.
+template <int THREADS>
+__device__ __forceinline__ void count_slots(const int32_t* __restrict__ idx,
+                                            const uint8_t* __restrict__ mask, int T, int Nh, int Ne,
+                                            int k, DivMagic by_k, int32_t* hist) {
+  const int n = T * k;
+  for (int i0 = threadIdx.x; i0 < n; i0 += 8 * THREADS) {
+    int e[8];
+    uint8_t counted[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int i = i0 < n - j * THREADS ? i0 + j * THREADS : i0;
+      const int t = div_by_magic(i, by_k);
+      e[j] = idx[(int64_t)t * Nh * k + (i - t * k)];
+      counted[j] = mask ? mask[t] : 1;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (i0 < n - j * THREADS && counted[j] && (unsigned)e[j] < (unsigned)Ne)
+        atomicAdd(&hist[e[j]], 1);
+  }
+}
+
 // All of head blockIdx.x's slots, where they are few: no launch in front to clear the
 // counts.
 constexpr int kCountAllThreads = 1024;
@@ -55,22 +79,7 @@ __global__ __launch_bounds__(kCountAllThreads) void expert_counts_all_kernel(
   __shared__ int32_t hist[kMaxExperts];
   if ((int)threadIdx.x < Ne) hist[threadIdx.x] = 0;
   __syncthreads();
-  const int n = (int)T * k;
-  for (int i0 = threadIdx.x; i0 < n; i0 += 8 * kCountAllThreads) {
-    int e[8];
-    uint8_t counted[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int i = i0 + j * kCountAllThreads < n ? i0 + j * kCountAllThreads : i0;
-      const int t = div_by_magic(i, by_k);
-      e[j] = idx[((int64_t)t * Nh + blockIdx.x) * k + (i - t * k)];
-      counted[j] = mask ? mask[t] : 1;
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (i0 + j * kCountAllThreads < n && counted[j] && (unsigned)e[j] < (unsigned)Ne)
-        atomicAdd(&hist[e[j]], 1);
-  }
+  count_slots<kCountAllThreads>(idx + blockIdx.x * k, mask, (int)T, Nh, Ne, k, by_k, hist);
   __syncthreads();
   if ((int)threadIdx.x < Ne) counts[(int64_t)blockIdx.x * Ne + threadIdx.x] = hist[threadIdx.x];
 }
@@ -85,12 +94,8 @@ __global__ __launch_bounds__(kCountThreads) void expert_counts_kernel(
   __syncthreads();
   const int64_t t0 = (int64_t)blockIdx.x * tokens;
   const int here = (int)(T - t0 < tokens ? T - t0 : tokens);
-  for (int i = threadIdx.x; i < here * k; i += kCountThreads) {
-    const int t = div_by_magic(i, by_k);
-    if (mask && !mask[t0 + t]) continue;
-    const int e = idx[((t0 + t) * Nh + blockIdx.y) * k + (i - t * k)];
-    if ((unsigned)e < (unsigned)Ne) atomicAdd(&hist[e], 1);
-  }
+  count_slots<kCountThreads>(idx + (t0 * Nh + blockIdx.y) * k, mask ? mask + t0 : nullptr, here, Nh,
+                             Ne, k, by_k, hist);
   __syncthreads();
   for (int e = threadIdx.x; e < Ne; e += kCountThreads)
     if (hist[e]) atomicAdd(&counts[(int64_t)blockIdx.y * Ne + e], hist[e]);
@@ -899,26 +904,27 @@ __global__ __launch_bounds__(kTokenWaves* kWave) void balance_dx_kernel(
 
 // ---------------------------------------------------------------------------
 // dW: a block of 32 experts per wavefront, whose weights stay in its registers, over
-// a chunk of the tokens, 32 SUB at a time through LDS in two buffers (SUB = 4 / EW
-// wavefronts share a block of experts where there are fewer than four blocks, each
-// with 32 tokens of its own).  X lies in LDS as pieces of x up (a token's power of
+// a chunk of the tokens, 32 SUB at a time through LDS in two buffers (EW blocks of
+// experts in a workgroup; SUB = 4 / EW wavefronts share one where there are fewer than
+// four, each with 32 tokens of its own).  X lies in LDS as pieces of x up (a token's power of
 // two), read along d for the scores and transposed for dW; what up adds is taken off
 // ds in its exponential.  ds is two fp16 values times S, a power of two that every
 // expert (lane) has for itself: it is lowered, and the sums with it, when a ds does not
 // fit any more, so an expert that gets little weight keeps its digits.
 // ---------------------------------------------------------------------------
 constexpr int kDwWaves = 4;
+constexpr int dw_waves(int blocks) { return blocks > kDwWaves ? blocks : kDwWaves; }
 constexpr float kDwFirst = 0x1p60f;  // S before the first ds: any above 2^-45 lowers it
 
 template <int DH, bool F32, int EW>
 struct DwShared {
-  static constexpr int NX = F32 ? 2 : 1, SUB = kDwWaves / EW;
+  static constexpr int NX = F32 ? 2 : 1, SUB = dw_waves(EW) / EW;
   static constexpr int kTiles = 2 * NX * SUB * Tile<DH>::kBytes;
   static constexpr int kSums = (SUB - 1) * EW * 32 * DH * 4;  // of all but a block's first wavefront
   __align__(16) uint8_t xs[kTiles > kSums ? kTiles : kSums];
   __align__(16) float ms[2][32 * SUB], refs[2][32 * SUB], us[2][32 * SUB];
-  long long totals[kDwWaves];
-  uint32_t tops[kDwWaves][2];
+  long long totals[dw_waves(EW)];
+  uint32_t tops[dw_waves(EW)][2];
 };
 
 struct DwArgs {
@@ -937,9 +943,9 @@ struct DwArgs {
 template <int DH, bool F32, int EW>
 __device__ __forceinline__ void balance_dw(const DwArgs& a, unsigned block,
                                            DwShared<DH, F32, EW>& sm) {
-  constexpr int NX = F32 ? 2 : 1, SUB = kDwWaves / EW, kTokens = 32 * SUB;
+  constexpr int NX = F32 ? 2 : 1, SUB = dw_waves(EW) / EW, kTokens = 32 * SUB;
   constexpr int kUnits = DH / 8;                               // 16-byte units of a row
-  constexpr int kPer = kTokens * kUnits / (kDwWaves * kWave);  // units per thread
+  constexpr int kPer = kTokens * kUnits / (dw_waves(EW) * kWave);  // units per thread
   constexpr int kPiece = SUB * Tile<DH>::kBytes;
   const void* __restrict__ X = a.X;
   const float* __restrict__ W = a.W;
@@ -972,7 +978,7 @@ __device__ __forceinline__ void balance_dw(const DwArgs& a, unsigned block,
   auto fetch = [&](int64_t tile) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const int unit = i * kDwWaves * kWave + threadIdx.x;
+      const int unit = i * dw_waves(EW) * kWave + threadIdx.x;
       int64_t t = tile * kTokens + unit / kUnits;
       t = t < T ? t : T - 1;
       const uint8_t* p = static_cast<const uint8_t*>(X) +
@@ -988,7 +994,7 @@ __device__ __forceinline__ void balance_dw(const DwArgs& a, unsigned block,
   // the lane's expert: f' and, scaled alike for all of the workgroup's experts, its weights
   WOperand<DH> w;
   const uint32_t top = w.load(W + (int64_t)h * Ne * DH, e, Ne, g);
-  const HeadCounts hc = head_counts<kDwWaves * kWave>(counts + (int64_t)h * Ne, Ne, sm.totals, sm.tops);
+  const HeadCounts hc = head_counts<dw_waves(EW) * kWave>(counts + (int64_t)h * Ne, Ne, sm.totals, sm.tops);
   const float f = live ? excess(counts[(int64_t)h * Ne + e], Ne, hc.total) : 0.0f;
   {
     uint32_t most = wave_max(top);
@@ -996,7 +1002,7 @@ __device__ __forceinline__ void balance_dw(const DwArgs& a, unsigned block,
     if (lane == 0) sm.tops[wave][0] = most;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kDwWaves; ++i) most = umax(most, sm.tops[i][0]);
+    for (int i = 0; i < dw_waves(EW); ++i) most = umax(most, sm.tops[i][0]);
     w.split(most);
   }
   const float down = w.down;
@@ -1007,7 +1013,7 @@ __device__ __forceinline__ void balance_dw(const DwArgs& a, unsigned block,
   auto store = [&](int64_t tile, int buf) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const int unit = i * kDwWaves * kWave + threadIdx.x, r = unit / kUnits;
+      const int unit = i * dw_waves(EW) * kWave + threadIdx.x, r = unit / kUnits;
       const bool ok = tile * kTokens + r < T && counted[i];
       float v[8];
       uint32_t top = 0;
@@ -1142,35 +1148,34 @@ __device__ __forceinline__ void balance_dw(const DwArgs& a, unsigned block,
 }
 
 template <int DH, bool F32, int EW>
-__global__ __launch_bounds__(kDwWaves* kWave) void balance_dw_kernel(const DwArgs a) {
+__global__ __launch_bounds__(dw_waves(EW)* kWave) void balance_dw_kernel(const DwArgs a) {
   __shared__ DwShared<DH, F32, EW> sm;
   balance_dw<DH, F32, EW>(a, blockIdx.x, sm);
 }
 
 // ---------------------------------------------------------------------------
 // The gradient where there are few tokens, in one launch: the first workgroups make dX,
-// the others dW.  For dX four wavefronts, EG of them for the blocks of experts in turn,
-// the others for as many groups of 32 tokens; weights straight from memory, and through
+// the others dW.  For dX EG wavefronts of a workgroup take the blocks of experts in turn,
+// the others as many groups of 32 tokens; weights straight from memory, and through
 // a Tile of the wavefront's own to be read transposed.  The products add up in the unit
 // of the largest weights so far (down), to which both are lowered when larger ones come.
 // ---------------------------------------------------------------------------
-constexpr int kDxFewWaves = kDwWaves;
-
 template <int DH, bool F32, int EG>
 struct DxFewShared {
   static constexpr int NP = F32 ? 2 : 1;
-  static constexpr int kTiles = kDxFewWaves * NP * Tile<DH>::kBytes;
-  static constexpr int kSums = (kDxFewWaves - kDxFewWaves / EG) * 32 * DH * 4;
+  static constexpr int kTiles = kDwWaves * NP * Tile<DH>::kBytes;
+  static constexpr int kSums = (kDwWaves - kDwWaves / EG) * 32 * DH * 4;
   __align__(16) uint8_t ws[kTiles > kSums ? kTiles : kSums];
   __align__(16) float fex[kMaxExperts];
-  long long totals[kDxFewWaves];
-  uint32_t tops[kDxFewWaves][2];
+  long long totals[kDwWaves];
+  uint32_t tops[kDwWaves][2];
 };
 
 template <int DH, bool F32, int EG>
 __device__ __forceinline__ void balance_dx_few(const DwArgs& a, const void* dX_add, void* dX,
-                                               unsigned block, DxFewShared<DH, F32, EG>& sm) {
-  constexpr int NP = F32 ? 2 : 1, TG = kDxFewWaves / EG;
+                                               unsigned block,
+                                               DxFewShared<DH, F32, EG>& sm) {
+  constexpr int NP = F32 ? 2 : 1, TG = kDwWaves / EG;
   const int64_t T = a.T;
   const int Nh = a.Nh, Ne = a.Ne;
   const int h = block % Nh, lane = lane_id(), g = lane >> 5, wave = threadIdx.x >> 6;
@@ -1183,8 +1188,8 @@ __device__ __forceinline__ void balance_dx_few(const DwArgs& a, const void* dX_a
   WOperand<DH> w;
   uint32_t top = w.load(Wh, 32 * eg + (lane & 31), Ne, g);
   float2 st = a.stats[near * Nh + h];
-  const HeadCounts hc = head_counts<kDxFewWaves * kWave>(counts, Ne, sm.totals, sm.tops);
-  for (int e = threadIdx.x; e < ((Ne + 31) & ~31); e += kDxFewWaves * kWave)
+  const HeadCounts hc = head_counts<kDwWaves * kWave>(counts, Ne, sm.totals, sm.tops);
+  for (int e = threadIdx.x; e < ((Ne + 31) & ~31); e += kDwWaves * kWave)
     sm.fex[e] = e < Ne ? excess(counts[e], Ne, hc.total) : 0.0f;
   const float F = ds_exponent(hc.most, hc.least, Ne, hc.total);
   const bool ok = t < T && counted;
@@ -1260,10 +1265,10 @@ __device__ __forceinline__ void balance_dx_few(const DwArgs& a, const void* dX_a
   if (t < T) store_dx<DH, F32>(dx, ok ? 1.0f : 0.0f, t * Nh + h, dX_add, dX);
 }
 
+// EG: also the blocks of experts per workgroup of dW.
 template <int DH, bool F32, int EG>
 __global__ __launch_bounds__(kDwWaves* kWave) void balance_bwd_few_kernel(
     const DwArgs a, const void* dX_add, void* dX, unsigned dx_blocks) {
-  // as many blocks of experts per workgroup of dW as wavefronts share them for dX
   __shared__ union Shared {
     DxFewShared<DH, F32, EG> dx;
     DwShared<DH, F32, EG> dw;
@@ -1412,44 +1417,51 @@ hipError_t launch_balance_dx(const void* X, const void* weights, const float* st
 
 static DwArgs dw_args(const void* X, const float* W, const int32_t* counts, const float* stats,
                       const float* dloss, const uint8_t* mask, const float* dW_add, int64_t T,
-                      int Nh, int Ne, float* dW, float* part) {
+                      int Nh, int dh, int Ne, float* dW, float* part) {
   return DwArgs{X, W, counts, reinterpret_cast<const float2*>(stats), dloss, mask, dW_add, T, Nh,
-                Ne, (int)ceil_div(balance_blocks(Ne), balance_dw_blocks(Ne)),
-                (int)balance_splits(T, Nh, Ne), dW, part};
+                Ne, (int)ceil_div(balance_blocks(Ne), balance_dw_blocks(T, Nh, dh, Ne)),
+                (int)balance_splits(T, Nh, dh, Ne), dW, part};
 }
 static unsigned dw_workgroups(const DwArgs& a) {
   return (unsigned)(ceil_div((int64_t)a.Nh * a.splits, kXcds) * kXcds * a.groups);
 }
 
-// CALL(DH, F32, blocks of experts per workgroup of dW)
-#define MHL_BALANCE_DW(CALL)      \
-  do {                            \
-    const int ew = balance_dw_blocks(Ne); \
-    if (ew == 1) {                \
-      MHL_BALANCE_TYPES(CALL##_1) \
-    } else if (ew == 2) {         \
-      MHL_BALANCE_TYPES(CALL##_2) \
-    } else {                      \
-      MHL_BALANCE_TYPES(CALL##_4) \
-    }                             \
-  } while (0)
+template <int V>
+using Int = std::integral_constant<int, V>;
+
+// call(d_h, X in fp32, blocks of experts per workgroup of dW) as compile-time constants.
+template <class F>
+static void for_dw(int dh, bool f32, int ew, F&& call) {
+  auto blocks = [&](auto DH, auto F32) {
+    if (ew == 1)
+      call(DH, F32, Int<1>{});
+    else if (ew == 2)
+      call(DH, F32, Int<2>{});
+    else if (ew == 4)
+      call(DH, F32, Int<4>{});
+    else if constexpr (decltype(DH)::value == 128)
+      call(DH, F32, Int<8>{});
+  };
+  if (dh == 128 && f32)
+    blocks(Int<128>{}, std::true_type{});
+  else if (dh == 128)
+    blocks(Int<128>{}, std::false_type{});
+  else if (f32)
+    blocks(Int<64>{}, std::true_type{});
+  else
+    blocks(Int<64>{}, std::false_type{});
+}
 
 hipError_t launch_balance_dw(const void* X, const float* W, const int32_t* counts,
                              const float* stats, const float* dloss, const uint8_t* mask,
                              const float* dW_add, int64_t T, int Nh, int dh, int Ne, bool f32,
                              float* dW, float* part, hipStream_t s) {
-  const DwArgs a = dw_args(X, W, counts, stats, dloss, mask, dW_add, T, Nh, Ne, dW, part);
-#define MHL_DW(DH, F32, EW)                                                                      \
-  hipLaunchKernelGGL((balance_dw_kernel<DH, F32, EW>), dim3(dw_workgroups(a)),                   \
-                     dim3(kDwWaves* kWave), 0, s, a)
-#define MHL_DW_1(DH, F32) MHL_DW(DH, F32, 1)
-#define MHL_DW_2(DH, F32) MHL_DW(DH, F32, 2)
-#define MHL_DW_4(DH, F32) MHL_DW(DH, F32, 4)
-  MHL_BALANCE_DW(MHL_DW);
-#undef MHL_DW_1
-#undef MHL_DW_2
-#undef MHL_DW_4
-#undef MHL_DW
+  const DwArgs a = dw_args(X, W, counts, stats, dloss, mask, dW_add, T, Nh, dh, Ne, dW, part);
+  for_dw(dh, f32, balance_dw_blocks(T, Nh, dh, Ne), [&](auto DH, auto F32, auto EW) {
+    hipLaunchKernelGGL((balance_dw_kernel<decltype(DH)::value, decltype(F32)::value,
+                                          decltype(EW)::value>),
+                       dim3(dw_workgroups(a)), dim3(dw_waves(decltype(EW)::value) * kWave), 0, s, a);
+  });
   return hipGetLastError();
 }
 
@@ -1458,20 +1470,16 @@ hipError_t launch_balance_bwd_few(const void* X, const float* W, const int32_t* 
                                   const void* dX_add, const float* dW_add, int64_t T, int Nh,
                                   int dh, int Ne, bool f32, void* dX, float* dW, float* part,
                                   hipStream_t s) {
-  const DwArgs a = dw_args(X, W, counts, stats, dloss, mask, dW_add, T, Nh, Ne, dW, part);
-  const unsigned dx_blocks =
-      (unsigned)(Nh * ceil_div(T, 32 * (kDxFewWaves / balance_dw_blocks(Ne))));
-#define MHL_FEW(DH, F32, EW)                                                                       \
-  hipLaunchKernelGGL((balance_bwd_few_kernel<DH, F32, EW>), dim3(dx_blocks + dw_workgroups(a)),    \
-                     dim3(kDwWaves* kWave), 0, s, a, dX_add, dX, dx_blocks)
-#define MHL_FEW_1(DH, F32) MHL_FEW(DH, F32, 1)
-#define MHL_FEW_2(DH, F32) MHL_FEW(DH, F32, 2)
-#define MHL_FEW_4(DH, F32) MHL_FEW(DH, F32, 4)
-  MHL_BALANCE_DW(MHL_FEW);
-#undef MHL_FEW_1
-#undef MHL_FEW_2
-#undef MHL_FEW_4
-#undef MHL_FEW
+  const DwArgs a = dw_args(X, W, counts, stats, dloss, mask, dW_add, T, Nh, dh, Ne, dW, part);
+  for_dw(dh, f32, balance_dw_blocks(T, Nh, dh, Ne), [&](auto DH, auto F32, auto EW) {
+    constexpr int EG = decltype(EW)::value;
+    if constexpr (EG <= kDwWaves) {
+      const unsigned dx_blocks = (unsigned)(Nh * ceil_div(T, 32 * (kDwWaves / EG)));
+      hipLaunchKernelGGL((balance_bwd_few_kernel<decltype(DH)::value, decltype(F32)::value, EG>),
+                         dim3(dx_blocks + dw_workgroups(a)), dim3(kDwWaves * kWave), 0, s, a,
+                         dX_add, dX, dx_blocks);
+    }
+  });
   return hipGetLastError();
 }
 
@@ -1481,7 +1489,7 @@ hipError_t launch_balance_dw_sum(const float* part, const float* stats, const fl
   const int padded = 32 * balance_blocks(Ne), dh4 = dh / 4;
   const dim3 grid((unsigned)ceil_div(Ne * dh4, 256), (unsigned)Nh);
   hipLaunchKernelGGL(balance_dw_sum_kernel, grid, dim3(256), 0, s,
-                     reinterpret_cast<const f32x4*>(part), balance_splits(T, Nh, Ne),
+                     reinterpret_cast<const f32x4*>(part), balance_splits(T, Nh, dh, Ne),
                      (int64_t)Nh * padded * dh4, reinterpret_cast<const float2*>(stats) + T * Nh,
                      dloss, reinterpret_cast<const f32x4*>(dW_add), Ne, padded, dh4,
                      reinterpret_cast<f32x4*>(dW));

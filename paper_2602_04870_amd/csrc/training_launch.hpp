@@ -118,16 +118,21 @@ inline int64_t balance_token_blocks(int64_t T, int Nh, int Ne) {
 inline bool balance_loss_at_once(int64_t T, int Nh, int Ne) {
   return T > 0 && balance_few(T, Nh, Ne) && balance_token_blocks(T, Nh, Ne) == 1;
 }
-// dW: blocks of experts that a workgroup's four wavefronts have (they share them out
-// over the tokens where there are fewer than three), and the chunks that the tokens
-// are cut into, of at least four tiles, so that there are about 512 workgroups, two per
-// CU at once (us of the gradient in bf16 with 512 and 1024: 122 and 138 at 16384 x 16
-// heads x 128 experts, 63 and 76 at 8192 x 8 x 256, 1024 and 1029 at 65536 x 8 x 1024).
-inline int balance_dw_blocks(int Ne) { return Ne <= 32 ? 1 : Ne <= 64 ? 2 : 4; }
-inline int64_t balance_splits(int64_t T, int Nh, int Ne) {
-  const int ew = balance_dw_blocks(Ne);
+// dW: blocks of experts that a workgroup has, a wavefront each (four wavefronts share
+// them out over the tokens where there are fewer than three), and the chunks that the
+// tokens are cut into, of at least four tiles, so that there are eight wavefronts per
+// CU at once (us of the gradient in bf16 with 512 workgroups of four wavefronts and with
+// 1024: 122 and 138 at 16384 x 16 heads x 128 experts).  Eight blocks share the splitting of
+// their tokens' X (65536 x 8 x 1024: 942 us, with four 1017; d_h 64: 97, 94 at 16384 x
+// 16 x 200).
+inline int balance_dw_blocks(int64_t T, int Nh, int dh, int Ne) {
+  return Ne <= 32 ? 1 : Ne <= 64 ? 2 : Ne <= 128 || dh < 128 || balance_few(T, Nh, Ne) ? 4 : 8;
+}
+inline int64_t balance_splits(int64_t T, int Nh, int dh, int Ne) {
+  const int ew = balance_dw_blocks(T, Nh, dh, Ne);
   const int64_t groups = Nh * ceil_div(balance_blocks(Ne), ew);
-  const int64_t want = ceil_div(512, groups), most = ceil_div(T, 4 * 32 * (4 / ew));
+  const int64_t want = ceil_div(ew == 8 ? 256 : 512, groups);
+  const int64_t most = ceil_div(T, 4 * 32 * (ew < 4 ? 4 / ew : 1));
   return want < most ? want : most;
 }
 hipError_t launch_balance_weights(const float* W, const int32_t* counts, int Nh, int dh, int Ne,

@@ -55,7 +55,10 @@ def test_expert_counts_are_the_routers():
 CASES = [  # T, Nh, dh, Ne, k
     (1, 1, 64, 1, 1), (1, 2, 128, 4, 2), (31, 1, 64, 31, 3), (33, 3, 128, 33, 4), (130, 2, 64, 65, 8),
     (257, 2, 128, 96, 4), (300, 1, 128, 1024, 32), (515, 3, 64, 200, 4), (1100, 2, 128, 130, 2),
-    (2500, 1, 64, 8, 2)]
+    (2500, 1, 64, 8, 2),
+    # enough tokens that the weights are laid out first: one, two, four and more blocks of experts
+    (33100, 1, 64, 20, 2), (16601, 1, 128, 50, 2), (8200, 1, 128, 100, 3), (2900, 3, 64, 129, 3),
+    (4150, 2, 128, 300, 4)]
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])

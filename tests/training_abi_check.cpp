@@ -63,8 +63,8 @@ int main() {
                       st == MHLMOE_OK ? b : 0);
           // every launch is of fewer than 2^32 threads, the partial results' count is T's
           if (st == MHLMOE_OK) {
-            const int64_t splits = mhl::balance_splits(T, Nh, Ne);
-            const int64_t groups = mhl::ceil_div(mhl::balance_blocks(Ne), mhl::balance_dw_blocks(Ne));
+            const int64_t splits = mhl::balance_splits(T, Nh, dh, Ne);
+            const int64_t groups = mhl::ceil_div(mhl::balance_blocks(Ne), mhl::balance_dw_blocks(T, Nh, dh, Ne));
             expect("splits", splits <= 1024 && (T == 0 || splits >= 1), 1);
             expect("dw", (Nh * splits + 7) * groups < (int64_t(1) << 24), 1);
             expect("tokens", Nh * mhl::balance_token_blocks(T, Nh, Ne) < (int64_t(1) << 24), 1);
