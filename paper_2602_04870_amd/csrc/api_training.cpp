@@ -43,8 +43,8 @@ mhlmoe_status check_workspace(const void* ws, size_t have, size_t need_bytes) {
 
 size_t layernorm_bwd_bytes(int64_t T, int d_model, size_t* rows_at) {
   size_t cur = 0;
-  bump(cur, sizeof(float) * 2 * (size_t)mhl::rmsnorm_bwd_parts(T, d_model) * d_model);
-  const size_t at = bump(cur, mhl::rmsnorm_bwd_wide(d_model)
+  bump(cur, sizeof(float) * 2 * (size_t)mhl::layernorm_bwd_parts(T, d_model) * d_model);
+  const size_t at = bump(cur, mhl::layernorm_bwd_wide(d_model)
                                   ? mhl::kLayernormRowFloats * sizeof(float) * (size_t)T
                                   : 0);
   if (rows_at) *rows_at = at;
@@ -221,7 +221,7 @@ mhlmoe_status mhlmoe_layernorm_backward(const void* h, const float* weight, cons
                                        dx, part, at<float>(workspace, rows_at), stream);
     }));
   return run_kernel("layernorm_dw", stream, [&] {
-    return mhl::launch_layernorm_dw(part, mhl::rmsnorm_bwd_parts(T, d_model), d_model, dweight,
+    return mhl::launch_layernorm_dw(part, mhl::layernorm_bwd_parts(T, d_model), d_model, dweight,
                                     dbias, stream);
   });
 }

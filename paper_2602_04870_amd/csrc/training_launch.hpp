@@ -14,10 +14,21 @@ hipError_t launch_layernorm(const void* x, const void* residual, const float* w,
                             int64_t T, int d, float eps, bool f32, void* sum, void* y, void* q,
                             float* scales, hipStream_t s);
 
-// The gradient: dx, and dw and db as rmsnorm_bwd_parts partial rows of 2 d floats,
+// Rows are held as the RMS norm's of the next multiple of 8 (NormForm; the wide ones of
+// no multiple of 8 column by column).
+inline NormForm layernorm_form(int d) { return norm_form((d + 7) / 8 * 8); }
+inline bool layernorm_bwd_wide(int d) { return layernorm_form(d) >= NormForm::kLarge8; }
+
+// The gradient: dx, and dw and db as layernorm_bwd_parts partial rows of 2 d floats,
 // which launch_layernorm_dw adds in order (db may be NULL).  rows:
-// kLayernormRowFloats T floats where rmsnorm_bwd_wide, else unused.
+// kLayernormRowFloats T floats where layernorm_bwd_wide, else unused.
 constexpr int kLayernormRowFloats = 5;
+inline int64_t layernorm_bwd_parts(int64_t T, int d) {
+  const int padded = (d + 7) / 8 * 8;
+  if (!layernorm_bwd_wide(d)) return rmsnorm_bwd_parts(T, padded);
+  const int64_t fill = (int64_t(1) << (d % 8 == 0 ? 22 : 19)) / d, most = fill > 16 ? fill : 16;
+  return ceil_div(T, 8) < most ? ceil_div(T, 8) : most;
+}
 hipError_t launch_layernorm_bwd(const void* h, const float* w, const void* dy, const void* dsum,
                                 int64_t T, int d, float eps, bool f32, void* dx, float* part,
                                 float* rows, hipStream_t s);
