@@ -25,7 +25,13 @@ inline bool layernorm_bwd_wide(int d) { return layernorm_form(d) >= NormForm::kL
 constexpr int kLayernormRowFloats = 5;
 inline int64_t layernorm_bwd_parts(int64_t T, int d) {
   const int padded = (d + 7) / 8 * 8;
-  if (!layernorm_bwd_wide(d)) return rmsnorm_bwd_parts(T, padded);
+  if (!layernorm_bwd_wide(d)) {
+    // A workgroup per row: at least two rows to a partial one, four of more than 8192
+    // columns (us with one, two, four: 20, 16, 20 at 300 x 8192, 62, 62, 49 at 1000 x 16000).
+    const int64_t n = rmsnorm_bwd_parts(T, padded);
+    const int64_t most = norm_rows(layernorm_form(d)) > 1 ? n : ceil_div(T, padded > 8192 ? 4 : 2);
+    return n < most ? n : most;
+  }
   const int64_t fill = (int64_t(1) << (d % 8 == 0 ? 22 : 19)) / d, most = fill > 16 ? fill : 16;
   return ceil_div(T, 8) < most ? ceil_div(T, 8) : most;
 }
