@@ -331,14 +331,22 @@ mhlmoe_status mhlmoe_balance_loss_backward(
       return mhl::launch_balance_weights(W_router, counts, n_heads, d_head, n_experts, weights,
                                          stream);
     }));
-    MHL_TRY(run_kernel("balance_dx", stream, [&] {
-      return mhl::launch_balance_dx(X, weights, stats, dloss, mask, dX_add, T, n_heads, d_head,
-                                    n_experts, f32, dX, stream);
-    }));
-    MHL_TRY(run_kernel("balance_dw", stream, [&] {
-      return mhl::launch_balance_dw(X, W_router, counts, stats, dloss, mask, dW_add, T, n_heads,
-                                    d_head, n_experts, f32, dW_router, part, stream);
-    }));
+    if (mhl::balance_together(T, n_heads, d_head, n_experts)) {
+      MHL_TRY(run_kernel("balance_dx_dw", stream, [&] {
+        return mhl::launch_balance_dw_dx(X, W_router, weights, counts, stats, dloss, mask, dX_add,
+                                         dW_add, T, n_heads, d_head, n_experts, f32, dX, dW_router,
+                                         part, stream);
+      }));
+    } else {
+      MHL_TRY(run_kernel("balance_dx", stream, [&] {
+        return mhl::launch_balance_dx(X, weights, stats, dloss, mask, dX_add, T, n_heads, d_head,
+                                      n_experts, f32, dX, stream);
+      }));
+      MHL_TRY(run_kernel("balance_dw", stream, [&] {
+        return mhl::launch_balance_dw(X, W_router, counts, stats, dloss, mask, dW_add, T, n_heads,
+                                      d_head, n_experts, f32, dW_router, part, stream);
+      }));
+    }
   }
   if (mhl::balance_splits(T, n_heads, d_head, n_experts) == 1) return MHLMOE_OK;
   return run_kernel("balance_sum", stream, [&] {

@@ -851,32 +851,51 @@ __device__ __forceinline__ float head_down(const HeadInfo& info, int nb) {
   return uniform(d);
 }
 
+struct DxArgs {
+  const void* X;
+  const uint8_t* weights;
+  const HeadInfo* info;
+  const float2* stats;
+  const float* dloss;
+  const uint8_t* mask;
+  const void* dX_add;
+  int64_t T;
+  int Nh, Ne;
+  void* dX;
+};
+template <int DH>
+struct DxShared {
+  __align__(16) uint8_t w[2][2 * Tile<DH>::kBytes];
+  __align__(16) float fex[kMaxExperts];
+};
+
 template <int DH, bool F32>
-__global__ __launch_bounds__(kTokenWaves* kWave) void balance_dx_kernel(
-    const void* __restrict__ X, const uint8_t* __restrict__ weights,
-    const HeadInfo* __restrict__ info, const float2* __restrict__ stats,
-    const float* __restrict__ dloss, const uint8_t* __restrict__ mask, const void* dX_add,
-    int64_t T, int Nh, int Ne, void* dX) {
+__device__ __forceinline__ void balance_dx(const DxArgs& a, unsigned block, DxShared<DH>& sm) {
   constexpr int NP = F32 ? 2 : 1;
   constexpr uint32_t kBlock = 2 * Tile<DH>::kBytes;
-  __shared__ __align__(16) uint8_t w[2][kBlock];
-  __shared__ __align__(16) float fex[kMaxExperts];
-  const int h = blockIdx.x % Nh, lane = lane_id(), g = lane >> 5, wave = threadIdx.x >> 6;
-  const int64_t t = (int64_t)(blockIdx.x / Nh) * kBalanceTokens + wave * 32 + (lane & 31);
+  const float2* __restrict__ stats = a.stats;
+  const HeadInfo* __restrict__ info = a.info;
+  const uint8_t* __restrict__ mask = a.mask;
+  const int64_t T = a.T;
+  const int Nh = a.Nh, Ne = a.Ne;
+  auto& w = sm.w;
+  auto& fex = sm.fex;
+  const int h = block % Nh, lane = lane_id(), g = lane >> 5, wave = threadIdx.x >> 6;
+  const int64_t t = (int64_t)(block / Nh) * kBalanceTokens + wave * 32 + (lane & 31);
   const int64_t row = t * Nh + h;
   const bool ok = t < T && (!mask || mask[t < T ? t : 0]);
   const int nb = (Ne + 31) / 32;
-  const u32x4 rsrc = buffer_words(weights + (int64_t)h * nb * kBlock, (uint32_t)nb * kBlock);
+  const u32x4 rsrc = buffer_words(a.weights + (int64_t)h * nb * kBlock, (uint32_t)nb * kBlock);
   fetch_block<DH>(rsrc, 0, w[0]);
   const Tile<DH> at;
   for (int e = threadIdx.x; e < nb * 32; e += kTokenWaves * kWave) fex[e] = info[h].f[e];
   XOperand<DH, F32> x;
-  x.load(X, (t < T ? t : T - 1) * Nh + h, ok, g);
+  x.load(a.X, (t < T ? t : T - 1) * Nh + h, ok, g);
   // a token that does not count: p = exp2(-infinity) = 0
   const float2 st = ok ? stats[row] : float2{INFINITY, 0.0f};
   const float down = head_down(info[h], nb), F = info[h].F;
   const float u = st.y, lse = st.x * kLog2e - F;
-  const float c = dloss[h] * stats[T * Nh + h].x * __builtin_amdgcn_ldexpf(down, -(int)F);
+  const float c = a.dloss[h] * stats[T * Nh + h].x * __builtin_amdgcn_ldexpf(down, -(int)F);
   f32x16 dx[DH / 32];
 #pragma unroll
   for (int i = 0; i < DH / 32; ++i) dx[i] = zero16();
@@ -899,7 +918,13 @@ __global__ __launch_bounds__(kTokenWaves* kWave) void balance_dx_kernel(
   }
   __syncthreads();  // the weights' LDS is the rows' now
   store_dx_rows<DH, F32>(dx, ok, c, t - (lane & 31), T, Nh, h, &w[0][0] + wave * Tile<DH>::kBytes,
-                         dX_add, dX);
+                         a.dX_add, a.dX);
+}
+
+template <int DH, bool F32>
+__global__ __launch_bounds__(kTokenWaves* kWave) void balance_dx_kernel(const DxArgs a) {
+  __shared__ DxShared<DH> sm;
+  balance_dx<DH, F32>(a, blockIdx.x, sm);
 }
 
 // ---------------------------------------------------------------------------
@@ -1153,6 +1178,24 @@ __global__ __launch_bounds__(dw_waves(EW)* kWave) void balance_dw_kernel(const D
   balance_dw<DH, F32, EW>(a, blockIdx.x, sm);
 }
 
+// dW (first, its workgroups take longest) and dX in one launch, where neither fills the
+// card.
+template <int DH, bool F32, int EW>
+__global__ __launch_bounds__(kDwWaves* kWave) void balance_dw_dx_kernel(const DwArgs dw,
+                                                                        const DxArgs dx,
+                                                                        unsigned dw_blocks) {
+  static_assert(kDwWaves == kTokenWaves, "one launch");
+  __shared__ union Shared {
+    DwShared<DH, F32, EW> dw;
+    DxShared<DH> dx;
+    __device__ Shared() {}
+  } sm;
+  if (blockIdx.x < dw_blocks)
+    balance_dw<DH, F32, EW>(dw, blockIdx.x, sm.dw);
+  else
+    balance_dx<DH, F32>(dx, blockIdx.x - dw_blocks, sm.dx);
+}
+
 // ---------------------------------------------------------------------------
 // The gradient where there are few tokens, in one launch: the first workgroups make dX,
 // the others dW.  For dX EG wavefronts of a workgroup take the blocks of experts in turn,
@@ -1402,19 +1445,6 @@ hipError_t launch_balance_loss_sum(const double* part, const int32_t* counts, co
   return hipGetLastError();
 }
 
-hipError_t launch_balance_dx(const void* X, const void* weights, const float* stats,
-                             const float* dloss, const uint8_t* mask, const void* dX_add, int64_t T,
-                             int Nh, int dh, int Ne, bool f32, void* dX, hipStream_t s) {
-  const dim3 grid((unsigned)(Nh * ceil_div(T, kBalanceTokens)));
-#define MHL_DX(DH, F32)                                                                       \
-  hipLaunchKernelGGL((balance_dx_kernel<DH, F32>), grid, dim3(kTokenWaves* kWave), 0, s, X,   \
-                     static_cast<const uint8_t*>(weights), head_info(weights, Nh, dh, Ne),      \
-                     reinterpret_cast<const float2*>(stats), dloss, mask, dX_add, T, Nh, Ne, dX)
-  MHL_BALANCE_TYPES(MHL_DX)
-#undef MHL_DX
-  return hipGetLastError();
-}
-
 static DwArgs dw_args(const void* X, const float* W, const int32_t* counts, const float* stats,
                       const float* dloss, const uint8_t* mask, const float* dW_add, int64_t T,
                       int Nh, int dh, int Ne, float* dW, float* part) {
@@ -1452,6 +1482,19 @@ static void for_dw(int dh, bool f32, int ew, F&& call) {
     blocks(Int<64>{}, std::false_type{});
 }
 
+hipError_t launch_balance_dx(const void* X, const void* weights, const float* stats,
+                             const float* dloss, const uint8_t* mask, const void* dX_add, int64_t T,
+                             int Nh, int dh, int Ne, bool f32, void* dX, hipStream_t s) {
+  const DxArgs a{X, static_cast<const uint8_t*>(weights), head_info(weights, Nh, dh, Ne),
+                 reinterpret_cast<const float2*>(stats), dloss, mask, dX_add, T, Nh, Ne, dX};
+  const dim3 grid((unsigned)(Nh * ceil_div(T, kBalanceTokens)));
+#define MHL_DX(DH, F32) \
+  hipLaunchKernelGGL((balance_dx_kernel<DH, F32>), grid, dim3(kTokenWaves* kWave), 0, s, a)
+  MHL_BALANCE_TYPES(MHL_DX)
+#undef MHL_DX
+  return hipGetLastError();
+}
+
 hipError_t launch_balance_dw(const void* X, const float* W, const int32_t* counts,
                              const float* stats, const float* dloss, const uint8_t* mask,
                              const float* dW_add, int64_t T, int Nh, int dh, int Ne, bool f32,
@@ -1461,6 +1504,25 @@ hipError_t launch_balance_dw(const void* X, const float* W, const int32_t* count
     hipLaunchKernelGGL((balance_dw_kernel<decltype(DH)::value, decltype(F32)::value,
                                           decltype(EW)::value>),
                        dim3(dw_workgroups(a)), dim3(dw_waves(decltype(EW)::value) * kWave), 0, s, a);
+  });
+  return hipGetLastError();
+}
+
+hipError_t launch_balance_dw_dx(const void* X, const float* W, const void* weights,
+                                const int32_t* counts, const float* stats, const float* dloss,
+                                const uint8_t* mask, const void* dX_add, const float* dW_add,
+                                int64_t T, int Nh, int dh, int Ne, bool f32, void* dX, float* dW,
+                                float* part, hipStream_t s) {
+  const DwArgs dw = dw_args(X, W, counts, stats, dloss, mask, dW_add, T, Nh, dh, Ne, dW, part);
+  const DxArgs dx{X, static_cast<const uint8_t*>(weights), head_info(weights, Nh, dh, Ne),
+                  reinterpret_cast<const float2*>(stats), dloss, mask, dX_add, T, Nh, Ne, dX};
+  const unsigned dw_blocks = dw_workgroups(dw);
+  const dim3 grid(dw_blocks + (unsigned)(Nh * ceil_div(T, kBalanceTokens)));
+  for_dw(dh, f32, balance_dw_blocks(T, Nh, dh, Ne), [&](auto DH, auto F32, auto EW) {
+    if constexpr (decltype(EW)::value <= kDwWaves)
+      hipLaunchKernelGGL((balance_dw_dx_kernel<decltype(DH)::value, decltype(F32)::value,
+                                               decltype(EW)::value>),
+                         grid, dim3(kDwWaves * kWave), 0, s, dw, dx, dw_blocks);
   });
   return hipGetLastError();
 }

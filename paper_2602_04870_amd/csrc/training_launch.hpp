@@ -152,6 +152,16 @@ inline int64_t balance_splits(int64_t T, int Nh, int dh, int Ne) {
   const int64_t most = ceil_div(T, 4 * 32 * (ew < 4 ? 4 / ew : 1));
   return want < most ? want : most;
 }
+// Where not few tokens: dX and dW in one launch, whose workgroups then fill the card
+// together, unless dX loses too much by dW's registers and LDS.  us together / apart in
+// bf16 at 16 heads (fp32 alike):
+//   d_h   64: 33 / 39 at 3001 tokens x 200 experts, 84 / 93 at 32768 x 64
+//   d_h  128: 26 / 36 at 2000 x 100, 114 / 120 at 16384 x 128, 388 / 385 at 65536 x 128;
+//             30 / 38 at 2500 x 20, 48 / 45 at 6000 x 16, 112 / 95 at 16384 x 16
+inline bool balance_together(int64_t T, int Nh, int dh, int Ne) {
+  const int ew = balance_dw_blocks(T, Nh, dh, Ne);
+  return ew <= 4 && (dh < 128 || Nh * ceil_div(T, kBalanceTokens) <= (ew == 1 ? 512 : 2048));
+}
 hipError_t launch_balance_weights(const float* W, const int32_t* counts, int Nh, int dh, int Ne,
                                   void* out, hipStream_t s);
 hipError_t launch_balance_loss(const void* X, const float* W, const void* weights,
@@ -168,6 +178,12 @@ hipError_t launch_balance_dw(const void* X, const float* W, const int32_t* count
                              const float* stats, const float* dloss, const uint8_t* mask,
                              const float* dW_add, int64_t T, int Nh, int dh, int Ne, bool f32,
                              float* dW, float* part, hipStream_t s);
+// Both in one launch where balance_together.
+hipError_t launch_balance_dw_dx(const void* X, const float* W, const void* weights,
+                                const int32_t* counts, const float* stats, const float* dloss,
+                                const uint8_t* mask, const void* dX_add, const float* dW_add,
+                                int64_t T, int Nh, int dh, int Ne, bool f32, void* dX, float* dW,
+                                float* part, hipStream_t s);
 // dX and dW where balance_few.
 hipError_t launch_balance_bwd_few(const void* X, const float* W, const int32_t* counts,
                                   const float* stats, const float* dloss, const uint8_t* mask,
