@@ -106,6 +106,7 @@ __global__ __launch_bounds__(kCountThreads) void expert_counts_kernel(
 // ---------------------------------------------------------------------------
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
 typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
 
 __device__ __forceinline__ f32x16 mfma32_f16(u32x4 a, u32x4 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a),
@@ -121,6 +122,31 @@ __device__ __forceinline__ float minus_half(float v, uint32_t pair) {
   else
     asm("v_fma_mix_f32 %0, -%1, 1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(r) : "v"(pair), "v"(v));
   return r;
+}
+
+// Eight values times a power of two as N fp16 pieces, each the nearest to what the ones
+// before left.  The multiply comes with the conversion (v_fma_mix*_f16).
+template <int N>
+__device__ __forceinline__ void split8(const float (&f)[8], float up, u32x4 (&out)[N]) {
+  static_assert(N <= 2, "pieces");
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t w;
+    asm("v_fma_mixlo_f16 %0, %1, %2, 0" : "=v"(w) : "v"(f[2 * i]), "v"(up));
+    asm("v_fma_mixhi_f16 %0, %1, %2, 0" : "+v"(w) : "v"(f[2 * i + 1]), "v"(up));
+    out[0][i] = w;
+  }
+  if constexpr (N == 2) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float a, b;
+      asm("v_fma_mix_f32 %0, %1, %2, -%3 op_sel:[0,0,0] op_sel_hi:[0,0,1]"
+          : "=v"(a) : "v"(f[2 * i]), "v"(up), "v"(out[0][i]));
+      asm("v_fma_mix_f32 %0, %1, %2, -%3 op_sel:[0,0,1] op_sel_hi:[0,0,1]"
+          : "=v"(b) : "v"(f[2 * i + 1]), "v"(up), "v"(out[0][i]));
+      out[1][i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), f16x2));
+    }
+  }
 }
 
 // Eight values as N fp16 pieces, each the nearest to what the ones before left.
@@ -301,10 +327,8 @@ __global__ __launch_bounds__(256) void balance_weights_kernel(const float* __res
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
     const int unit = i * 256 + threadIdx.x;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[i][j] *= scale.up;
     u32x4 p[2];
-    split8(v[i], p);
+    split8(v[i], scale.up, p);
 #pragma unroll
     for (int q = 0; q < 2; ++q)
       *reinterpret_cast<u32x4*>(o + q * Tile<DH>::kBytes +
@@ -319,25 +343,28 @@ struct XOperand {
   static constexpr int NX = F32 ? 2 : 1;
   u32x4 x[NX][DH / 16];
   float down;
-  // row: readable; ok: whether it counts (zeros otherwise).
-  __device__ __forceinline__ void load(const void* X, int64_t row, bool ok, int g) {
-    u32x4 raw[DH / 16][F32 ? 2 : 1];
+  u32x4 raw[DH / 16][F32 ? 2 : 1];
+  // A readable row on its way; then as an operand, zeros unless ok (it counts).
+  __device__ __forceinline__ void fetch(const void* X, int64_t row, int g) {
     const uint8_t* p = static_cast<const uint8_t*>(X) + (row * DH + 8 * g) * (F32 ? 4 : 2);
 #pragma unroll
     for (int s = 0; s < DH / 16; ++s)
 #pragma unroll
       for (int i = 0; i < (F32 ? 2 : 1); ++i)
         raw[s][i] = *reinterpret_cast<const u32x4*>(p + 16 * s * (F32 ? 4 : 2) + 16 * i);
+  }
+  __device__ __forceinline__ void convert(bool ok) {
+    if (__any(!ok)) {
 #pragma unroll
-    for (int s = 0; s < DH / 16; ++s)
+      for (int s = 0; s < DH / 16; ++s)
 #pragma unroll
-      for (int i = 0; i < (F32 ? 2 : 1); ++i)
-        if (!ok) raw[s][i] = u32x4{0, 0, 0, 0};
+        for (int i = 0; i < (F32 ? 2 : 1); ++i)
+          if (!ok) raw[s][i] = u32x4{0, 0, 0, 0};
+    }
     uint32_t top = 0;
 #pragma unroll
-    for (int s = 0; s < DH / 16; ++s)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) top = umax(top, bits_abs(value(raw[s], i)));
+    for (int s = 0; s < DH / 16; ++s) top = top_of(raw[s], top);
+    top = widen(top);
     top = umax(top, __shfl_xor(top, 32, kWave));
     const Pow2 scale = pow2_below_2_15(top);
     down = scale.down;
@@ -346,11 +373,36 @@ struct XOperand {
       float f[8];
       u32x4 o[NX];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) f[i] = value(raw[s], i) * scale.up;
-      split8(f, o);
+      for (int i = 0; i < 8; ++i) f[i] = value(raw[s], i);
+      split8(f, scale.up, o);
 #pragma unroll
       for (int q = 0; q < NX; ++q) x[q][s] = o[q];
     }
+  }
+  __device__ __forceinline__ void load(const void* X, int64_t row, bool ok, int g) {
+    fetch(X, row, g);
+    convert(ok);
+  }
+  // The largest magnitude of eight and of top, for bf16 two at once, and its bits as fp32.
+  template <int N>
+  static __device__ __forceinline__ uint32_t top_of(const u32x4 (&raw)[N], uint32_t top) {
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (F32) {
+          top = umax(top, raw[n][i] & 0x7FFFFFFFu);
+        } else {
+          const uint32_t w = raw[n][i] & 0x7FFF7FFFu;
+          top = __builtin_bit_cast(
+              uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, top),
+                                                  __builtin_bit_cast(u16x2, w)));
+        }
+      }
+    return top;
+  }
+  static __device__ __forceinline__ uint32_t widen(uint32_t top) {
+    return F32 ? top : umax(top << 16, top & 0xFFFF0000u);
   }
   // element i of eight as they lie in memory
   template <int N>
@@ -390,10 +442,8 @@ struct WOperand {
     down = scale.down;
 #pragma unroll
     for (int s = 0; s < DH / 16; ++s) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[s][j] *= scale.up;
       u32x4 o[2];
-      split8(v[s], o);
+      split8(v[s], scale.up, o);
       w[0][s] = o[0];
       w[1][s] = o[1];
     }
@@ -550,14 +600,18 @@ __global__ __launch_bounds__(kTokenWaves* kWave) void balance_loss_kernel(
   __shared__ double loss[kTokenWaves];
   const int h = blockIdx.x % Nh, lane = lane_id(), g = lane >> 5, wave = threadIdx.x >> 6;
   const int64_t tb = blockIdx.x / Nh, t = tb * kBalanceTokens + wave * 32 + (lane & 31);
-  const bool ok = t < T && (!mask || mask[t < T ? t : 0]);
+  const int64_t near = t < T ? t : T - 1;
   const int nb = (Ne + 31) / 32;
   const u32x4 rsrc = buffer_words(weights + (int64_t)h * nb * kBlock, (uint32_t)nb * kBlock);
   fetch_block<DH>(rsrc, 0, w[0]);
   const Tile<DH> at;
-  for (int e = threadIdx.x; e < nb * 32; e += kTokenWaves * kWave) fex[e] = info[h].f[e];
+  // (workgroups that go on to further tokens, fetched ahead, gave nothing: 322.9 -> 330 us at
+  // 65536 x 8 heads x 1024 experts, 43.1 -> 43 at 16384 x 16 x 128 with its counts)
   XOperand<DH, F32> x;
-  x.load(X, (t < T ? t : T - 1) * Nh + h, ok, g);
+  x.fetch(X, near * Nh + h, g);
+  const bool ok = (mask ? mask[near] != 0 : true) && t < T;
+  for (int e = threadIdx.x; e < nb * 32; e += kTokenWaves * kWave) fex[e] = info[h].f[e];
+  x.convert(ok);
   Running run;
   for (int b = 0; b < nb; ++b) {
     const float m = x.down * info[h].down[b] * kLog2e;
@@ -1040,19 +1094,19 @@ __device__ __forceinline__ void balance_dw(const DwArgs& a, unsigned block,
     for (int i = 0; i < kPer; ++i) {
       const int unit = i * dw_waves(EW) * kWave + threadIdx.x, r = unit / kUnits;
       const bool ok = tile * kTokens + r < T && counted[i];
-      float v[8];
-      uint32_t top = 0;
+      if (__any(!ok)) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        v[k] = ok ? XOperand<DH, F32>::value(raw[i], k) : 0.0f;
-        top = umax(top, bits_abs(v[k]));
+        for (int k = 0; k < (F32 ? 2 : 1); ++k)
+          if (!ok) raw[i][k] = u32x4{0, 0, 0, 0};
       }
-      top = row_max<kUnits>(top);
-      const Pow2 scale = pow2_below_2_15(top);
+      using Row = XOperand<DH, F32>;
+      const Pow2 scale =
+          pow2_below_2_15(row_max<kUnits>(Row::widen(Row::top_of(raw[i], 0u))));
+      float v[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] *= scale.up;
+      for (int k = 0; k < 8; ++k) v[k] = Row::value(raw[i], k);
       u32x4 o[NX];
-      split8(v, o);
+      split8(v, scale.up, o);
 #pragma unroll
       for (int p = 0; p < NX; ++p)
         *reinterpret_cast<u32x4*>(xs + (buf * NX + p) * kPiece +
