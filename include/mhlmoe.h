@@ -688,7 +688,8 @@ mhlmoe_status mhlmoe_expert_counts(const int32_t *idx, const uint8_t *mask,
  *            where it does not count), and 1 / max(n, 1) and 0 as row T (out)
  * X may hold anything at tokens that do not count, NaN and infinities too.
  * Scores are of fp32 accuracy (the paper's FP32 router) and never leave the chip.
- * A token with a score that is not finite makes its head's loss NaN.
+ * A token with a score that is not finite makes its head's loss NaN.  |X| must stay
+ * below 2^64 (the gradient's intermediate values overflow beyond).
  * d_head 64 or 128, 1 <= n_heads, n_experts <= 1024, (T + 128) * n_heads < 2^31.
  */
 mhlmoe_status mhlmoe_balance_loss_workspace(int64_t T, int n_heads, int d_head,
@@ -716,7 +717,9 @@ mhlmoe_status mhlmoe_balance_loss(const void *X, const float *W_router,
  *             dX_add; not X                                           (out)
  *   dW_router [n_heads][n_experts][d_head] float; not W_router        (out)
  * The other arguments are those of the mhlmoe_balance_loss call that wrote
- * stats.  dX_add (dW_add) is added in fp32 before the one rounding of dX.
+ * stats.  dX_add (dW_add) is added in fp32 before the one rounding of dX.  Products
+ * are of fp32 accuracy, but for a bf16 dX, whose terms are off by up to 2^-10 of
+ * themselves each before they are added in fp32.
  */
 mhlmoe_status mhlmoe_balance_loss_backward_workspace(int64_t T, int n_heads,
                                                      int d_head, int n_experts,

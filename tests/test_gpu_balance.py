@@ -106,6 +106,51 @@ def test_balance_loss_and_gradient(T, Nh, dh, Ne, k, dtype, mask):
             assert torch.equal(gX, dX) and torch.equal(gW, dW)
 
 
+def test_balance_past_4_gib():
+    """More than 2^31 elements of X: the last tokens are those of a call of their own on
+    the same counts."""
+    T, Nh, dh, Ne, n = 140000, 128, 128, 6, 300
+    announce(f"balance T={T} Nh={Nh}")
+    g = _gen(92)
+    X = torch.zeros(T, Nh, dh, dtype=BF16, device="cuda")
+    X[-n:] = _randn(g, n, Nh, dh, dtype=BF16)
+    W = _randn(g, Nh, Ne, dh) * 0.1
+    counts = torch.randint(1, 1000, (Nh, Ne), generator=g, device="cuda", dtype=torch.int32)
+    loss, stats = mh.mhlmoe_balance_loss(X, W, counts)
+    _, tail = mh.mhlmoe_balance_loss(X[-n:], W, counts)
+    # every form is within e_lse and e_u of the exact value: twice that apart
+    b = ref.Balance(ref.host(X[-n:, :2]), ref.host(W[:2]), counts[:2].cpu().numpy().astype(np.int64), None)
+    s, t = ref.host(stats[T - n:T, :2]), ref.host(tail[:n, :2])
+    assert np.all(np.abs(s[..., 0] - t[..., 0]) <= 2 * b.e_lse)
+    assert np.all(np.abs(s[..., 1] - t[..., 1]) <= 2 * b.e_u + 4 * ref.U * np.abs(b.u))
+    dloss = torch.ones(Nh, device="cuda")
+    dX, dW = mh.mhlmoe_balance_loss_backward(X, W, counts, stats, dloss)
+    part = torch.cat([stats[T - n:T], stats[T:]]).contiguous()
+    tX, _ = mh.mhlmoe_balance_loss_backward(X[-n:].contiguous(), W, counts, part, dloss)
+    wX, _, off, _ = b.backward(np.full(2, n / T), None, None, True)  # (its n is that of the tail)
+    for got in (dX[-n:, :2], tX[:, :2]):
+        assert np.all(np.abs(ref.host(got) - wX) <= off + ref.HALF[BF16] * (np.abs(wX) + off) + 2.0 ** -133)
+    assert torch.isfinite(dW).all() and torch.isfinite(loss).all()
+
+
+def test_balance_on_another_stream_than_the_current():
+    """Given by argument: the call's own workspace and outputs belong to that stream."""
+    g, X, W, idx, m = _problem(5000, 4, 64, 100, 4, BF16, "some", 21)
+    counts = mh.mhlmoe_expert_counts(idx, 100, mask=m)
+    want = mh.mhlmoe_balance_loss(X, W, counts, mask=m)
+    wantb = mh.mhlmoe_balance_loss_backward(X, W, counts, want[1], torch.ones(4, device="cuda"), mask=m)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    one = torch.ones(4, device="cuda")
+    side.wait_stream(torch.cuda.current_stream())
+    c = mh.mhlmoe_expert_counts(idx, 100, mask=m, stream=side)
+    got = mh.mhlmoe_balance_loss(X, W, c, mask=m, stream=side)
+    gotb = mh.mhlmoe_balance_loss_backward(X, W, c, got[1], one, mask=m, stream=side)
+    side.synchronize()
+    for a, b in zip((counts, *want, *wantb), (c, *got, *gotb)):
+        assert torch.equal(a, b)
+
+
 def test_balance_gradient_against_differences():
     """dX and dW against central differences of the 64-bit loss."""
     T, Nh, dh, Ne = 40, 2, 64, 24

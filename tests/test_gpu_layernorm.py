@@ -159,6 +159,49 @@ def test_layernorm_gradient_against_differences():
         assert abs((grad * v).sum() - diff) <= 1e-5 * np.abs(grad * v).sum()
 
 
+@pytest.mark.parametrize("d", [33001, 65535, 65536])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_layernorm_widest(d, dtype):
+    """Rows that no workgroup holds, forward and gradient."""
+    g = _gen(d)
+    T = 19
+    x, dy = (_randn(g, T, d) + _randn(g, T, 1)).to(dtype), _randn(g, T, d, dtype=dtype)
+    r, w, b = _randn(g, T, d, dtype=dtype), 1 + 0.3 * _randn(g, d), _randn(g, d)
+    out = mh.mhlmoe_layernorm(x, w, EPS, bias=b, residual=r)
+    h = (x.float() + r.float()).to(dtype)
+    assert torch.equal(out["sum"], h)
+    want, off = ref.layernorm64(ref.host(h), ref.host(w), ref.host(b), EPS)
+    assert np.all(np.abs(ref.host(out["y"]) - want) <= off + ref.HALF[dtype] * (np.abs(want) + off))
+    dx, dw, db = mh.mhlmoe_layernorm_backward(h, w, EPS, dy, dsum=r)
+    want, wdw, wdb, x_off, dw_off, db_off = ref.layernorm_backward64(
+        ref.host(h), ref.host(w), EPS, ref.host(dy), ref.host(r))
+    off = np.abs(ref.host(dx) - want)
+    assert np.all(off <= x_off + (ref.HALF[dtype] + ref.U) * (np.abs(want) + x_off)), off.max()
+    assert np.all(np.abs(ref.host(dw) - wdw) <= dw_off) and np.all(np.abs(ref.host(db) - wdb) <= db_off)
+
+
+def test_layernorm_past_4_gib():
+    """More than 2^31 elements: the last rows are those of a call of their own."""
+    d, T = 2048, (1 << 20) + 4099
+    announce(f"layernorm T={T} d={d}")
+    g = _gen(91)
+    tail = _randn(g, 5000, d, dtype=BF16)
+    x = torch.zeros(T, d, dtype=BF16, device="cuda")
+    x[-5000:] = tail
+    w, b = 1 + 0.1 * _randn(g, d), _randn(g, d)
+    y = mh.mhlmoe_layernorm(x, w, EPS, bias=b)["y"]
+    assert torch.equal(y[-5000:], mh.mhlmoe_layernorm(tail, w, EPS, bias=b)["y"])
+    assert torch.equal(y[0].float(), b.to(BF16).float())
+    dx, dw, db = mh.mhlmoe_layernorm_backward(x, w, EPS, x)
+    tx, tw, tb = mh.mhlmoe_layernorm_backward(tail, w, EPS, tail)
+    assert torch.equal(dx[-5000:], tx) and not dx[:1000].any()
+    # the zero rows add nothing: the same 5000 terms per column in another order
+    n, _ = ref.norm_parts(ref.host(tail), EPS)
+    mag = np.abs(ref.host(tail) * n).sum(axis=0)
+    assert np.all(np.abs(ref.host(dw) - ref.host(tw)) <= 2 * 5002 * ref.U * mag)
+    assert np.all(np.abs(ref.host(db) - ref.host(tb)) <= 2 * 5002 * ref.U * np.abs(ref.host(tail)).sum(axis=0))
+
+
 def test_layernorm_empty():
     x = torch.empty(0, 64, dtype=BF16, device="cuda")
     w = torch.ones(64, device="cuda")
