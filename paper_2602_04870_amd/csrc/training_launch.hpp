@@ -145,13 +145,6 @@ inline bool balance_loss_at_once(int64_t T, int Nh, int Ne) {
 inline int balance_dw_blocks(int64_t T, int Nh, int dh, int Ne) {
   return Ne <= 32 ? 1 : Ne <= 64 ? 2 : Ne <= 128 || dh < 128 || balance_few(T, Nh, Ne) ? 4 : 8;
 }
-inline int64_t balance_splits(int64_t T, int Nh, int dh, int Ne) {
-  const int ew = balance_dw_blocks(T, Nh, dh, Ne);
-  const int64_t groups = Nh * ceil_div(balance_blocks(Ne), ew);
-  const int64_t want = ceil_div(ew == 8 ? 256 : 512, groups);
-  const int64_t most = ceil_div(T, 4 * 32 * (ew < 4 ? 4 / ew : 1));
-  return want < most ? want : most;
-}
 // Where not few tokens: dX and dW in one launch, whose workgroups then fill the card
 // together, unless dX loses too much by dW's registers and LDS.  us together / apart in
 // bf16 at 16 heads (fp32 alike):
@@ -161,6 +154,18 @@ inline int64_t balance_splits(int64_t T, int Nh, int dh, int Ne) {
 inline bool balance_together(int64_t T, int Nh, int dh, int Ne) {
   const int ew = balance_dw_blocks(T, Nh, dh, Ne);
   return ew <= 4 && (dh < 128 || Nh * ceil_div(T, kBalanceTokens) <= (ew == 1 ? 512 : 2048));
+}
+inline int64_t balance_splits(int64_t T, int Nh, int dh, int Ne) {
+  const int ew = balance_dw_blocks(T, Nh, dh, Ne);
+  const int64_t groups = Nh * ceil_div(balance_blocks(Ne), ew);
+  int64_t want = ceil_div(ew == 8 ? 256 : 512, groups);
+  // beside dX's workgroups: what the card then still holds at once (3001 x 16 heads x 200
+  // experts, d_h 64, fp32: 38 -> 35 us)
+  const int64_t dx = Nh * ceil_div(T, kBalanceTokens), free = 256 * (dh < 128 ? 3 : 2) - dx;
+  if (balance_together(T, Nh, dh, Ne) && !balance_few(T, Nh, Ne) && free >= groups)
+    want = free / groups;
+  const int64_t most = ceil_div(T, 4 * 32 * (ew < 4 ? 4 / ew : 1));
+  return want < most ? want : most;
 }
 hipError_t launch_balance_weights(const float* W, const int32_t* counts, int Nh, int dh, int Ne,
                                   void* out, hipStream_t s);
