@@ -992,12 +992,16 @@ class AdamWTensors:
     and v_scale [ceil(n / 128)] float32, where v is the root of v), all of one
     shape, and, with a bfloat16 param, master (float32) if there is one; and the
     numbers weight_decay (0 if left out) and seed (of the 8-bit states' rounding;
-    the tensor's place in the list if left out)."""
+    the tensor's place in the list if left out).  The memory that they have now is what
+    every step reads and writes, also after a tensor was given other memory (.data)
+    or let go: it is held here, and a new gradient tensor needs a new AdamWTensors."""
 
     _KEYS = {"param", "master", "grad", "m", "v", "m_scale", "v_scale", "weight_decay", "seed"}
 
     def __init__(self, tensors):
-        self.tensors = [dict(t) for t in tensors]  # (keeps their memory)
+        # aliases, which keep the memory
+        self.tensors = [{k: v.detach() if isinstance(v, torch.Tensor) else v for k, v in t.items()}
+                        for t in tensors]
         self.array = (_AdamWTensor * max(len(self.tensors), 1))()
         self.device = None
         f32 = torch.float32

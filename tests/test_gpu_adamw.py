@@ -223,3 +223,17 @@ def test_adamw_past_32_bits():
         root = np.sqrt(v1)
         ref.check_random_blocks(ref.host(part["v"]), ref.host(part["v_scale"]), root, 5 * ref.U * root, uv,
                                 True, f"v {at}")
+
+
+def test_adamw_tensors_keep_the_memory_they_were_given():
+    g = _gen(13)
+    t, _ = _tensor(g, 1000, "f32", F32, 32, 0)
+    c = {k: v.clone() if isinstance(v, torch.Tensor) else v for k, v in t.items()}
+    plan = mh.AdamWTensors([t])
+    was = t["param"].detach()
+    t["param"].data = torch.zeros(1000, device="cuda")
+    del t["grad"], t["m"], t["v"]
+    torch.full((8192,), 7.0, device="cuda")  # where freed memory of theirs would be taken again
+    mh.mhlmoe_adamw(plan, LR, step=3)
+    mh.mhlmoe_adamw([c], LR, step=3)
+    assert torch.equal(was, c["param"]) and not t["param"].any()
