@@ -58,7 +58,9 @@ CASES = [  # T, Nh, dh, Ne, k
     (2500, 1, 64, 8, 2),
     # enough tokens that the weights are laid out first: one, two, four and more blocks of experts
     (33100, 1, 64, 20, 2), (16601, 1, 128, 50, 2), (8200, 1, 128, 100, 3), (2900, 3, 64, 129, 3),
-    (4150, 2, 128, 300, 4), (66000, 1, 128, 10, 2), (8200, 1, 64, 600, 4)]
+    (4150, 2, 128, 300, 4), (66000, 1, 128, 10, 2), (8200, 1, 64, 600, 4),
+    # dX and dW in one pass over X: chunks of two to four tiles
+    (15001, 3, 128, 77, 3), (33100, 2, 128, 128, 4), (4997, 11, 128, 65, 2)]
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
