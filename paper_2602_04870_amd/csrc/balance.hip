@@ -12,7 +12,7 @@
 // The T x E scores stay on the chip: the loss takes one sweep over the experts with
 // a running maximum, sum and weighted sum, and keeps log sum exp and u_t of every
 // token; the gradient computes the scores again, once token by token for dX and
-// once expert by expert for dW (a fixed order, no atomics).
+// once expert by expert for dW, or once for both (a fixed order, no atomics).
 //
 // All products go to the fp16 matrix instructions at fp32 accuracy.  A value scaled
 // by a power of two is two fp16 ones, w = w0 + w1, each the nearest to what is left:
@@ -771,8 +771,8 @@ __global__ __launch_bounds__(256) void balance_loss_sum_kernel(
 // ---------------------------------------------------------------------------
 // dX: 32 tokens of a head per wavefront, over all experts, as in the loss.  A bf16 dX
 // takes ds and W as one fp16 value each (2^-10 of each term off at most; where terms are
-// alike that adds up to a sixth of what bf16's own rounding does), an fp32 one as two.  ds comes out of the
-// exponential as ds 2^(F + K - k_b), with the block's power k_b and the head's smallest
+// alike that adds up to a sixth of what bf16's own rounding does), an fp32 one as two.  ds
+// comes out of the exponential as ds 2^(F + K - k_b), with the block's power k_b and the head's smallest
 // K, so that all blocks' products add up alike; the rest of the factors come at the end.
 // ---------------------------------------------------------------------------
 template <int NP>
@@ -1114,7 +1114,8 @@ __device__ __forceinline__ void balance_dw(const DwArgs& a, unsigned block,
   // the lane's expert: f' and, scaled alike for all of the workgroup's experts, its weights
   WOperand<DH> w;
   const uint32_t top = w.load(W + (int64_t)h * Ne * DH, e, Ne, g);
-  const HeadCounts hc = head_counts<dw_waves(EW) * kWave>(counts + (int64_t)h * Ne, Ne, sm.totals, sm.tops);
+  const HeadCounts hc =
+      head_counts<dw_waves(EW) * kWave>(counts + (int64_t)h * Ne, Ne, sm.totals, sm.tops);
   const float f = live ? excess(counts[(int64_t)h * Ne + e], Ne, hc.total) : 0.0f;
   {
     uint32_t most = wave_max(top);

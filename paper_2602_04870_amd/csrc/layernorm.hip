@@ -14,8 +14,9 @@
 // the mean's own rounding leaves, r = mean (h - mu), is found in the same sums and
 // taken off:  mean (h - mu)^2 - r^2  and  n = (h - mu - r) rs.
 //
-// HBM bounds both: every element is read once, rows in registers as in norm.hip
-// (NormForm).  Widths that are no multiple of 8 take the form of the next one (ODD): their
+// HBM bounds both (16384 x 2048 in bf16 with a residual: 51 us, 5.3 TB/s; the gradient with
+// dsum 52 us, 5.1 TB/s, and 5 us of layernorm_dw_kernel): every element is read once, rows in
+// registers as in norm.hip (NormForm).  Widths that are no multiple of 8 take the form of the next one (ODD): their
 // rows begin anywhere, so pieces are loaded and stored at any address, the last one by
 // elements (column by column, as the RMS norm has them, 30000 x 100 in bf16 took 17 us
 // and its gradient 26).  Rows too wide for registers are walked three times by a
