@@ -184,6 +184,13 @@ __device__ __forceinline__ float log2_of(float power) {  // exactly
 __device__ __forceinline__ float uniform(float v) {
   return __uint_as_float((uint32_t)__builtin_amdgcn_readfirstlane((int)__float_as_uint(v)));
 }
+// What takes a block's scores (the products of x up and w up) to powers of two: log2 e
+// over both powers.  At least 2^-126: an expert that is not there has the score -infinity,
+// which times zero (a row of zeros, weights below 2^-9) would be NaN.  The scores are below
+// 2^37 in the products' unit, so none moves by more than 2^-89.
+__device__ __forceinline__ float score_scale(float x_down, float w_down) {
+  return fmaxf(x_down * w_down * kLog2e, 0x1p-126f);
+}
 __device__ __forceinline__ uint32_t bits_abs(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 __device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
 
@@ -614,7 +621,7 @@ __global__ __launch_bounds__(kTokenWaves* kWave) void balance_loss_kernel(
   x.convert(ok);
   Running run;
   for (int b = 0; b < nb; ++b) {
-    const float m = x.down * info[h].down[b] * kLog2e;
+    const float m = score_scale(x.down, info[h].down[b]);
     barrier_vm<0>();
     if (b + 1 < nb) fetch_block<DH>(rsrc, b + 1, w[(b + 1) & 1]);
     run.add(score_tile<DH, F32>(w[b & 1], at, x, 32 * b, Ne), m, fex + 32 * b, g);
@@ -670,7 +677,7 @@ __global__ __launch_bounds__(kFewThreads) void balance_loss_few_kernel(
   Running run;
   for (int b = eg; b * 32 < Ne; b += EG) {
     w.split(wave_max(top));
-    const float m = x.down * w.down * kLog2e;
+    const float m = score_scale(x.down, w.down);
     const f32x16 z = score_tile<DH, F32>(w, x, 32 * b, Ne);
     if ((b + EG) * 32 < Ne) top = w.load(Wh, 32 * (b + EG) + (lane & 31), Ne, g);
     run.add(z, m, fex + 32 * b, g);
@@ -955,7 +962,7 @@ __device__ __forceinline__ void balance_dx(const DxArgs& a, unsigned block, DxSh
   for (int i = 0; i < DH / 32; ++i) dx[i] = zero16();
   for (int b = 0; b < nb; ++b) {
     const float down_b = info[h].down[b];
-    const float m = x.down * down_b * kLog2e;
+    const float m = score_scale(x.down, down_b);
     const float ref = lse - (log2_of(down_b) - log2_of(down));
     barrier_vm<0>();
     if (b + 1 < nb) fetch_block<DH>(rsrc, b + 1, w[(b + 1) & 1]);
@@ -1323,7 +1330,7 @@ __device__ __forceinline__ void balance_dx_few(const DwArgs& a, const void* dX_a
       for (int s = 0; s < DH / 16; ++s)
         *reinterpret_cast<u32x4*>(ws + q * Tile<DH>::kBytes + (at.rows ^ (s * 32))) = w.w[q][s];
     wave_lds_order();
-    const float m = x.down * down_b * kLog2e;
+    const float m = score_scale(x.down, down_b);
     f32x16 z = score_tile<DH, F32>(w, x, 32 * b, Ne);
     if ((b + EG) * 32 < Ne) top = w.load(Wh, 32 * (b + EG) + (lane & 31), Ne, g);
     if (down_b > down) {
