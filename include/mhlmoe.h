@@ -718,8 +718,7 @@ mhlmoe_status mhlmoe_balance_loss(const void *X, const float *W_router,
  *   dW_router [n_heads][n_experts][d_head] float; not W_router        (out)
  * The other arguments are those of the mhlmoe_balance_loss call that wrote
  * stats.  dX_add (dW_add) is added in fp32 before the one rounding of dX.  Products
- * are of fp32 accuracy, but for a bf16 dX, whose terms are off by up to 2^-10 of
- * themselves each before they are added in fp32.
+ * are of fp32 accuracy.
  */
 mhlmoe_status mhlmoe_balance_loss_backward_workspace(int64_t T, int n_heads,
                                                      int d_head, int n_experts,

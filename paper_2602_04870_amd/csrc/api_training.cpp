@@ -79,7 +79,7 @@ BalanceLayout balance_layout(int64_t T, int n_heads, int d_head, int n_experts, 
   size_t cur = 0;
   L.weights = bump(cur, mhl::balance_weight_bytes(n_heads, d_head, n_experts));
   L.part = bump(cur, backward ? sizeof(float) *
-                                    (size_t)mhl::balance_most_splits(T, n_heads, d_head, n_experts) *
+                                    (size_t)mhl::balance_splits(T, n_heads, d_head, n_experts) *
                                     n_heads * mhl::balance_blocks(n_experts) * 32 * d_head
                               : sizeof(double) * (size_t)n_heads *
                                     mhl::balance_token_blocks(T, n_heads, n_experts));
@@ -327,11 +327,6 @@ mhlmoe_status mhlmoe_balance_loss_backward(
                                          n_heads, d_head, n_experts, f32, dX, dW_router, part,
                                          stream);
     }));
-  } else if (T > 0 && mhl::balance_both(T, n_heads, d_head, n_experts, f32)) {
-    MHL_TRY(run_kernel("balance_dx_dw", stream, [&] {
-      return mhl::launch_balance_bwd(X, W_router, counts, stats, dloss, mask, dX_add, dW_add, T,
-                                     n_heads, d_head, n_experts, dX, dW_router, part, stream);
-    }));
   } else if (T > 0) {
     MHL_TRY(run_kernel("balance_weights", stream, [&] {
       return mhl::launch_balance_weights(W_router, counts, n_heads, d_head, n_experts, weights,
@@ -354,10 +349,10 @@ mhlmoe_status mhlmoe_balance_loss_backward(
       }));
     }
   }
-  if (mhl::balance_splits(T, n_heads, d_head, n_experts, f32) == 1) return MHLMOE_OK;
+  if (mhl::balance_splits(T, n_heads, d_head, n_experts) == 1) return MHLMOE_OK;
   return run_kernel("balance_sum", stream, [&] {
     return mhl::launch_balance_dw_sum(part, stats, dloss, dW_add, T, n_heads, d_head, n_experts,
-                                      f32, dW_router, stream);
+                                      dW_router, stream);
   });
 }
 

@@ -12,7 +12,7 @@
 // The T x E scores stay on the chip: the loss takes one sweep over the experts with
 // a running maximum, sum and weighted sum, and keeps log sum exp and u_t of every
 // token; the gradient computes the scores again, once token by token for dX and
-// once expert by expert for dW, or once for both (a fixed order, no atomics).
+// once expert by expert for dW (a fixed order, no atomics).
 //
 // All products go to the fp16 matrix instructions at fp32 accuracy.  A value scaled
 // by a power of two is two fp16 ones, w = w0 + w1, each the nearest to what is left:
@@ -776,14 +776,12 @@ __global__ __launch_bounds__(256) void balance_loss_sum_kernel(
 }
 
 // ---------------------------------------------------------------------------
-// dX: 32 tokens of a head per wavefront, over all experts, as in the loss.  A bf16 dX
-// takes ds and W as one fp16 value each (2^-10 of each term off at most; where terms are
-// alike that adds up to a sixth of what bf16's own rounding does), an fp32 one as two.  ds
+// dX: 32 tokens of a head per wavefront, over all experts, as in the loss; ds and W as two
+// fp16 values each, whatever X's type: dX is rounded once, when dX_add is added.  ds
 // comes out of the exponential as ds 2^(F + K - k_b), with the block's power k_b and the head's smallest
 // K, so that all blocks' products add up alike; the rest of the factors come at the end.
 // ---------------------------------------------------------------------------
-template <int NP>
-__device__ __forceinline__ void split_ds(const f32x16& ds, int s, u32x4 (&out)[NP]) {
+__device__ __forceinline__ void split_ds(const f32x16& ds, int s, u32x4 (&out)[2]) {
   float f[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) f[j] = ds[8 * s + j];
@@ -791,20 +789,20 @@ __device__ __forceinline__ void split_ds(const f32x16& ds, int s, u32x4 (&out)[N
 }
 
 // dX^T += W^T ds of 32 experts x 32 tokens.
-template <int DH, int NP>
+template <int DH>
 __device__ __forceinline__ void add_dx(const f32x16& z, const uint8_t* w, const Tile<DH>& at,
                                        f32x16 (&dx)[DH / 32]) {
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
-    u32x4 ds[NP];
+    u32x4 ds[2];
     split_ds(z, s, ds);
 #pragma unroll
     for (int dt = 0; dt < DH / 32; ++dt)
 #pragma unroll
-      for (int q = NP - 1; q >= 0; --q) {
+      for (int q = 1; q >= 0; --q) {
         const u32x4 a = at.col_operand(w + q * Tile<DH>::kBytes, dt, s);
 #pragma unroll
-        for (int p = NP - 1 - q; p >= 0; --p) dx[dt] = mfma32_f16(a, ds[p], dx[dt]);
+        for (int p = 1 - q; p >= 0; --p) dx[dt] = mfma32_f16(a, ds[p], dx[dt]);
       }
   }
 }
@@ -932,7 +930,6 @@ struct DxShared {
 
 template <int DH, bool F32>
 __device__ __forceinline__ void balance_dx(const DxArgs& a, unsigned block, DxShared<DH>& sm) {
-  constexpr int NP = F32 ? 2 : 1;
   constexpr uint32_t kBlock = 2 * Tile<DH>::kBytes;
   const float2* __restrict__ stats = a.stats;
   const HeadInfo* __restrict__ info = a.info;
@@ -975,7 +972,7 @@ __device__ __forceinline__ void balance_dx(const DxArgs& a, unsigned block, DxSh
       for (int i = 0; i < 4; ++i)
         z[4 * q + i] = __builtin_amdgcn_exp2f(fmaf(z[4 * q + i], m, -ref)) * (f[i] - u);
     }
-    add_dx<DH, NP>(z, wb, at, dx);
+    add_dx<DH>(z, wb, at, dx);
   }
   __syncthreads();  // the weights' LDS is the rows' now
   store_dx_rows<DH, F32>(dx, ok, c, t - (lane & 31), T, Nh, h, &w[0][0] + wave * Tile<DH>::kBytes,
@@ -1276,10 +1273,9 @@ __global__ __launch_bounds__(kDwWaves* kWave) void balance_dw_dx_kernel(const Dw
 // a Tile of the wavefront's own to be read transposed.  The products add up in the unit
 // of the largest weights so far (down), to which both are lowered when larger ones come.
 // ---------------------------------------------------------------------------
-template <int DH, bool F32, int EG>
+template <int DH, int EG>
 struct DxFewShared {
-  static constexpr int NP = F32 ? 2 : 1;
-  static constexpr int kTiles = kDwWaves * NP * Tile<DH>::kBytes;
+  static constexpr int kTiles = kDwWaves * 2 * Tile<DH>::kBytes;
   static constexpr int kSums = (kDwWaves - kDwWaves / EG) * 32 * DH * 4;
   __align__(16) uint8_t ws[kTiles > kSums ? kTiles : kSums];
   __align__(16) float fex[kMaxExperts];
@@ -1290,8 +1286,8 @@ struct DxFewShared {
 template <int DH, bool F32, int EG>
 __device__ __forceinline__ void balance_dx_few(const DwArgs& a, const void* dX_add, void* dX,
                                                unsigned block,
-                                               DxFewShared<DH, F32, EG>& sm) {
-  constexpr int NP = F32 ? 2 : 1, TG = kDwWaves / EG;
+                                               DxFewShared<DH, EG>& sm) {
+  constexpr int TG = kDwWaves / EG;
   const int64_t T = a.T;
   const int Nh = a.Nh, Ne = a.Ne;
   const int h = block % Nh, lane = lane_id(), g = lane >> 5, wave = threadIdx.x >> 6;
@@ -1317,7 +1313,7 @@ __device__ __forceinline__ void balance_dx_few(const DwArgs& a, const void* dX_a
 #pragma unroll
   for (int i = 0; i < DH / 32; ++i) dx[i] = zero16();
   const Tile<DH> at;
-  uint8_t* const ws = sm.ws + wave * NP * Tile<DH>::kBytes;
+  uint8_t* const ws = sm.ws + wave * 2 * Tile<DH>::kBytes;
   float down = 0x1p-126f;
   __syncthreads();
   for (int b = eg; b * 32 < Ne; b += EG) {
@@ -1325,7 +1321,7 @@ __device__ __forceinline__ void balance_dx_few(const DwArgs& a, const void* dX_a
     const float down_b = uniform(w.down);
     wave_lds_order();  // the readers of the block before
 #pragma unroll
-    for (int q = 0; q < NP; ++q)
+    for (int q = 0; q < 2; ++q)
 #pragma unroll
       for (int s = 0; s < DH / 16; ++s)
         *reinterpret_cast<u32x4*>(ws + q * Tile<DH>::kBytes + (at.rows ^ (s * 32))) = w.w[q][s];
@@ -1349,7 +1345,7 @@ __device__ __forceinline__ void balance_dx_few(const DwArgs& a, const void* dX_a
       for (int i = 0; i < 4; ++i)
         z[4 * q + i] = __builtin_amdgcn_exp2f(fmaf(z[4 * q + i], m, -ref)) * (f[i] - st.y);
     }
-    add_dx<DH, NP>(z, ws, at, dx);
+    add_dx<DH>(z, ws, at, dx);
   }
   const float c = a.dloss[h] * a.stats[T * Nh + h].x * __builtin_amdgcn_ldexpf(down, -(int)F);
 #pragma unroll
@@ -1386,7 +1382,7 @@ template <int DH, bool F32, int EG>
 __global__ __launch_bounds__(kDwWaves* kWave) void balance_bwd_few_kernel(
     const DwArgs a, const void* dX_add, void* dX, unsigned dx_blocks) {
   __shared__ union Shared {
-    DxFewShared<DH, F32, EG> dx;
+    DxFewShared<DH, EG> dx;
     DwShared<DH, F32, EG> dw;
     __device__ Shared() {}
   } sm;
@@ -1394,272 +1390,6 @@ __global__ __launch_bounds__(kDwWaves* kWave) void balance_bwd_few_kernel(
     balance_dx_few<DH, F32, EG>(a, dX_add, dX, blockIdx.x, sm.dx);
   else
     balance_dw<DH, F32, EG>(a, blockIdx.x - dx_blocks, sm.dw);
-}
-
-// ---------------------------------------------------------------------------
-// The gradient of a bf16 X in one pass, 65 to 128 experts at d_h 128: a workgroup has all
-// of a head's experts, 32 to each of four wavefronts, over a chunk of the tokens, 32 at a
-// time.  A wavefront's ds go to its dW from registers as above, and to LDS, [expert][token],
-// from where every wavefront takes all of them for 32 of dX's columns (one product of
-// fp16 values, as above).  A tile's dX is made beside the next one's scores, so that a
-// tile has one barrier.  Five passes of products instead of seven, and X read once (us
-// against dX and dW by themselves: 92 / 122 at 16384 tokens x 16 heads x 128 experts, 290 /
-// 389 at 65536, 41 / 55 at 6000 x 100).  W for dX lies in LDS: in registers, of which two
-// wavefronts share a SIMD's, it spilled (152 us), as rows on their way must not: what
-// spills waits for its load.  With an fp32 X, whose pieces take one wavefront to a SIMD, it
-// gained nothing (625 / 625 at 65536 x 128), nor with two wavefronts for 64 experts
-// (101 / 91 at 16384).
-// ---------------------------------------------------------------------------
-struct BothShared {
-  __align__(16) uint8_t xs[2][Tile<128>::kBytes];
-  __align__(16) uint8_t ds[2][kDwWaves * 32 * 64];
-  __align__(16) u32x4 wt[kDwWaves][2 * kDwWaves][kWave];  // W as a wavefront's operands
-  __align__(16) uint8_t rows[kDwWaves][32 * 64];          // of dX, on their way out
-  __align__(16) float ms[2][32], refs[2][32], us[2][32], downs[2][32];
-  int counted[2][32];
-  long long totals[kDwWaves];
-  uint32_t tops[kDwWaves][2];
-};
-
-__global__ __launch_bounds__(kDwWaves* kWave, 2) void balance_bwd_kernel(const DwArgs a,
-                                                                         const void* dX_add,
-                                                                         void* dX) {
-  constexpr int DH = 128, kThreads = kDwWaves * kWave;
-  static_assert(kThreads == 32 * 8, "eight threads to a row of X");
-  using Row = XOperand<DH, false>;
-  __shared__ BothShared sm;
-  const uint16_t* __restrict__ X = static_cast<const uint16_t*>(a.X);
-  const float2* __restrict__ stats = a.stats;
-  const uint8_t* __restrict__ mask = a.mask;
-  const int64_t T = a.T;
-  const int Nh = a.Nh, Ne = a.Ne;
-  const int lane = lane_id(), g = lane >> 5, wave = threadIdx.x >> 6;
-  const int h = blockIdx.x % Nh, split = blockIdx.x / Nh;
-  const int e = 32 * wave + (lane & 31);
-  const bool live = e < Ne;
-  const int64_t tiles = (T + 31) / 32;
-  const int64_t begin = tiles * split / a.splits, end = tiles * (split + 1) / a.splits;
-
-  // 16 values of a row, its stats and mask on their way
-  const int r_x = threadIdx.x / 8, unit_x = 2 * (threadIdx.x % 8);
-  u32x4 raw[2][1];
-  float2 st;
-  uint8_t counted;
-  auto fetch = [&](int64_t tile) {
-    int64_t t = tile * 32 + r_x;
-    t = t < T ? t : T - 1;
-    const u32x4* p = reinterpret_cast<const u32x4*>(X + (t * Nh + h) * DH) + unit_x;
-    raw[0][0] = p[0];
-    raw[1][0] = p[1];
-    st = stats[t * Nh + h];
-    counted = mask ? mask[t] : 1;
-  };
-  if (begin < end) fetch(begin);
-
-  // the weights: the lane's expert, and this wavefront's columns of all of them
-  const float* __restrict__ Wh = a.W + (int64_t)h * Ne * DH;
-  const int32_t* __restrict__ counts = a.counts + (int64_t)h * Ne;
-  WOperand<DH> w;
-  const uint32_t top_w = w.load(Wh, e, Ne, g);
-  const HeadCounts hc = head_counts<kThreads>(counts, Ne, sm.totals, sm.tops);
-  const float f = live ? excess(counts[e], Ne, hc.total) : 0.0f;
-  const float F = uniform(ds_exponent(hc.most, hc.least, Ne, hc.total));
-  {
-    uint32_t most = wave_max(top_w);
-    __syncthreads();  // the readers of tops
-    if (lane == 0) sm.tops[wave][0] = most;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kDwWaves; ++i) most = umax(most, sm.tops[i][0]);
-    w.split(most);
-  }
-  const float down = uniform(w.down);
-  const Tile<DH> at;
-  {
-    // through Tiles in its own place
-    uint8_t* const tiles_w = reinterpret_cast<uint8_t*>(sm.wt);
-    u32x4 o[2 * kDwWaves];
-#pragma unroll
-    for (int s = 0; s < DH / 16; ++s)
-      *reinterpret_cast<u32x4*>(tiles_w + wave * Tile<DH>::kBytes + (at.rows ^ (s * 32))) = w.w[0][s];
-    __syncthreads();
-#pragma unroll
-    for (int s = 0; s < 2 * kDwWaves; ++s)
-      o[s] = at.col_operand(tiles_w + (s >> 1) * Tile<DH>::kBytes, wave, s & 1);
-    __syncthreads();
-#pragma unroll
-    for (int s = 0; s < 2 * kDwWaves; ++s) sm.wt[wave][s][lane] = o[s];
-  }
-  const float c = a.dloss[h] * stats[T * Nh + h].x;
-  const float c_dx = c * __builtin_amdgcn_ldexpf(down, -(int)F);
-
-  f32x16 dw[DH / 32];
-#pragma unroll
-  for (int i = 0; i < DH / 32; ++i) dw[i] = zero16();
-  float S = kDwFirst * __builtin_amdgcn_exp2f(-F);  // of ds 2^F
-  auto store = [&](int64_t tile, int buf) {
-    const bool ok = tile * 32 + r_x < T && counted;
-    if (__any(!ok)) {
-      if (!ok) raw[0][0] = raw[1][0] = u32x4{0, 0, 0, 0};
-    }
-    const Pow2 scale =
-        pow2_below_2_15(row_max<8>(Row::widen(Row::top_of(raw[1], Row::top_of(raw[0], 0u)))));
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      float v[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = Row::value(raw[i], k);
-      u32x4 o[1];
-      split8(v, scale.up, o);
-      *reinterpret_cast<u32x4*>(sm.xs[buf] + Tile<DH>::unit(r_x, unit_x + i)) = o[0];
-    }
-    if (unit_x == 0) {
-      // a token that does not count: p = exp2(-infinity) = 0
-      sm.ms[buf][r_x] = scale.down * down * kLog2e;
-      sm.refs[buf][r_x] = ok ? fmaf(st.x, kLog2e, -F) : INFINITY;
-      sm.us[buf][r_x] = ok ? st.y : 0.0f;
-      sm.downs[buf][r_x] = scale.down;
-      sm.counted[buf][r_x] = ok;
-    }
-  };
-
-  // dX's rows of a tile, this wavefront's 32 columns, 64 bytes: four lanes to a row
-  u32x4 add[2];
-  auto token = [&](int64_t tile, int i) { return tile * 32 + 16 * i + (lane >> 2); };
-  auto place = [&](int64_t t) { return ((t * Nh + h) * DH + 32 * wave) * 2 + 16 * (lane & 3); };
-  auto fetch_add = [&](int64_t tile) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int64_t t = token(tile, i);
-      add[i] = t < T ? *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(dX_add) + place(t))
-                     : u32x4{0, 0, 0, 0};
-    }
-  };
-  uint8_t* const rows = sm.rows[wave];
-  auto row_unit = [](int row, int j) { return row * 64 + ((j ^ ((row >> 2) & 3)) * 16); };
-  // ds as 8-byte pieces of four tokens, piece j of an expert's row at j ^ (row / 4) % 8:
-  // a lane's expert's pieces g + 2 k + 4 s, and the operand with the token as its column
-  const int ds_write = wave * 2048 + (lane & 31) * 64 + ((g ^ ((lane & 31) >> 2)) * 8);
-  int ds_read[2];
-#pragma unroll
-  for (int k = 0; k < 2; ++k)
-    ds_read[k] = (4 * g + 8 * k + ((lane & 15) >> 2)) * 64 +
-                 (((4 * ((lane >> 4) & 1) + (lane & 3)) ^ (g + 2 * k)) * 8);
-  auto make_dx = [&](int64_t tile, int buf, bool ok) {
-    f32x16 dx = zero16();
-#pragma unroll
-    for (int s = 0; s < 2 * kDwWaves; ++s) {
-      const uint8_t* p = sm.ds[buf] + 16 * 64 * s;
-      const u32x2 lo = lds_read_tr16(p + (ds_read[0] ^ (32 * (s & 1))));
-      const u32x2 hi = lds_read_tr16(p + (ds_read[1] ^ (32 * (s & 1))));
-      dx = mfma32_f16(sm.wt[wave][s][lane], u32x4{lo[0], lo[1], hi[0], hi[1]}, dx);
-    }
-    if (dX_add) {
-      wave_lds_order();  // the readers of what was there
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-        *reinterpret_cast<u32x4*>(rows + row_unit(16 * i + (lane >> 2), lane & 3)) = add[i];
-    }
-    wave_lds_order();
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      u32x2* p = reinterpret_cast<u32x2*>(rows + row_unit(lane & 31, q) + 8 * g);
-      float v[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] = ok ? dx[4 * q + k] * c_dx : 0.0f;
-      if (dX_add) {
-        const u32x2 b = *p;
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          v[k] += bf16_bits_to_f32((b[k >> 1] >> (16 * (k & 1))) & 0xFFFFu);
-      }
-      *p = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-    }
-    wave_lds_order();
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int64_t t = token(tile, i);
-      if (t < T)
-        *reinterpret_cast<u32x4*>(static_cast<uint8_t*>(dX) + place(t)) =
-            *reinterpret_cast<const u32x4*>(rows + row_unit(16 * i + (lane >> 2), lane & 3));
-    }
-  };
-
-  if (begin < end) store(begin, 0);
-  bool ok = false;
-  for (int64_t tile = begin; tile < end; ++tile) {
-    const int buf = (int)(tile - begin) & 1;
-    __syncthreads();
-    if (tile > begin) make_dx(tile - 1, buf ^ 1, ok);
-    __builtin_amdgcn_sched_barrier(0);
-    if (dX_add) fetch_add(tile);
-    ok = sm.counted[buf][lane & 31];
-    if (tile + 1 < end) fetch(tile + 1);
-    const uint8_t* xb = sm.xs[buf];
-    // scores of 32 tokens (rows) x 32 experts (lanes)
-    f32x16 z = zero16();
-#pragma unroll
-    for (int s = 0; s < DH / 16; ++s) {
-      const u32x4 x = at.row_operand(xb, s);
-      z = mfma32_f16(x, w.w[1][s], z);
-      z = mfma32_f16(x, w.w[0][s], z);
-    }
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int r = 8 * q + 4 * g;
-      const f32x4 m4 = *reinterpret_cast<const f32x4*>(&sm.ms[buf][r]);
-      const f32x4 r4 = *reinterpret_cast<const f32x4*>(&sm.refs[buf][r]);
-      const f32x4 u4 = *reinterpret_cast<const f32x4*>(&sm.us[buf][r]);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        z[4 * q + i] = __builtin_amdgcn_exp2f(fmaf(z[4 * q + i], m4[i], -r4[i])) * (f - u4[i]);
-    }
-    if (32 * wave + 32 > Ne) {
-      asm volatile("");  // a branch, not 16 instructions for every block
-#pragma unroll
-      for (int v = 0; v < 16; ++v) z[v] = live ? z[v] : 0.0f;
-    }
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      u32x4 d[1];
-      split_ds(z, s, d);
-#pragma unroll
-      for (int k = 0; k < 2; ++k)
-        *reinterpret_cast<u32x2*>(sm.ds[buf] + (ds_write ^ (32 * s + 16 * k))) =
-            u32x2{d[0][2 * k], d[0][2 * k + 1]};
-    }
-    float top = 0.0f;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const f32x4 d4 = *reinterpret_cast<const f32x4*>(&sm.downs[buf][8 * q + 4 * g]);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        z[4 * q + i] *= d4[i] * S;
-        top = fmaxf(top, fabsf(z[4 * q + i]));
-      }
-    }
-    lower_to_fit(top, z, dw, S);
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      u32x4 ds[2];
-      split_ds(z, s, ds);
-#pragma unroll
-      for (int dt = 0; dt < DH / 32; ++dt) {
-        const u32x4 x = at.col_operand(xb, dt, s);
-        dw[dt] = mfma32_f16(x, ds[1], dw[dt]);
-        dw[dt] = mfma32_f16(x, ds[0], dw[dt]);
-      }
-    }
-    if (tile + 1 < end) store(tile + 1, buf ^ 1);
-  }
-  __syncthreads();
-  if (begin < end) make_dx(end - 1, (int)(end - 1 - begin) & 1, ok);
-  const float k = __builtin_amdgcn_exp2f(-F) / S;
-#pragma unroll
-  for (int dt = 0; dt < DH / 32; ++dt)
-#pragma unroll
-    for (int v = 0; v < 16; ++v) dw[dt][v] *= k;
-  store_dw<DH>(a, dw, h, split, (Ne + 31) / 32, e, c);
 }
 
 // dW = dW_add + dloss / n times the sum of n partial results, in order.
@@ -1786,10 +1516,10 @@ hipError_t launch_balance_loss_sum(const double* part, const int32_t* counts, co
 
 static DwArgs dw_args(const void* X, const float* W, const int32_t* counts, const float* stats,
                       const float* dloss, const uint8_t* mask, const float* dW_add, int64_t T,
-                      int Nh, int dh, int Ne, bool f32, float* dW, float* part) {
+                      int Nh, int dh, int Ne, float* dW, float* part) {
   return DwArgs{X, W, counts, reinterpret_cast<const float2*>(stats), dloss, mask, dW_add, T, Nh,
                 Ne, (int)ceil_div(balance_blocks(Ne), balance_dw_blocks(T, Nh, dh, Ne)),
-                (int)balance_splits(T, Nh, dh, Ne, f32), dW, part};
+                (int)balance_splits(T, Nh, dh, Ne), dW, part};
 }
 static unsigned dw_workgroups(const DwArgs& a) {
   return (unsigned)(ceil_div((int64_t)a.Nh * a.splits, kXcds) * kXcds * a.groups);
@@ -1838,7 +1568,7 @@ hipError_t launch_balance_dw(const void* X, const float* W, const int32_t* count
                              const float* stats, const float* dloss, const uint8_t* mask,
                              const float* dW_add, int64_t T, int Nh, int dh, int Ne, bool f32,
                              float* dW, float* part, hipStream_t s) {
-  const DwArgs a = dw_args(X, W, counts, stats, dloss, mask, dW_add, T, Nh, dh, Ne, f32, dW, part);
+  const DwArgs a = dw_args(X, W, counts, stats, dloss, mask, dW_add, T, Nh, dh, Ne, dW, part);
   for_dw(dh, f32, balance_dw_blocks(T, Nh, dh, Ne), [&](auto DH, auto F32, auto EW) {
     hipLaunchKernelGGL((balance_dw_kernel<decltype(DH)::value, decltype(F32)::value,
                                           decltype(EW)::value>),
@@ -1852,7 +1582,7 @@ hipError_t launch_balance_dw_dx(const void* X, const float* W, const void* weigh
                                 const uint8_t* mask, const void* dX_add, const float* dW_add,
                                 int64_t T, int Nh, int dh, int Ne, bool f32, void* dX, float* dW,
                                 float* part, hipStream_t s) {
-  const DwArgs dw = dw_args(X, W, counts, stats, dloss, mask, dW_add, T, Nh, dh, Ne, f32, dW, part);
+  const DwArgs dw = dw_args(X, W, counts, stats, dloss, mask, dW_add, T, Nh, dh, Ne, dW, part);
   const DxArgs dx{X, static_cast<const uint8_t*>(weights), head_info(weights, Nh, dh, Ne),
                   reinterpret_cast<const float2*>(stats), dloss, mask, dX_add, T, Nh, Ne, dX};
   const unsigned dw_blocks = dw_workgroups(dw);
@@ -1866,22 +1596,12 @@ hipError_t launch_balance_dw_dx(const void* X, const float* W, const void* weigh
   return hipGetLastError();
 }
 
-hipError_t launch_balance_bwd(const void* X, const float* W, const int32_t* counts,
-                              const float* stats, const float* dloss, const uint8_t* mask,
-                              const void* dX_add, const float* dW_add, int64_t T, int Nh, int dh,
-                              int Ne, void* dX, float* dW, float* part, hipStream_t s) {
-  const DwArgs a = dw_args(X, W, counts, stats, dloss, mask, dW_add, T, Nh, dh, Ne, false, dW, part);
-  hipLaunchKernelGGL(balance_bwd_kernel, dim3((unsigned)(Nh * a.splits)), dim3(kDwWaves * kWave), 0,
-                     s, a, dX_add, dX);
-  return hipGetLastError();
-}
-
 hipError_t launch_balance_bwd_few(const void* X, const float* W, const int32_t* counts,
                                   const float* stats, const float* dloss, const uint8_t* mask,
                                   const void* dX_add, const float* dW_add, int64_t T, int Nh,
                                   int dh, int Ne, bool f32, void* dX, float* dW, float* part,
                                   hipStream_t s) {
-  const DwArgs a = dw_args(X, W, counts, stats, dloss, mask, dW_add, T, Nh, dh, Ne, f32, dW, part);
+  const DwArgs a = dw_args(X, W, counts, stats, dloss, mask, dW_add, T, Nh, dh, Ne, dW, part);
   for_dw(dh, f32, balance_dw_blocks(T, Nh, dh, Ne), [&](auto DH, auto F32, auto EW) {
     constexpr int EG = decltype(EW)::value;
     if constexpr (EG <= kDwWaves) {
@@ -1895,12 +1615,12 @@ hipError_t launch_balance_bwd_few(const void* X, const float* W, const int32_t* 
 }
 
 hipError_t launch_balance_dw_sum(const float* part, const float* stats, const float* dloss,
-                                 const float* dW_add, int64_t T, int Nh, int dh, int Ne, bool f32,
-                                 float* dW, hipStream_t s) {
+                                 const float* dW_add, int64_t T, int Nh, int dh, int Ne, float* dW,
+                                 hipStream_t s) {
   const int padded = 32 * balance_blocks(Ne), dh4 = dh / 4;
   const dim3 grid((unsigned)ceil_div(Ne * dh4, 256), (unsigned)Nh);
   hipLaunchKernelGGL(balance_dw_sum_kernel, grid, dim3(256), 0, s,
-                     reinterpret_cast<const f32x4*>(part), balance_splits(T, Nh, dh, Ne, f32),
+                     reinterpret_cast<const f32x4*>(part), balance_splits(T, Nh, dh, Ne),
                      (int64_t)Nh * padded * dh4, reinterpret_cast<const float2*>(stats) + T * Nh,
                      dloss, reinterpret_cast<const f32x4*>(dW_add), Ne, padded, dh4,
                      reinterpret_cast<f32x4*>(dW));

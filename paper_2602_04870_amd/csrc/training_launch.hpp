@@ -147,7 +147,7 @@ inline int balance_dw_blocks(int64_t T, int Nh, int dh, int Ne) {
 }
 // Where not few tokens: dX and dW in one launch, whose workgroups then fill the card
 // together, unless dX loses too much by dW's registers and LDS.  us together / apart in
-// bf16 at 16 heads (fp32 alike; balance_both not taken):
+// bf16 at 16 heads (fp32 alike):
 //   d_h   64: 33 / 39 at 3001 tokens x 200 experts, 84 / 93 at 32768 x 64
 //   d_h  128: 26 / 36 at 2000 x 100, 114 / 120 at 16384 x 128, 388 / 385 at 65536 x 128;
 //             30 / 38 at 2500 x 20, 48 / 45 at 6000 x 16, 112 / 95 at 16384 x 16
@@ -166,27 +166,6 @@ inline int64_t balance_splits(int64_t T, int Nh, int dh, int Ne) {
     want = free / groups;
   const int64_t most = ceil_div(T, 4 * 32 * (ew < 4 ? 4 / ew : 1));
   return want < most ? want : most;
-}
-// dX and dW in one pass over a bf16 X (balance_bwd_kernel) where its workgroups, of four
-// tiles of 32 tokens at least, fill the card, and the chunks that it cuts the tokens into (us
-// so / by the forms above: 35 / 38 at 3000 tokens x 16 heads x 128 experts, 92 / 122 at
-// 16384; 28 / 27 at 2100 x 16 x 66, 37 / 34 at 20000 x 2 x 80).  The partial results' room
-// is either form's: its size has no type.
-inline bool balance_both(int64_t T, int Nh, int dh, int Ne, bool f32) {
-  return !f32 && dh == 128 && Ne > 64 && Ne <= 128 && !balance_few(T, Nh, Ne) &&
-         Nh * ceil_div(T, 4 * 32) > 320;
-}
-inline int64_t balance_both_splits(int64_t T, int Nh) {
-  const int64_t want = ceil_div(512, Nh), most = ceil_div(T, 4 * 32);
-  return want < most ? want : most;
-}
-inline int64_t balance_splits(int64_t T, int Nh, int dh, int Ne, bool f32) {
-  return balance_both(T, Nh, dh, Ne, f32) ? balance_both_splits(T, Nh)
-                                          : balance_splits(T, Nh, dh, Ne);
-}
-inline int64_t balance_most_splits(int64_t T, int Nh, int dh, int Ne) {
-  const int64_t a = balance_splits(T, Nh, dh, Ne, false), b = balance_splits(T, Nh, dh, Ne, true);
-  return a > b ? a : b;
 }
 hipError_t launch_balance_weights(const float* W, const int32_t* counts, int Nh, int dh, int Ne,
                                   void* out, hipStream_t s);
@@ -210,11 +189,6 @@ hipError_t launch_balance_dw_dx(const void* X, const float* W, const void* weigh
                                 const uint8_t* mask, const void* dX_add, const float* dW_add,
                                 int64_t T, int Nh, int dh, int Ne, bool f32, void* dX, float* dW,
                                 float* part, hipStream_t s);
-// dX and dW where balance_both.
-hipError_t launch_balance_bwd(const void* X, const float* W, const int32_t* counts,
-                              const float* stats, const float* dloss, const uint8_t* mask,
-                              const void* dX_add, const float* dW_add, int64_t T, int Nh, int dh,
-                              int Ne, void* dX, float* dW, float* part, hipStream_t s);
 // dX and dW where balance_few.
 hipError_t launch_balance_bwd_few(const void* X, const float* W, const int32_t* counts,
                                   const float* stats, const float* dloss, const uint8_t* mask,
@@ -222,7 +196,7 @@ hipError_t launch_balance_bwd_few(const void* X, const float* W, const int32_t* 
                                   int dh, int Ne, bool f32, void* dX, float* dW, float* part,
                                   hipStream_t s);
 hipError_t launch_balance_dw_sum(const float* part, const float* stats, const float* dloss,
-                                 const float* dW_add, int64_t T, int Nh, int dh, int Ne, bool f32,
-                                 float* dW, hipStream_t s);
+                                 const float* dW_add, int64_t T, int Nh, int dh, int Ne, float* dW,
+                                 hipStream_t s);
 
 }  // namespace mhl

@@ -16,7 +16,7 @@ BF16, F32 = torch.bfloat16, torch.float32
 
 # T, Nh, dh, Ne: no number of experts is a multiple of 32
 FEW = [(40, 1, 64, 1), (70, 2, 64, 6), (70, 2, 128, 33), (130, 3, 64, 100)]
-# dX and dW together, dX by itself, one pass over a bf16 X
+# the weights laid out first; dX and dW in one launch, or each by itself (66000 x 10, 300)
 MANY = [(33100, 1, 64, 20), (16601, 1, 128, 50), (66000, 1, 128, 10), (4150, 2, 128, 300),
         (15001, 3, 128, 77)]
 
@@ -53,3 +53,45 @@ def test_balance_zero_and_tiny(T, Nh, dh, Ne, dtype, rows, weights):
     W = W * weights
     counts = mh.mhlmoe_expert_counts(idx, Ne, mask=m)
     _check(X, W, counts, m, 1 + 0.2 * torch.rand((Nh,), generator=g, device="cuda"))
+
+
+def _one_value(v):
+    """v [n, ...] as single fp16 values of a power of two that all of them share."""
+    k = 13 - np.floor(np.log2(np.abs(v).max()))
+    return np.float16(v * 2.0 ** k).astype(np.float64) * 2.0 ** -k
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("T,Nh,dh,Ne", [(70, 2, 64, 6), (70, 2, 128, 33), (130, 3, 64, 100), (33100, 1, 64, 20),
+                                        (16601, 1, 128, 50), (66000, 1, 128, 10), (15001, 3, 128, 77)])
+def test_balance_dx_terms(T, Nh, dh, Ne, dtype):
+    """dX is rounded once: where dX_add takes nearly all of it away, what is left shows its
+    terms.  Rows of zeros have exact scores, so little else is off; terms of one fp16 value
+    each, 2^-11 off, would be seen."""
+    announce(f"balance dX T={T} Nh={Nh} dh={dh} Ne={Ne} {dtype}")
+    g, X, W, _, _ = _problem(T, Nh, dh, Ne, 1, dtype, None, T + Ne)
+    X.zero_()
+    # an even load but for up to eight experts, whose terms are then most of dX
+    counts = torch.full((Nh, Ne), 500, device="cuda", dtype=torch.int32)
+    n = min(4, Ne // 2)
+    at = torch.randperm(Ne, generator=g, device="cuda")[:2 * n]
+    more = torch.randint(100, 500, (Nh, n), generator=g, device="cuda", dtype=torch.int32)
+    counts[:, at[:n]] += more
+    counts[:, at[n:]] -= more
+    dloss = 1 + 0.2 * torch.rand((Nh,), generator=g, device="cuda")
+    _, stats = mh.mhlmoe_balance_loss(X, W, counts)
+    # a token is like all others: three of them, of which the reference has n = 3
+    c64, dl = counts.cpu().numpy().astype(np.int64), ref.host(dloss) * 3 / T
+    b = ref.Balance(ref.host(X[:3]), ref.host(W), c64, None)
+    v, _, _, _ = b.backward(dl, None, None, False)
+    add = torch.from_numpy(-v).to(dtype)
+    w, _, off, _ = b.backward(dl, ref.host(add), None, False)
+    ds = (b.p * (b.f - b.u[..., None]))[0] * (dl / 3)[:, None]
+    one = np.einsum("he,hed->hd", np.stack([_one_value(d) for d in ds]),
+                    np.stack([_one_value(h) for h in ref.host(W)]))
+    half = ref.HALF[dtype]
+    assert np.any(np.abs(one - v[0]) > 2 * off[0] + half * (np.abs(w[0]) + off[0]))
+    dX, _ = mh.mhlmoe_balance_loss_backward(X, W, counts, stats, dloss,
+                                            dX_add=add[:1].cuda().expand(T, Nh, dh).contiguous())
+    err = np.abs(ref.host(dX) - w[0])
+    assert np.all(err <= off[0] + half * (np.abs(w[0]) + off[0])), (err / off[0]).max()
