@@ -17,7 +17,8 @@
 // All products go to the fp16 matrix instructions at fp32 accuracy.  A value scaled
 // by a power of two is two fp16 ones, w = w0 + w1, each the nearest to what is left:
 // off by 2^-23 of itself, or by 2^-39 of the largest of those that share the scale
-// (a token's row of X, 32 experts' rows of W, an expert's ds so far).  A bf16 x is one
+// (a token's row of X; 32 experts' rows of W, for dW all of a workgroup's, up to 256; the
+// head's ds for dX, an expert's ds so far, times 2^60 at most, for dW).  A bf16 x is one
 // fp16 value, exactly (down to 2^-31 of its row's largest).  Products of pieces kept:
 // w0 x, w1 x with a bf16 x; w0 x0, w0 x1, w1 x0 with an fp32 x (up to 2^-22 of the
 // product left out).  So a score takes 2 or 3 passes; in three bf16 pieces each it took 3 or 6
