@@ -718,10 +718,11 @@ mhlmoe_status mhlmoe_balance_loss(const void *X, const float *W_router,
  *   dW_router [n_heads][n_experts][d_head] float; not W_router        (out)
  * The other arguments are those of the mhlmoe_balance_loss call that wrote
  * stats.  dX_add (dW_add) is added in fp32 before the one rounding of dX.  Products
- * are of fp32 accuracy: off by up to 2^-22 of themselves.  What is far below its head's
- * largest has fewer bits: with D = dloss[h] / n, a term of dX may besides be off by
- * 2^-37 D R max |W_router[h]|, R = n_experts (max f - min f), and one of dW_router by
- * 2^-70 D.
+ * are of fp32 accuracy: off by up to 2^-21 of themselves.  What is far below the largest
+ * beside it has fewer bits: a value of X or W_router, here and in the scores, may be off
+ * by 2^-39 of the largest of its token's row or of up to 256 experts next to it; and, with
+ * D = dloss[h] / n, a term of dX by 2^-37 D R max |W_router[h]|, R = n_experts (max f -
+ * min f), and one of dW_router by 2^-70 D.
  */
 mhlmoe_status mhlmoe_balance_loss_backward_workspace(int64_t T, int n_heads,
                                                      int d_head, int n_experts,
