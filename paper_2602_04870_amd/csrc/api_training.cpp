@@ -78,9 +78,11 @@ BalanceLayout balance_layout(int64_t T, int n_heads, int d_head, int n_experts, 
   BalanceLayout L;
   size_t cur = 0;
   L.weights = bump(cur, mhl::balance_weight_bytes(n_heads, d_head, n_experts));
-  L.part = bump(cur, backward ? sizeof(float) *
-                                    (size_t)mhl::balance_splits(T, n_heads, d_head, n_experts) *
-                                    n_heads * mhl::balance_blocks(n_experts) * 32 * d_head
+  // dW's partial results (none where there is one: it is dW), or the loss's
+  const size_t splits = (size_t)mhl::balance_splits(T, n_heads, d_head, n_experts);
+  L.part = bump(cur, backward ? (splits == 1 ? 0
+                                             : sizeof(float) * splits * n_heads *
+                                                   mhl::balance_blocks(n_experts) * 32 * d_head)
                               : sizeof(double) * (size_t)n_heads *
                                     mhl::balance_token_blocks(T, n_heads, n_experts));
   L.total = cur;
