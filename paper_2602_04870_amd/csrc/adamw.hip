@@ -9,13 +9,13 @@
 // kernel arguments (one launch for kAdamTensors tensors, nothing to upload).
 //
 // States in 8 bits are m and sqrt(v), e4m3 with a scale per 128 elements (16 lanes
-// of 8 elements).  An update moves a state by a few percent or less, below half a
-// step of e4m3 (2^-4), so rounding to the nearest would leave it where it is; each
-// is rounded up with the probability of the part below the step instead, so that
-// it moves by the update on average.  The random numbers are a hash of the key
-// and the element's place, nothing is kept.  sqrt(v) is held rather than v: it has
-// half the exponents, and what is not zero is not rounded to zero, which would make
-// a step as large as m / eps.
+// of 8 elements).  m changes by (1 - b1) (g - m), v by (1 - b2) (g^2 - v): where the betas
+// are near 1, or g near m, often less than half a step of e4m3 (2^-4), and rounding to
+// the nearest would leave the state where it is.  Each is rounded up with the probability
+// of the part below the step instead, so that it moves by the update on average.  The
+// random numbers are a hash of the key and the element's place, nothing is kept.  sqrt(v)
+// is held rather than v: it has half the exponents, and what is not zero is not rounded
+// to zero, which would make a step as large as m / eps.
 //
 // The states' arithmetic is one rounding per operation, with no fused multiply-add:
 // an 8-bit value that falls on the other side of its random border is a whole step
