@@ -105,12 +105,14 @@ constexpr int kBalanceTokens = 128;  // per workgroup of the loss and of dX
 // us at 8 heads, d_h 128, bf16, so / with the weights laid out (a call of the loss and
 // the counts, of the gradient):
 //   tokens  experts   loss       gradient
-//      512    1024   28 / 40     35 / 71
-//     1024    1024   29 / 40     64 / 79
-//     2048      64   21 / 24     30 / 32
-//     2048     256   26 / 24     50 / 42
-//     4096      16   21 / 25     33 / 37
-//     4096      64   21 / 25     41 / 35
+//      512    1024   29 / 41     41 / 88
+//     1024    1024   31 / 41     70 / 91
+//     2048      64   23 / 25     31 / 24
+//     2048     256   27 / 24     53 / 48
+//     4096      16   24 / 27     35 / 28
+//     4096      64   24 / 28     43 / 26
+// (the limit is the loss's; the gradient of 2048 tokens and more with few experts would be
+// faster with the weights laid out).
 constexpr int kBalanceFewWaves = 8;
 inline bool balance_few(int64_t T, int Nh, int Ne) {
   const int64_t groups = Nh * ceil_div(T, 32);
@@ -139,18 +141,18 @@ inline bool balance_loss_at_once(int64_t T, int Nh, int Ne) {
 // them out over the tokens where there are fewer than three), and the chunks that the
 // tokens are cut into, of at least four tiles, so that there are eight wavefronts per
 // CU at once (us of the gradient in bf16 with 512 workgroups of four wavefronts and with
-// 1024: 122 and 138 at 16384 x 16 heads x 128 experts).  Eight blocks share the splitting of
-// their tokens' X (65536 x 8 x 1024: 942 us, with four 1017; d_h 64: 97, 94 at 16384 x
-// 16 x 200).
+// 1024: 128 and 138 at 16384 x 16 heads x 128 experts, 71 and 87 at 8000).  Eight blocks
+// share the splitting of their tokens' X (65536 x 8 x 1024: 1127 us, with four 1207;
+// 16384 x 16 x 256 188, 192; d_h 64: 3 us more at 16384 x 16 x 200).
 inline int balance_dw_blocks(int64_t T, int Nh, int dh, int Ne) {
   return Ne <= 32 ? 1 : Ne <= 64 ? 2 : Ne <= 128 || dh < 128 || balance_few(T, Nh, Ne) ? 4 : 8;
 }
 // Where not few tokens: dX and dW in one launch, whose workgroups then fill the card
 // together, unless dX loses too much by dW's registers and LDS.  us together / apart in
 // bf16 at 16 heads (fp32 alike):
-//   d_h   64: 33 / 39 at 3001 tokens x 200 experts, 84 / 93 at 32768 x 64
-//   d_h  128: 26 / 36 at 2000 x 100, 114 / 120 at 16384 x 128, 388 / 385 at 65536 x 128;
-//             30 / 38 at 2500 x 20, 48 / 45 at 6000 x 16, 112 / 95 at 16384 x 16
+//   d_h   64: 33 / 41 at 3001 tokens x 200 experts, 91 / 97 at 32768 x 64
+//   d_h  128: 28 / 38 at 2000 x 100, 124 / 132 at 16384 x 128, 443 / 435 at 65536 x 128;
+//             31 / 40 at 2500 x 20, 49 / 46 at 6000 x 16, 115 / 97 at 16384 x 16
 inline bool balance_together(int64_t T, int Nh, int dh, int Ne) {
   const int ew = balance_dw_blocks(T, Nh, dh, Ne);
   return ew <= 4 && (dh < 128 || Nh * ceil_div(T, kBalanceTokens) <= (ew == 1 ? 512 : 2048));
