@@ -722,7 +722,8 @@ mhlmoe_status mhlmoe_balance_loss(const void *X, const float *W_router,
  * beside it has fewer bits: a value of X or W_router, here and in the scores, may be off
  * by 2^-39 of the largest of its token's row or of up to 256 experts next to it; and, with
  * D = dloss[h] / n, a term of dX by 2^-37 D R max |W_router[h]|, R = n_experts (max f -
- * min f), and one of dW_router by 2^-70 D.
+ * min f), and one of dW_router by 2^-70 D.  p_t comes from the fp32 log sum in stats, so it
+ * is off by about 2^-22 times the token's largest |score|.
  */
 mhlmoe_status mhlmoe_balance_loss_backward_workspace(int64_t T, int n_heads,
                                                      int d_head, int n_experts,
